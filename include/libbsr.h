@@ -63,7 +63,11 @@ typedef enum {
                                beyond int32 element offsets)                                    */
 } bsr_status;
 
-typedef enum { BSR_F32 = 0, BSR_BF16 = 1 } bsr_dtype;
+typedef enum {
+    BSR_F32 = 0,
+    BSR_BF16 = 1,
+    BSR_I8 = 2 /* 8-bit integers with fp32 scales; only where an entry point names it */
+} bsr_dtype;
 
 /* A BSR matrix in device memory (all pointers device pointers, owned by the caller). */
 typedef struct {
@@ -459,6 +463,128 @@ LIBBSR_API bsr_status bsr_cast_f32_bf16(const float *src, uint16_t *dst, int64_t
 LIBBSR_API bsr_status bsr_iht_update(const float *W, int64_t ldw, const float *G, int64_t ldg,
                                      const float *C0, int64_t ldc, float eta, int64_t N,
                                      int64_t K, float *V, int64_t ldv, void *stream);
+
+/*
+ * Dense products with 8-bit operands: the other compression of a layer that stays dense.  A row x
+ * of an fp32 or bf16 matrix (a token of the activations, or an output channel of a weight) becomes
+ * integers q and one scale s with x ~ s q:
+ *   a = max |x_k| over the row;  s = a / 127;  r = 127 / a;  q_k = x_k r rounded to the nearest
+ *   integer, ties to even; every operation is rounded to fp32, so q and s are defined to the bit.
+ *   A row with a < 2^-64 is multiplied by 2^64 first (exact), for r and q only.  |q| <= 127.
+ * A row of zeros has q = 0 and s = 0.  A row that holds an infinity has s = infinity and q = 0; one
+ * that holds a NaN has s = NaN and q = 0: every output of a product with it is NaN.
+ * X: device, T x K of x_dtype (BSR_F32 or BSR_BF16), row pitch ldx >= K.  Q: device int8, T x K,
+ *   row pitch ldq >= K; columns from K on are not written.  scale: device fp32[T].  T = 0 is a
+ *   no-op; K >= 1.  Outputs must not overlap X or each other.
+ * Errors: BSR_ERR_NULL, BSR_ERR_SHAPE, BSR_ERR_ARG (unknown dtype, overlap), BSR_ERR_DTYPE
+ *   (BSR_I8), BSR_ERR_UNSUPPORTED (K or a pitch above 2^20, T above 2^24), BSR_ERR_ARCH,
+ *   BSR_ERR_HIP.
+ */
+LIBBSR_API bsr_status bsr_quantize_rows(const void *X, bsr_dtype x_dtype, int64_t T, int64_t K,
+                                        int64_t ldx, int8_t *Q, int64_t ldq, float *scale,
+                                        void *stream);
+
+/*
+ * The product of 8-bit rows with a scale for each token and each output channel:
+ *   Y[t][n] = sx[t] * sw[n] * sum over k of Xq[t][k] Wq[n][k]  +  bias[n].
+ * The integer sum is exact; it is converted to fp32, multiplied by sx[t], then by sw[n], and the
+ * bias added in fp32; bf16 output is rounded once from that (nearest, ties to even).  The result
+ * does not depend on how the work is split.
+ * Xq: device int8, T x K, row pitch ldx >= K.  Wq: device int8, N x K, row pitch ldw >= K (any
+ *   pitch and base; 16-byte aligned rows load faster).  sx: device fp32[T], sw: fp32[N], bias:
+ *   fp32[N] or NULL.  Y: device, T x N of y_dtype (BSR_F32 or BSR_BF16), row pitch ldy >= N.
+ * T = 0 is a no-op; N, K >= 1.  Y must not overlap an input.
+ * Errors: BSR_ERR_NULL, BSR_ERR_SHAPE, BSR_ERR_ARG (unknown dtype, overlap), BSR_ERR_DTYPE (y_dtype
+ *   BSR_I8), BSR_ERR_UNSUPPORTED (K above 131071, where the 32-bit sum could overflow; N or a pitch
+ *   above 2^20, T above 2^24, T * N above 2^37), BSR_ERR_ARCH, BSR_ERR_HIP.
+ */
+LIBBSR_API bsr_status bsr_matmul_i8(const int8_t *Xq, int64_t T, int64_t K, int64_t ldx,
+                                    const float *sx, const int8_t *Wq, int64_t N, int64_t ldw,
+                                    const float *sw, const float *bias, void *Y,
+                                    bsr_dtype y_dtype, int64_t ldy, void *stream);
+
+/* The activation of a gated feed-forward block. */
+typedef enum {
+    BSR_ACT_SILU = 0,      /* g / (1 + exp(-g))                                              */
+    BSR_ACT_GELU = 1,      /* g (1 + erf(g / sqrt 2)) / 2                                    */
+    BSR_ACT_GELU_TANH = 2, /* g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2              */
+    BSR_ACT_RELU = 3       /* max(g, 0), slope 0 at 0                                        */
+} bsr_act;
+
+/* The weights of a gated feed-forward block of input width K and hidden width F (all pointers
+ * device pointers, owned by the caller). */
+typedef struct {
+    int64_t K, F;            /* input width, hidden width                                     */
+    const void *Wg, *Wu;     /* F x K each: gate and up projection, of type `dtype`           */
+    int64_t ldg, ldu;        /* their row pitches in elements, >= K                           */
+    const float *sg, *su;    /* BSR_I8: fp32[F] scale of every row; NULL otherwise            */
+    const float *bg, *bu;    /* fp32[F] biases, each may be NULL (adds +0)                    */
+    bsr_dtype dtype;         /* BSR_F32 or BSR_BF16; BSR_I8 for bsr_gated_i8                  */
+    int32_t act;             /* a bsr_act value                                               */
+} bsr_gated_t;
+
+/*
+ * The gated feed-forward block up to its down projection (which is an ordinary product):
+ *   G = X Wg^T + bg,  U = X Wu^T + bu,  H = act(G) * U  elementwise,
+ * both projections, the activation and the product in one kernel.  fp32 accumulation; H is of the
+ * block's dtype, rounded once (bf16: nearest, ties to even).
+ * X: device, T x K of W->dtype, row pitch ldx.  H: device, T x F of W->dtype, row pitch ldh.
+ * G, U: device fp32, T x F with row pitch ldp, or both NULL: the pre-activations, kept for
+ *   bsr_gated_backward (fp32 also for bf16 blocks, so that the gradients are not those of rounded
+ *   pre-activations).
+ * fp32 blocks form their products in fp32 arithmetic.
+ * T = 0 is a no-op.  H, G and U must not overlap an input or each other.
+ * Errors: BSR_ERR_NULL (also: one of G and U without the other), BSR_ERR_SHAPE, BSR_ERR_ARG (unknown
+ *   dtype or activation, overlap), BSR_ERR_DTYPE (BSR_I8), BSR_ERR_UNSUPPORTED (K, F or a pitch
+ *   above 2^20, T above 2^24, T * F above 2^36), BSR_ERR_ARCH, BSR_ERR_HIP.
+ */
+LIBBSR_API bsr_status bsr_gated(const void *X, int64_t T, int64_t ldx, const bsr_gated_t *W,
+                                void *H, int64_t ldh, float *G, float *U, int64_t ldp,
+                                void *stream);
+
+/* Device workspace bytes of bsr_gated_backward for T tokens (0 if the sizes or the dtype are
+ * invalid).  Host only. */
+LIBBSR_API size_t bsr_gated_workspace_bytes(int64_t T, int64_t K, int64_t F, bsr_dtype dtype);
+
+/*
+ * The gradients of bsr_gated from dH, the gradient of H, and the pre-activations it kept:
+ *   dG = dH * U * act'(G),  dU = dH * act(G)  (fp32, then rounded to the block's dtype as operands
+ *   of the products below),
+ *   dX = dG Wg + dU Wu,  dWg = dG^T X,  dWu = dU^T X,
+ *   dbg[f] = sum over t of dG[t][f],  dbu[f] = sum over t of dU[t][f]  (of the unrounded values).
+ * Sums are fp32 in a fixed order: repeated calls are bitwise reproducible.
+ * dH: device, T x F of W->dtype, row pitch lddh.  X, W as in the forward call (biases are not
+ *   read).  G, U: device fp32, T x F, row pitch ldp, as bsr_gated wrote them.
+ * dX: device, T x K of W->dtype, row pitch lddx, or NULL (not wanted).
+ * dWg, dWu: device, F x K of grad_dtype (BSR_F32 or BSR_BF16), row pitch lddw, or both NULL.
+ * dbg, dbu: device, F elements of grad_dtype; each may be NULL.
+ * workspace: device memory of at least bsr_gated_workspace_bytes(T, K, F, W->dtype) bytes, 16-byte
+ *   aligned; its contents on entry do not matter.  It is in use until the enqueued work completes:
+ *   calls that may overlap in time (other streams, graphs replayed side by side) need one each.
+ * T = 0 sets the weight and bias gradients to zero.  Outputs and workspace must not overlap an input
+ * or each other.
+ * Errors: those of bsr_gated, BSR_ERR_NULL (one of dWg and dWu without the other), BSR_ERR_WORKSPACE
+ *   (missing, too small or misaligned), BSR_ERR_UNSUPPORTED (T above 2^20).
+ */
+LIBBSR_API bsr_status bsr_gated_backward(const void *dH, int64_t lddh, const void *X, int64_t T,
+                                         int64_t ldx, const bsr_gated_t *W, const float *G,
+                                         const float *U, int64_t ldp, void *dX, int64_t lddx,
+                                         void *dWg, void *dWu, int64_t lddw, void *dbg, void *dbu,
+                                         bsr_dtype grad_dtype, void *workspace, size_t ws_bytes,
+                                         void *stream);
+
+/*
+ * The gated block on 8-bit rows, for serving: G and U as in bsr_matmul_i8 (exact integer sums,
+ * scaled by sx[t] and the row's sg[f] or su[f], plus the bias), H = act(G) * U in fp32, rounded
+ * once to h_dtype.
+ * Xq: device int8, T x W->K, row pitch ldx; sx: device fp32[T].  W: dtype BSR_I8, with sg and su.
+ * H: device, T x F of h_dtype (BSR_F32 or BSR_BF16), row pitch ldh.  T = 0 is a no-op.
+ * Errors: as bsr_gated; BSR_ERR_DTYPE (W->dtype not BSR_I8, or h_dtype BSR_I8),
+ *   BSR_ERR_UNSUPPORTED (also K above 131071).
+ */
+LIBBSR_API bsr_status bsr_gated_i8(const int8_t *Xq, int64_t T, int64_t ldx, const float *sx,
+                                   const bsr_gated_t *W, void *H, bsr_dtype h_dtype, int64_t ldh,
+                                   void *stream);
 
 /* Static, human-readable name of a status code. */
 LIBBSR_API const char *bsr_status_str(bsr_status s);

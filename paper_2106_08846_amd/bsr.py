@@ -15,7 +15,7 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIBRARY = os.path.join(_HERE, "libbsr.so")
 
-BSR_F32, BSR_BF16 = 0, 1
+BSR_F32, BSR_BF16, BSR_I8 = 0, 1, 2
 _I32, _F32 = torch.int32, torch.float32
 _DATA_DTYPES = (torch.float32, torch.bfloat16)
 STATUS = {0: "BSR_OK", 1: "BSR_ERR_NULL", 2: "BSR_ERR_SHAPE", 3: "BSR_ERR_ARG",
@@ -30,11 +30,14 @@ EXPORTS = ["bsr_prune_count", "bsr_prune_count_ex", "bsr_prune_workspace_bytes",
            "bsr_plan_prepare_ex", "bsr_spmm_batched_planned", "bsr_attention", "bsr_reblock",
            "bsr_to_dense",
            "bsr_cast_f32_bf16", "bsr_iht_update",
+           "bsr_quantize_rows", "bsr_matmul_i8", "bsr_gated", "bsr_gated_workspace_bytes",
+           "bsr_gated_backward", "bsr_gated_i8",
            "bsr_status_str", "bsr_last_hip_error"]
 NORM_L2, NORM_L1 = 0, 1
 SELECT_GLOBAL, SELECT_PER_ROW = 0, 1
 KERNEL_AUTO, KERNEL_GENERIC, KERNEL_TILED, KERNEL_VALU = 0, 1, 2, 3
 ARITH_AUTO, ARITH_NATIVE, ARITH_BF16X3 = 0, 1, 2
+ACTS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3}
 
 
 class BSRError(RuntimeError):
@@ -78,6 +81,15 @@ class bsr_plan_t(ctypes.Structure):
                 ("max_units", ctypes.c_int64), ("uptr_offset", ctypes.c_int64),
                 ("col_offset", ctypes.c_int64), ("val_offset", ctypes.c_int64),
                 ("arith", ctypes.c_int32)]
+
+
+class bsr_gated_t(ctypes.Structure):
+    _fields_ = [("K", ctypes.c_int64), ("F", ctypes.c_int64),
+                ("Wg", ctypes.c_void_p), ("Wu", ctypes.c_void_p),
+                ("ldg", ctypes.c_int64), ("ldu", ctypes.c_int64),
+                ("sg", ctypes.c_void_p), ("su", ctypes.c_void_p),
+                ("bg", ctypes.c_void_p), ("bu", ctypes.c_void_p),
+                ("dtype", ctypes.c_int), ("act", ctypes.c_int32)]
 
 
 _LIB = None
@@ -145,6 +157,20 @@ def _lib() -> ctypes.CDLL:
         lib.bsr_iht_update.argtypes = [p, i64, p, i64, p, i64, ctypes.c_float, i64, i64, p, i64,
                                        p]
         lib.bsr_iht_update.restype = st
+        lib.bsr_quantize_rows.argtypes = [p, st, i64, i64, i64, p, i64, p, p]
+        lib.bsr_quantize_rows.restype = st
+        lib.bsr_matmul_i8.argtypes = [p, i64, i64, i64, p, p, i64, i64, p, p, p, st, i64, p]
+        lib.bsr_matmul_i8.restype = st
+        block = ctypes.POINTER(bsr_gated_t)
+        lib.bsr_gated.argtypes = [p, i64, i64, block, p, i64, p, p, i64, p]
+        lib.bsr_gated.restype = st
+        lib.bsr_gated_workspace_bytes.argtypes = [i64, i64, i64, st]
+        lib.bsr_gated_workspace_bytes.restype = sz
+        lib.bsr_gated_backward.argtypes = [p, i64, p, i64, i64, block, p, p, i64, p, i64, p, p,
+                                           i64, p, p, st, p, sz, p]
+        lib.bsr_gated_backward.restype = st
+        lib.bsr_gated_i8.argtypes = [p, i64, i64, p, block, p, st, i64, p]
+        lib.bsr_gated_i8.restype = st
         lib.bsr_status_str.argtypes = [ctypes.c_int]
         lib.bsr_status_str.restype = ctypes.c_char_p
         lib.bsr_last_hip_error.argtypes = []
@@ -772,3 +798,252 @@ def bsr_cast_f32_bf16(src: torch.Tensor, dst: torch.Tensor | None = None,
     _check(_lib().bsr_cast_f32_bf16(_ptr(src), _ptr(dst), src.numel(), _stream(stream)),
            "bsr_cast_f32_bf16")
     return dst
+
+
+_DTYPE_CODE = {torch.float32: BSR_F32, torch.bfloat16: BSR_BF16, torch.int8: BSR_I8}
+
+
+def _matrix_arg(t, name: str, rows: int | None, cols: int | None, dtypes) -> int:
+    """Check a 2-D argument of the dense products (None: any size); returns its row pitch."""
+    if (not isinstance(t, torch.Tensor) or t.dim() != 2
+            or (rows is not None and t.shape[0] != rows)
+            or (cols is not None and t.shape[1] != cols)):
+        raise ValueError(f"{name} must be [{'T' if rows is None else rows}, "
+                         f"{'K' if cols is None else cols}]")
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name} must be {' or '.join(str(d) for d in dtypes)}, got {t.dtype}")
+    ld = _pitch(t, name)
+    if ld < t.shape[1]:     # expanded or overlapping rows
+        raise ValueError(f"{name}'s rows overlap (row stride {ld} < {t.shape[1]} columns)")
+    return ld
+
+
+def _vector_arg(t, name: str, n: int, dtype=torch.float32):
+    if t is None:
+        return
+    if (not isinstance(t, torch.Tensor) or t.dim() != 1 or t.numel() != n
+            or not t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous [{n}] tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+
+
+def _one_device(*tensors) -> None:
+    """Every given tensor is on the current GPU, whose stream the work is enqueued on."""
+    dev = None
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise TypeError("every tensor must be a CUDA (HIP) tensor")
+        if dev is None:
+            dev = t.device
+            now = _cur_device() if _cur_device is not None else torch.cuda.current_device()
+            if dev.index != now:
+                raise ValueError(f"the tensors are on {dev}, the current device is cuda:{now}: "
+                                 "make theirs current (torch.cuda.device)")
+        elif t.device != dev:
+            raise ValueError(f"tensors on {dev} and on {t.device} in one call")
+
+
+def _on_stream(stream, *tensors) -> int | None:
+    """The call's raw stream.  Tensors that the binding allocated (on torch's current stream) are
+    recorded on it when it is another one, so that torch keeps their memory until it has run."""
+    st = _stream(stream)
+    made = [t for t in tensors if t is not None]
+    if stream is not None and made and st != torch.cuda.current_stream().cuda_stream:
+        side = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(st)
+        side.wait_stream(torch.cuda.current_stream())   # memory the allocator reuses is free there
+        for t in made:
+            t.record_stream(side)
+    return st
+
+
+def bsr_quantize_rows(X: torch.Tensor, Q: torch.Tensor | None = None,
+                      scale: torch.Tensor | None = None, stream=None):
+    """X's rows in 8 bits (bsr_quantize_rows): returns (Q int8 [T, K], scale fp32 [T]) with
+    X ~ scale[:, None] * Q.  X is float32 or bfloat16; it may be activations, or a weight whose rows
+    are its output channels."""
+    ldx = _matrix_arg(X, "X", None, None, _DATA_DTYPES)
+    T, K = X.shape
+    made = []
+    if Q is None:
+        Q = torch.empty((T, K), dtype=torch.int8, device=X.device)
+        made.append(Q)
+    if scale is None:
+        scale = torch.empty((T,), dtype=_F32, device=X.device)
+        made.append(scale)
+    ldq = _matrix_arg(Q, "Q", T, K, (torch.int8,))
+    _vector_arg(scale, "scale", T)
+    _one_device(X, Q, scale)
+    _check(_lib().bsr_quantize_rows(_ptr(X), _DTYPE_CODE[X.dtype], T, K, ldx, _ptr(Q), ldq,
+                                    _ptr(scale), _on_stream(stream, *made)), "bsr_quantize_rows")
+    return Q, scale
+
+
+def bsr_matmul_i8(Xq: torch.Tensor, sx: torch.Tensor, Wq: torch.Tensor, sw: torch.Tensor,
+                  bias: torch.Tensor | None = None, Y: torch.Tensor | None = None,
+                  out_dtype: torch.dtype = torch.float32, stream=None) -> torch.Tensor:
+    """Y = diag(sx) Xq Wq^T diag(sw) + bias from 8-bit rows (bsr_matmul_i8): Xq int8 [T, K], Wq int8
+    [N, K], scales and bias fp32; Y float32 or bfloat16 (out_dtype, when Y is None)."""
+    ldx = _matrix_arg(Xq, "Xq", None, None, (torch.int8,))
+    T, K = Xq.shape
+    ldw = _matrix_arg(Wq, "Wq", None, K, (torch.int8,))
+    N = Wq.shape[0]
+    _vector_arg(sx, "sx", T)
+    _vector_arg(sw, "sw", N)
+    _vector_arg(bias, "bias", N)
+    if sx is None or sw is None:
+        raise ValueError("give both scales")
+    made = None
+    if Y is None:
+        Y = made = torch.empty((T, N), dtype=out_dtype, device=Xq.device)
+    ldy = _matrix_arg(Y, "Y", T, N, _DATA_DTYPES)
+    _one_device(Xq, sx, Wq, sw, bias, Y)
+    _check(_lib().bsr_matmul_i8(_ptr(Xq), T, K, ldx, _ptr(sx), _ptr(Wq), N, ldw, _ptr(sw),
+                                _ptr(bias), _ptr(Y), _DTYPE_CODE[Y.dtype], ldy,
+                                _on_stream(stream, made)), "bsr_matmul_i8")
+    return Y
+
+
+def _gated_block(X, Wg, Wu, sg, su, bg, bu, act: str, dtypes) -> bsr_gated_t:
+    """Check a gated block's weights against X and describe them for the C side (the caller checks
+    the devices)."""
+    if act not in ACTS:
+        raise ValueError(f"act must be one of {', '.join(ACTS)}")
+    _matrix_arg(X, "X", None, None, dtypes)
+    K = X.shape[1]
+    ldg = _matrix_arg(Wg, "Wg", None, K, (X.dtype,))
+    F = Wg.shape[0]
+    ldu = _matrix_arg(Wu, "Wu", F, K, (X.dtype,))
+    for t, name in ((sg, "sg"), (su, "su"), (bg, "bg"), (bu, "bu")):
+        _vector_arg(t, name, F)
+    return bsr_gated_t(K, F, _ptr(Wg), _ptr(Wu), ldg, ldu, _ptr(sg), _ptr(su), _ptr(bg), _ptr(bu),
+                       _DTYPE_CODE[X.dtype], ACTS[act])
+
+
+def bsr_gated(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor,
+              bg: torch.Tensor | None = None, bu: torch.Tensor | None = None, act: str = "silu",
+              save: bool = False, H: torch.Tensor | None = None, G: torch.Tensor | None = None,
+              U: torch.Tensor | None = None, stream=None):
+    """The gated feed-forward block H = act(X Wg^T + bg) * (X Wu^T + bu) in one kernel (bsr_gated):
+    X [T, K], Wg and Wu [F, K], all float32 or all bfloat16, biases fp32; H [T, F] of X's type.
+    act: "silu", "gelu", "gelu_tanh" or "relu".  With save (or G and U given) returns (H, G, U), G and
+    U the fp32 pre-activations that bsr_gated_backward reads; otherwise H."""
+    block = _gated_block(X, Wg, Wu, None, None, bg, bu, act, _DATA_DTYPES)
+    T, F = X.shape[0], block.F
+    if (G is None) != (U is None):
+        raise ValueError("give both G and U, or neither")
+    made = []
+    if H is None:
+        H = torch.empty((T, F), dtype=X.dtype, device=X.device)
+        made.append(H)
+    ldp = 0
+    if save and G is None:
+        G = torch.empty((T, F), dtype=_F32, device=X.device)
+        U = torch.empty((T, F), dtype=_F32, device=X.device)
+        made += [G, U]
+    ldh = _matrix_arg(H, "H", T, F, (X.dtype,))
+    if G is not None:
+        ldp = _matrix_arg(G, "G", T, F, (_F32,))
+        if _matrix_arg(U, "U", T, F, (_F32,)) != ldp:
+            raise ValueError("G and U must have the same row pitch")
+    _one_device(X, Wg, Wu, bg, bu, H, G, U)
+    _check(_lib().bsr_gated(_ptr(X), T, _pitch(X, "X"), ctypes.byref(block), _ptr(H), ldh, _ptr(G),
+                            _ptr(U), ldp, _on_stream(stream, *made)), "bsr_gated")
+    return H if G is None else (H, G, U)
+
+
+def bsr_gated_workspace_bytes(T: int, K: int, F: int, dtype: torch.dtype) -> int:
+    """Device bytes of bsr_gated_backward's workspace."""
+    return int(_lib().bsr_gated_workspace_bytes(T, K, F, _DTYPE_CODE[dtype]))
+
+
+def bsr_gated_backward(dH: torch.Tensor, X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor,
+                       G: torch.Tensor, U: torch.Tensor, act: str = "silu", bias: bool = False,
+                       dX: torch.Tensor | None = None, dWg: torch.Tensor | None = None,
+                       dWu: torch.Tensor | None = None, dbg: torch.Tensor | None = None,
+                       dbu: torch.Tensor | None = None, grad_dtype: torch.dtype | None = None,
+                       need=("X", "W"), workspace: torch.Tensor | None = None, stream=None):
+    """The gradients of bsr_gated (bsr_gated_backward) from dH, the gradient of H, and the G and U
+    that the forward call saved: returns (dX, dWg, dWu, dbg, dbu).
+
+    `need` names what is wanted of "X" (dX) and "W" (dWg and dWu), `bias` whether the bias gradients
+    are; what is not wanted is None.  Weight and bias gradients are of grad_dtype (default: X's type;
+    float32 suits bsr_iht_update and fp32 master weights), allocated here unless given.  `workspace`
+    is a uint8 device tensor of bsr_gated_workspace_bytes, allocated here when None; calls that may
+    overlap in time need one each."""
+    block = _gated_block(X, Wg, Wu, None, None, None, None, act, _DATA_DTYPES)
+    T, K, F = X.shape[0], block.K, block.F
+    if any(n not in ("X", "W") for n in need):
+        raise ValueError('need may name "X" and "W"')
+    if (dWg is None) != (dWu is None):
+        raise ValueError("give both dWg and dWu, or neither")
+    lddh = _matrix_arg(dH, "dH", T, F, (X.dtype,))
+    ldp = _matrix_arg(G, "G", T, F, (_F32,))
+    if _matrix_arg(U, "U", T, F, (_F32,)) != ldp:
+        raise ValueError("G and U must have the same row pitch")
+    given = next((t for t in (dWg, dbg, dbu) if t is not None), None)
+    if grad_dtype is None:
+        grad_dtype = X.dtype if given is None else given.dtype
+    if grad_dtype not in _DATA_DTYPES:
+        raise TypeError("grad_dtype must be float32 or bfloat16")
+    made = []
+
+    def make(*shape, dtype):
+        made.append(torch.empty(shape, dtype=dtype, device=X.device))
+        return made[-1]
+
+    if "X" in need and dX is None:
+        dX = make(T, K, dtype=X.dtype)
+    if "W" in need and dWg is None:
+        dWg, dWu = make(F, K, dtype=grad_dtype), make(F, K, dtype=grad_dtype)
+    if bias and dbg is None:
+        dbg = make(F, dtype=grad_dtype)
+    if bias and dbu is None:
+        dbu = make(F, dtype=grad_dtype)
+    lddx = lddw = 0
+    if dX is not None:
+        lddx = _matrix_arg(dX, "dX", T, K, (X.dtype,))
+    if dWg is not None:
+        lddw = _matrix_arg(dWg, "dWg", F, K, (grad_dtype,))
+        if _matrix_arg(dWu, "dWu", F, K, (grad_dtype,)) != lddw:
+            raise ValueError("dWg and dWu must have the same row pitch")
+    _vector_arg(dbg, "dbg", F, grad_dtype)
+    _vector_arg(dbu, "dbu", F, grad_dtype)
+    nbytes = bsr_gated_workspace_bytes(T, K, F, X.dtype)
+    if workspace is None:
+        workspace = make(max(nbytes, 1), dtype=torch.uint8)
+    if (not isinstance(workspace, torch.Tensor) or workspace.dtype != torch.uint8
+            or workspace.dim() != 1 or not workspace.is_contiguous()):
+        raise ValueError("workspace must be a contiguous uint8 tensor")
+    _one_device(dH, X, Wg, Wu, G, U, dX, dWg, dWu, dbg, dbu, workspace)
+    _check(_lib().bsr_gated_backward(_ptr(dH), lddh, _ptr(X), T, _pitch(X, "X"),
+                                     ctypes.byref(block), _ptr(G), _ptr(U), ldp, _ptr(dX), lddx,
+                                     _ptr(dWg), _ptr(dWu), lddw, _ptr(dbg), _ptr(dbu),
+                                     _DTYPE_CODE[grad_dtype], _ptr(workspace), workspace.numel(),
+                                     _on_stream(stream, *made)), "bsr_gated_backward")
+    return dX, dWg, dWu, dbg, dbu
+
+
+def bsr_gated_i8(Xq: torch.Tensor, sx: torch.Tensor, Wgq: torch.Tensor, sg: torch.Tensor,
+                 Wuq: torch.Tensor, su: torch.Tensor, bg: torch.Tensor | None = None,
+                 bu: torch.Tensor | None = None, act: str = "silu",
+                 H: torch.Tensor | None = None, out_dtype: torch.dtype = torch.bfloat16,
+                 stream=None) -> torch.Tensor:
+    """The gated block from 8-bit rows (bsr_gated_i8): Xq int8 [T, K] with sx fp32 [T], Wgq and Wuq
+    int8 [F, K] with sg and su fp32 [F]; H float32 or bfloat16 (out_dtype, when H is None)."""
+    if sg is None or su is None or sx is None:
+        raise ValueError("give every scale")
+    block = _gated_block(Xq, Wgq, Wuq, sg, su, bg, bu, act, (torch.int8,))
+    T, F = Xq.shape[0], block.F
+    _vector_arg(sx, "sx", T)
+    made = None
+    if H is None:
+        H = made = torch.empty((T, F), dtype=out_dtype, device=Xq.device)
+    ldh = _matrix_arg(H, "H", T, F, _DATA_DTYPES)
+    _one_device(Xq, sx, Wgq, sg, Wuq, su, bg, bu, H)
+    _check(_lib().bsr_gated_i8(_ptr(Xq), T, _pitch(Xq, "Xq"), _ptr(sx), ctypes.byref(block),
+                               _ptr(H), _DTYPE_CODE[H.dtype], ldh, _on_stream(stream, made)),
+           "bsr_gated_i8")
+    return H

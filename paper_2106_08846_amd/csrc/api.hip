@@ -494,4 +494,62 @@ bsr_status bsr_cast_f32_bf16(const float *src, uint16_t *dst, int64_t n, void *s
     return bsr::launch_cast(src, dst, n, stream);
 }
 
+bsr_status bsr_quantize_rows(const void *X, bsr_dtype x_dtype, int64_t T, int64_t K, int64_t ldx,
+                             int8_t *Q, int64_t ldq, float *scale, void *stream) {
+    const int32_t dt = bsr::raw_enum(x_dtype);
+    bsr_status s = bsr::check_quantize_rows(X, dt, T, K, ldx, Q, ldq, scale);
+    if (s != BSR_OK) return s;
+    if (T == 0) return BSR_OK;
+    if ((s = bsr::ensure_device()) != BSR_OK) return s;
+    return bsr::launch_quantize_rows(X, dt, T, K, ldx, Q, ldq, scale, stream);
+}
+
+bsr_status bsr_matmul_i8(const int8_t *Xq, int64_t T, int64_t K, int64_t ldx, const float *sx,
+                         const int8_t *Wq, int64_t N, int64_t ldw, const float *sw,
+                         const float *bias, void *Y, bsr_dtype y_dtype, int64_t ldy,
+                         void *stream) {
+    const int32_t dt = bsr::raw_enum(y_dtype);
+    bsr_status s = bsr::check_matmul_i8(Xq, T, K, ldx, sx, Wq, N, ldw, sw, bias, Y, dt, ldy);
+    if (s != BSR_OK) return s;
+    if (T == 0) return BSR_OK;
+    if ((s = bsr::ensure_device()) != BSR_OK) return s;
+    return bsr::launch_matmul_i8(Xq, T, K, ldx, sx, Wq, N, ldw, sw, bias, Y, dt, ldy, stream);
+}
+
+bsr_status bsr_gated(const void *X, int64_t T, int64_t ldx, const bsr_gated_t *W, void *H,
+                     int64_t ldh, float *G, float *U, int64_t ldp, void *stream) {
+    bsr_status s = bsr::check_gated(X, T, ldx, W, H, ldh, G, U, ldp);
+    if (s != BSR_OK) return s;
+    if (T == 0) return BSR_OK;
+    if ((s = bsr::ensure_device()) != BSR_OK) return s;
+    return bsr::launch_gated(X, T, ldx, *W, H, ldh, G, U, ldp, stream);
+}
+
+bsr_status bsr_gated_backward(const void *dH, int64_t lddh, const void *X, int64_t T, int64_t ldx,
+                              const bsr_gated_t *W, const float *G, const float *U, int64_t ldp,
+                              void *dX, int64_t lddx, void *dWg, void *dWu, int64_t lddw,
+                              void *dbg, void *dbu, bsr_dtype grad_dtype, void *workspace,
+                              size_t ws_bytes, void *stream) {
+    const int32_t gd = bsr::raw_enum(grad_dtype);
+    bsr_status s = bsr::check_gated_backward(dH, lddh, X, T, ldx, W, G, U, ldp, dX, lddx, dWg,
+                                             dWu, lddw, dbg, dbu, gd, workspace, ws_bytes);
+    if (s != BSR_OK) return s;
+    if (!dX && !dWg && !dbg && !dbu) return BSR_OK;
+    if (T == 0 && !dWg && !dbg && !dbu) return BSR_OK;
+    if ((s = bsr::ensure_device()) != BSR_OK) return s;
+    return bsr::launch_gated_backward(dH, lddh, X, T, ldx, *W, G, U, ldp, dX, lddx, dWg, dWu,
+                                      lddw, dbg, dbu, gd, workspace, stream);
+}
+
+bsr_status bsr_gated_i8(const int8_t *Xq, int64_t T, int64_t ldx, const float *sx,
+                        const bsr_gated_t *W, void *H, bsr_dtype h_dtype, int64_t ldh,
+                        void *stream) {
+    const int32_t dt = bsr::raw_enum(h_dtype);
+    bsr_status s = bsr::check_gated_i8(Xq, T, ldx, sx, W, H, dt, ldh);
+    if (s != BSR_OK) return s;
+    if (T == 0) return BSR_OK;
+    if ((s = bsr::ensure_device()) != BSR_OK) return s;
+    return bsr::launch_gated_i8(Xq, T, ldx, sx, *W, H, dt, ldh, stream);
+}
+
 }  // extern "C"

@@ -73,6 +73,36 @@ bsr_status check_attention(const float *Q, int64_t ldq, const float *K, int64_t 
                            int32_t batch, int32_t seq, int32_t heads, int32_t head_dim,
                            float scale);
 
+// The dense products (8-bit and gated): limits that keep every tile's byte offsets in 32 bits (a
+// tile spans at most 256 rows of at most 4 MiB) and every grid below 2^22 workgroups.
+constexpr int64_t kDenseMaxWidth = int64_t(1) << 20;    // columns and pitches, elements
+constexpr int64_t kDenseMaxTokens = int64_t(1) << 24;
+constexpr int64_t kDenseMaxOut = int64_t(1) << 37;      // elements of all outputs of one tile grid
+constexpr int64_t kGatedMaxBackwardTokens = int64_t(1) << 20;   // T is a pitch of the transposes
+constexpr int64_t kI8MaxK = 131071;                     // 2^14 * K stays below 2^31
+bsr_status check_quantize_rows(const void *X, int32_t x_dtype, int64_t T, int64_t K, int64_t ldx,
+                               const int8_t *Q, int64_t ldq, const float *scale);
+bsr_status check_matmul_i8(const int8_t *Xq, int64_t T, int64_t K, int64_t ldx, const float *sx,
+                           const int8_t *Wq, int64_t N, int64_t ldw, const float *sw,
+                           const float *bias, const void *Y, int32_t y_dtype, int64_t ldy);
+bsr_status check_gated(const void *X, int64_t T, int64_t ldx, const bsr_gated_t *W, const void *H,
+                       int64_t ldh, const float *G, const float *U, int64_t ldp);
+bsr_status check_gated_i8(const int8_t *Xq, int64_t T, int64_t ldx, const float *sx,
+                          const bsr_gated_t *W, const void *H, int32_t h_dtype, int64_t ldh);
+bsr_status check_gated_backward(const void *dH, int64_t lddh, const void *X, int64_t T,
+                                int64_t ldx, const bsr_gated_t *W, const float *G, const float *U,
+                                int64_t ldp, const void *dX, int64_t lddx, const void *dWg,
+                                const void *dWu, int64_t lddw, const void *dbg, const void *dbu,
+                                int32_t grad_dtype, const void *workspace, size_t ws_bytes);
+// Workspace of bsr_gated_backward: byte offsets of its regions, each on a 256-byte boundary.
+struct GatedWorkspace {
+    size_t grad_offset;    // [T][2F]: dG | dU, of the block's dtype
+    size_t partial_offset; // fp32 [row blocks][2F]: partial bias gradients
+    size_t total;
+};
+constexpr int kGatedRowsPerPartial = 64;
+GatedWorkspace gated_workspace_layout(int64_t T, int64_t K, int64_t F, int32_t dtype);
+
 // Device-side entry points (implemented in the .hip files).  Arguments are already validated.
 bsr_status ensure_device();  // current device is gfx950; caches its properties
 int device_cu_count();
@@ -102,6 +132,21 @@ bsr_status launch_spmm_generic(const void *X, int64_t T, int64_t ldx, const bsr_
 bsr_status launch_attention(const float *Q, int64_t ldq, const float *K, int64_t ldk,
                             const float *V, int64_t ldv, float *O, int64_t ldo, int batch,
                             int seq, int heads, float scale, void *stream);
+
+bsr_status launch_quantize_rows(const void *X, int x_dtype, int64_t T, int64_t K, int64_t ldx,
+                                int8_t *Q, int64_t ldq, float *scale, void *stream);
+bsr_status launch_matmul_i8(const int8_t *Xq, int64_t T, int64_t K, int64_t ldx, const float *sx,
+                            const int8_t *Wq, int64_t N, int64_t ldw, const float *sw,
+                            const float *bias, void *Y, int y_dtype, int64_t ldy, void *stream);
+bsr_status launch_gated(const void *X, int64_t T, int64_t ldx, const bsr_gated_t &W, void *H,
+                        int64_t ldh, float *G, float *U, int64_t ldp, void *stream);
+bsr_status launch_gated_i8(const int8_t *Xq, int64_t T, int64_t ldx, const float *sx,
+                           const bsr_gated_t &W, void *H, int h_dtype, int64_t ldh, void *stream);
+bsr_status launch_gated_backward(const void *dH, int64_t lddh, const void *X, int64_t T,
+                                 int64_t ldx, const bsr_gated_t &W, const float *G,
+                                 const float *U, int64_t ldp, void *dX, int64_t lddx, void *dWg,
+                                 void *dWu, int64_t lddw, void *dbg, void *dbu, int grad_dtype,
+                                 void *workspace, void *stream);
 
 void set_last_hip_error(const char *msg);
 

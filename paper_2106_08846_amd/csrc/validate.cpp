@@ -271,9 +271,175 @@ bsr_status check_attention(const float *Q, int64_t ldq, const float *K, int64_t 
     return BSR_OK;
 }
 
+namespace {
+
+// A byte range that a call reads or writes.
+struct Span {
+    const void *p;
+    int64_t bytes;
+};
+
+// `rows` rows of `width` elements of `size` bytes at pitch ld (sizes checked before).
+Span span(const void *p, int64_t rows, int64_t ld, int64_t width, int64_t size) {
+    return Span{p, rows > 0 ? ((rows - 1) * ld + width) * size : 0};
+}
+
+// No output overlaps an input or another output.
+template <size_t I, size_t O>
+bool disjoint(const Span (&in)[I], const Span (&out)[O]) {
+    for (size_t i = 0; i < O; ++i) {
+        for (size_t j = 0; j < I; ++j)
+            if (overlaps(out[i].p, out[i].bytes, in[j].p, in[j].bytes)) return false;
+        for (size_t j = i + 1; j < O; ++j)
+            if (overlaps(out[i].p, out[i].bytes, out[j].p, out[j].bytes)) return false;
+    }
+    return true;
+}
+
+bool known_dtype(int32_t d) { return d == BSR_F32 || d == BSR_BF16 || d == BSR_I8; }
+int64_t dtype_size(int32_t d) { return d == BSR_F32 ? 4 : d == BSR_BF16 ? 2 : 1; }
+
+// The block's own description, for a call whose operands are 8-bit or not; `T` bounds its outputs.
+bsr_status check_gated_block(const bsr_gated_t *W, bool i8, int64_t T, int64_t ldx) {
+    if (!W) return BSR_ERR_NULL;
+    const int32_t dt = raw_enum(W->dtype);
+    if (!known_dtype(dt) || W->act < BSR_ACT_SILU || W->act > BSR_ACT_RELU) return BSR_ERR_ARG;
+    if ((dt == BSR_I8) != i8) return BSR_ERR_DTYPE;
+    if (W->K < 1 || W->F < 1 || T < 0 || W->ldg < W->K || W->ldu < W->K || ldx < W->K)
+        return BSR_ERR_SHAPE;
+    if (W->K > kDenseMaxWidth || W->F > kDenseMaxWidth || W->ldg > kDenseMaxWidth ||
+        W->ldu > kDenseMaxWidth || ldx > kDenseMaxWidth || T > kDenseMaxTokens ||
+        W->F * T > kDenseMaxOut / 2 || (i8 && W->K > kI8MaxK))
+        return BSR_ERR_UNSUPPORTED;
+    if (!W->Wg || !W->Wu || (i8 && (!W->sg || !W->su))) return BSR_ERR_NULL;
+    return BSR_OK;
+}
+
+}  // namespace
+
+bsr_status check_quantize_rows(const void *X, int32_t x_dtype, int64_t T, int64_t K, int64_t ldx,
+                               const int8_t *Q, int64_t ldq, const float *scale) {
+    if (!known_dtype(x_dtype)) return BSR_ERR_ARG;
+    if (x_dtype == BSR_I8) return BSR_ERR_DTYPE;
+    if (T < 0 || K < 1 || ldx < K || ldq < K) return BSR_ERR_SHAPE;
+    if (ldx > kDenseMaxWidth || ldq > kDenseMaxWidth || T > kDenseMaxTokens)
+        return BSR_ERR_UNSUPPORTED;
+    if (T == 0) return BSR_OK;
+    if (!X || !Q || !scale) return BSR_ERR_NULL;
+    const Span in[] = {span(X, T, ldx, K, dtype_size(x_dtype))};
+    const Span out[] = {span(Q, T, ldq, K, 1), span(scale, 1, T, T, 4)};
+    return disjoint(in, out) ? BSR_OK : BSR_ERR_ARG;
+}
+
+bsr_status check_matmul_i8(const int8_t *Xq, int64_t T, int64_t K, int64_t ldx, const float *sx,
+                           const int8_t *Wq, int64_t N, int64_t ldw, const float *sw,
+                           const float *bias, const void *Y, int32_t y_dtype, int64_t ldy) {
+    if (!known_dtype(y_dtype)) return BSR_ERR_ARG;
+    if (y_dtype == BSR_I8) return BSR_ERR_DTYPE;
+    if (T < 0 || K < 1 || N < 1 || ldx < K || ldw < K || ldy < N) return BSR_ERR_SHAPE;
+    if (K > kI8MaxK || ldx > kDenseMaxWidth || ldw > kDenseMaxWidth || ldy > kDenseMaxWidth ||
+        T > kDenseMaxTokens || T * N > kDenseMaxOut)
+        return BSR_ERR_UNSUPPORTED;
+    if (T == 0) return BSR_OK;
+    if (!Xq || !sx || !Wq || !sw || !Y) return BSR_ERR_NULL;
+    const Span in[] = {span(Xq, T, ldx, K, 1), span(Wq, N, ldw, K, 1), span(sx, 1, T, T, 4),
+                       span(sw, 1, N, N, 4), span(bias, 1, N, N, 4)};
+    const Span out[] = {span(Y, T, ldy, N, dtype_size(y_dtype))};
+    return disjoint(in, out) ? BSR_OK : BSR_ERR_ARG;
+}
+
+bsr_status check_gated(const void *X, int64_t T, int64_t ldx, const bsr_gated_t *W, const void *H,
+                       int64_t ldh, const float *G, const float *U, int64_t ldp) {
+    const bsr_status s = check_gated_block(W, false, T, ldx);
+    if (s != BSR_OK) return s;
+    const bool keep = G || U;
+    if (ldh < W->F || (keep && ldp < W->F)) return BSR_ERR_SHAPE;
+    if (ldh > kDenseMaxWidth || (keep && ldp > kDenseMaxWidth)) return BSR_ERR_UNSUPPORTED;
+    if (T == 0) return BSR_OK;
+    if (!X || !H || (keep && (!G || !U))) return BSR_ERR_NULL;
+    const int64_t e = dtype_size(raw_enum(W->dtype)), K = W->K, F = W->F;
+    const Span in[] = {span(X, T, ldx, K, e), span(W->Wg, F, W->ldg, K, e),
+                       span(W->Wu, F, W->ldu, K, e), span(W->bg, 1, F, F, 4),
+                       span(W->bu, 1, F, F, 4)};
+    const Span out[] = {span(H, T, ldh, F, e), span(G, T, ldp, F, 4), span(U, T, ldp, F, 4)};
+    return disjoint(in, out) ? BSR_OK : BSR_ERR_ARG;
+}
+
+bsr_status check_gated_i8(const int8_t *Xq, int64_t T, int64_t ldx, const float *sx,
+                          const bsr_gated_t *W, const void *H, int32_t h_dtype, int64_t ldh) {
+    const bsr_status s = check_gated_block(W, true, T, ldx);
+    if (s != BSR_OK) return s;
+    if (!known_dtype(h_dtype)) return BSR_ERR_ARG;
+    if (h_dtype == BSR_I8) return BSR_ERR_DTYPE;
+    if (ldh < W->F) return BSR_ERR_SHAPE;
+    if (ldh > kDenseMaxWidth) return BSR_ERR_UNSUPPORTED;
+    if (T == 0) return BSR_OK;
+    if (!Xq || !sx || !H) return BSR_ERR_NULL;
+    const int64_t K = W->K, F = W->F;
+    const Span in[] = {span(Xq, T, ldx, K, 1), span(W->Wg, F, W->ldg, K, 1),
+                       span(W->Wu, F, W->ldu, K, 1), span(sx, 1, T, T, 4),
+                       span(W->sg, 1, F, F, 4), span(W->su, 1, F, F, 4),
+                       span(W->bg, 1, F, F, 4), span(W->bu, 1, F, F, 4)};
+    const Span out[] = {span(H, T, ldh, F, dtype_size(h_dtype))};
+    return disjoint(in, out) ? BSR_OK : BSR_ERR_ARG;
+}
+
+GatedWorkspace gated_workspace_layout(int64_t T, int64_t K, int64_t F, int32_t dtype) {
+    (void)K;
+    GatedWorkspace w{};
+    const size_t e = size_t(dtype_size(dtype));
+    const int64_t blocks = (T + kGatedRowsPerPartial - 1) / kGatedRowsPerPartial;
+    w.grad_offset = 0;
+    w.partial_offset = align256(size_t(T) * 2 * size_t(F) * e);
+    w.total = align256(w.partial_offset + size_t(blocks) * 2 * size_t(F) * 4);
+    if (w.total == 0) w.total = 256;
+    return w;
+}
+
+bsr_status check_gated_backward(const void *dH, int64_t lddh, const void *X, int64_t T,
+                                int64_t ldx, const bsr_gated_t *W, const float *G, const float *U,
+                                int64_t ldp, const void *dX, int64_t lddx, const void *dWg,
+                                const void *dWu, int64_t lddw, const void *dbg, const void *dbu,
+                                int32_t grad_dtype, const void *workspace, size_t ws_bytes) {
+    const bsr_status s = check_gated_block(W, false, T, ldx);
+    if (s != BSR_OK) return s;
+    if (!known_dtype(grad_dtype)) return BSR_ERR_ARG;
+    if (grad_dtype == BSR_I8) return BSR_ERR_DTYPE;
+    const int64_t K = W->K, F = W->F;
+    const bool dw = dWg || dWu;
+    if (lddh < F || ldp < F || (dX && lddx < K) || (dw && lddw < K)) return BSR_ERR_SHAPE;
+    if (T > kGatedMaxBackwardTokens || lddh > kDenseMaxWidth || ldp > kDenseMaxWidth ||
+        (dX && lddx > kDenseMaxWidth) || (dw && lddw > kDenseMaxWidth) ||
+        2 * F > kDenseMaxWidth || F * K > kDenseMaxOut / 2 || T * K > kDenseMaxOut)
+        return BSR_ERR_UNSUPPORTED;
+    if (dw && (!dWg || !dWu)) return BSR_ERR_NULL;
+    if (T > 0 && (!dH || !X || !G || !U)) return BSR_ERR_NULL;
+    const int32_t dt = raw_enum(W->dtype);
+    const int64_t e = dtype_size(dt), g = dtype_size(grad_dtype);
+    const size_t need = gated_workspace_layout(T, K, F, dt).total;
+    if (!workspace || ws_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 15) != 0)
+        return BSR_ERR_WORKSPACE;
+    const Span in[] = {span(dH, T, lddh, F, e), span(X, T, ldx, K, e),
+                       span(W->Wg, F, W->ldg, K, e), span(W->Wu, F, W->ldu, K, e),
+                       span(G, T, ldp, F, 4), span(U, T, ldp, F, 4)};
+    const Span out[] = {span(dX, T, lddx, K, e), span(dWg, F, lddw, K, g),
+                        span(dWu, F, lddw, K, g), span(dbg, 1, F, F, g), span(dbu, 1, F, F, g),
+                        Span{workspace, int64_t(need)}};
+    return disjoint(in, out) ? BSR_OK : BSR_ERR_ARG;
+}
+
 }  // namespace bsr
 
 extern "C" {
+
+size_t bsr_gated_workspace_bytes(int64_t T, int64_t K, int64_t F, bsr_dtype dtype) {
+    const int32_t dt = bsr::raw_enum(dtype);
+    if (T < 0 || K < 1 || F < 1 || T > bsr::kGatedMaxBackwardTokens ||
+        K > bsr::kDenseMaxWidth || 2 * F > bsr::kDenseMaxWidth ||
+        (dt != BSR_F32 && dt != BSR_BF16))
+        return 0;
+    return bsr::gated_workspace_layout(T, K, F, dt).total;
+}
 
 bsr_status bsr_prune_count(int64_t N, int64_t K, int32_t R, int32_t C, double density,
                            int64_t *k) {
