@@ -1,122 +1,48 @@
-// The dense products: 8-bit rows with scales, the gated block's projections and its gradients.  A
-// 64 x 64 tile of the output per workgroup, 16 columns of the contraction in LDS at a time, four by
-// four outputs to a thread, fp32 (8-bit operands: int32) accumulation.
+// The dense products' launches: 8-bit rows with scales, the gated block's projections and its
+// gradients, on the tiled matrix-core kernel (dense_tile.h).
 #include <type_traits>
 
-#include "dense_math.h"
+#include "dense_tile.h"
 
 namespace bsr {
 
 namespace {
 
-constexpr int kTile = 64;
-constexpr int kDepth = 16;
 constexpr int kThreads = 256;
 
-template <class T> struct Acc { using type = float; };
-template <> struct Acc<int8_t> { using type = int; };
-__device__ __forceinline__ int widen(int8_t x) { return x; }
-__device__ __forceinline__ float widen(float x) { return x; }
-__device__ __forceinline__ float widen(bf16 x) { return to_float(x); }
+template <class T> constexpr int64_t kSize = sizeof(T);
 
-// One operand: element (row, k) at p[row * rs + k * cs], zero outside rows x K.
-template <class T> struct Operand {
-    const T *p;
-    int64_t rs, cs, rows;
-};
-
-template <class T>
-__device__ void accumulate(typename Acc<T>::type (&acc)[4][4], const Operand<T> &A,
-                           const Operand<T> &B, int64_t m0, int64_t n0, int64_t K,
-                           typename Acc<T>::type (*sa)[kTile + 1],
-                           typename Acc<T>::type (*sb)[kTile + 1]) {
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    for (int64_t k0 = 0; k0 < K; k0 += kDepth) {
-        for (int e = threadIdx.x; e < kTile * kDepth; e += kThreads) {
-            const int r = e / kDepth, k = e % kDepth;
-            const bool in = k0 + k < K;
-            sa[k][r] = in && m0 + r < A.rows ? widen(A.p[(m0 + r) * A.rs + (k0 + k) * A.cs]) : 0;
-            sb[k][r] = in && n0 + r < B.rows ? widen(B.p[(n0 + r) * B.rs + (k0 + k) * B.cs]) : 0;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < kDepth; ++k)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] += sa[k][ty + 16 * i] * sb[k][tx + 16 * j];
-        __syncthreads();
-    }
+template <class E, int BM, int BN, int WM, int WN, int MF, bool DUAL, Out OUT>
+void launch_tile(ProductArgs a, bool aligned, void *stream) {
+    using K = TileKernel<E, BM, BN, WM, WN, MF, DUAL, true, OUT>;
+    a.tiles_m = int((a.M + BM - 1) / BM);
+    a.tiles_n = int((a.N + K::kTileN - 1) / K::kTileN);
+    const dim3 grid(unsigned(a.tiles_m) * unsigned(a.tiles_n)), block(K::kThreads);
+    if (aligned)
+        hipLaunchKernelGGL((dense_tile_kernel<E, BM, BN, WM, WN, MF, DUAL, true, OUT>), grid, block,
+                           0, as_stream(stream), a);
+    else if constexpr (OUT != Out::kStore)   // the gradients' operands are laid out by the library
+        hipLaunchKernelGGL((dense_tile_kernel<E, BM, BN, WM, WN, MF, DUAL, false, OUT>), grid,
+                           block, 0, as_stream(stream), a);
 }
 
-// DUAL: two products of the same A, passed to the epilogue together; otherwise the sum of one or two
-// products (A2.p set) over K each.
-template <class T, bool DUAL, class Epi>
-__global__ __launch_bounds__(kThreads) void product_kernel(Operand<T> A, Operand<T> B,
-                                                           Operand<T> A2, Operand<T> B2,
-                                                           int64_t K, int64_t ntiles, Epi epi) {
-    using A_t = typename Acc<T>::type;
-    __shared__ A_t sa[kDepth][kTile + 1], sb[kDepth][kTile + 1];
-    const int64_t m0 = int64_t(blockIdx.x) / ntiles * kTile, n0 = int64_t(blockIdx.x) % ntiles * kTile;
-    A_t acc[DUAL ? 2 : 1][4][4] = {};
-    accumulate(acc[0], A, B, m0, n0, K, sa, sb);
-    if (A2.p) accumulate(acc[DUAL ? 1 : 0], A2, B2, m0, n0, K, sa, sb);
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) {
-            const int64_t m = m0 + ty + 16 * i, n = n0 + tx + 16 * j;
-            if (m < A.rows && n < B.rows)
-                epi(m, n, float(acc[0][i][j]), float(acc[DUAL ? 1 : 0][i][j]));
-        }
+bool rows_aligned(const void *p, int64_t ld) {
+    return ((reinterpret_cast<uintptr_t>(p) | uintptr_t(ld)) & 15) == 0;
 }
 
-template <class T> struct StoreEpi {   // out[m][n], or out2[m - split][n] for m >= split
-    T *out, *out2;
-    int64_t ld, split;
-    __device__ void operator()(int64_t m, int64_t n, float v, float) const {
-        if (m < split)
-            out[m * ld + n] = from_float<T>(v);
-        else
-            out2[(m - split) * ld + n] = from_float<T>(v);
-    }
-};
-
-template <class T> struct ScaleEpi {
-    const float *sx, *sw, *bias;
-    T *Y;
-    int64_t ldy;
-    __device__ void operator()(int64_t m, int64_t n, float v, float) const {
-        const float y = v * sx[m] * sw[n];
-        Y[m * ldy + n] = from_float<T>(bias ? y + bias[n] : y);
-    }
-};
-
-template <class T, int ACT> struct GatedEpi {
-    const float *sx, *sg, *su, *bg, *bu;
-    T *H;
-    float *G, *U;
-    int64_t ldh, ldp;
-    __device__ void operator()(int64_t m, int64_t n, float g, float u) const {
-        if (sx) {
-            g = g * sx[m] * sg[n];
-            u = u * sx[m] * su[n];
-        }
-        if (bg) g += bg[n];
-        if (bu) u += bu[n];
-        H[m * ldh + n] = from_float<T>(activate<ACT>(g) * u);
-        if (G) {
-            G[m * ldp + n] = g;
-            U[m * ldp + n] = u;
-        }
-    }
-};
-
-template <class T, bool DUAL, class Epi>
-void launch(const Operand<T> &A, const Operand<T> &B, const Operand<T> &A2, const Operand<T> &B2,
-            int64_t K, const Epi &epi, void *stream) {
-    const int64_t mt = (A.rows + kTile - 1) / kTile, nt = (B.rows + kTile - 1) / kTile;
-    hipLaunchKernelGGL((product_kernel<T, DUAL, Epi>), dim3(unsigned(mt * nt)), dim3(kThreads), 0,
-                       as_stream(stream), A, B, A2, B2, K, nt, epi);
+// The tile for a product of M tokens and `rows` channels (both matrices' together where there are
+// two).
+template <class E, bool DUAL, Out OUT> void launch_product(const ProductArgs &a, void *stream) {
+    const bool aligned = a.Kb % 16 == 0 && rows_aligned(a.A, a.lda) && rows_aligned(a.B0, a.ldb0) &&
+                         (!DUAL || rows_aligned(a.B1, a.ldb1));
+    const int64_t rows = DUAL ? 2 * a.N : a.N;
+    auto tiles = [&](int bm, int bn) { return ((a.M + bm - 1) / bm) * ((rows + bn - 1) / bn); };
+    if (tiles(256, 256) >= 192)
+        launch_tile<E, 256, 256, 2, 4, 32, DUAL, OUT>(a, aligned, stream);
+    else if (tiles(128, 128) >= 192)
+        launch_tile<E, 128, 128, 2, 2, 32, DUAL, OUT>(a, aligned, stream);
+    else
+        launch_tile<E, 64, 64, 2, 2, 16, DUAL, OUT>(a, aligned, stream);
 }
 
 // f(constant activation) for the block's activation.
@@ -129,42 +55,100 @@ template <class F> void with_act(int act, F &&f) {
     }
 }
 
-template <class T, class TO>
+template <class T>
 void gated(const void *X, int64_t T_, int64_t ldx, const float *sx, const bsr_gated_t &W, void *H,
-           int64_t ldh, float *G, float *U, int64_t ldp, void *stream) {
-    const Operand<T> A{static_cast<const T *>(X), ldx, 1, T_};
-    const Operand<T> Bg{static_cast<const T *>(W.Wg), W.ldg, 1, W.F};
-    const Operand<T> Bu{static_cast<const T *>(W.Wu), W.ldu, 1, W.F};
-    with_act(W.act, [&](auto act) {
-        const GatedEpi<TO, decltype(act)::value> epi{sx, W.sg, W.su, W.bg, W.bu,
-                                                     static_cast<TO *>(H), G, U, ldh, ldp};
-        launch<T, true>(A, Bg, A, Bu, W.K, epi, stream);
-    });
+           int h_dtype, int64_t ldh, float *G, float *U, int64_t ldp, void *stream) {
+    ProductArgs a{};
+    a.A = static_cast<const char *>(X);
+    a.B0 = static_cast<const char *>(W.Wg);
+    a.B1 = static_cast<const char *>(W.Wu);
+    a.lda = ldx * kSize<T>;
+    a.ldb0 = W.ldg * kSize<T>;
+    a.ldb1 = W.ldu * kSize<T>;
+    a.M = T_;
+    a.N = W.F;
+    a.Kb = int(W.K * kSize<T>);
+    a.sx = sx;
+    a.s0 = W.sg;
+    a.s1 = W.su;
+    a.b0 = W.bg;
+    a.b1 = W.bu;
+    a.out = H;
+    a.ldo = ldh;
+    a.out_bf16 = h_dtype == BSR_BF16;
+    a.act = W.act;
+    a.G = G;
+    a.U = U;
+    a.ldp = ldp;
+    launch_product<T, true, Out::kGated>(a, stream);
 }
 
-// D[t][f] = dH U act'(G), D[t][F + f] = dH act(G), and the sums of their columns over 64 rows.
+// --- gradients ----------------------------------------------------------------------------------
+// The two gradient products sum over the hidden width and over the tokens, along which their
+// operands are not contiguous.  dG and dU are written in both orders where they are made; X and the
+// weights are transposed.  Padding keeps every row 16-byte aligned and holds zeros.
+
+constexpr int kT = 64;   // tile of the transposing kernels
+
+// out[c][r] = in[r][c] for r < R, c < C; out's rows are padded with zeros to `pad` columns.
+template <class T>
+__global__ __launch_bounds__(kThreads) void transpose_kernel(const T *__restrict__ in, int64_t ldi,
+                                                             int64_t R, int64_t C, T *__restrict__ out,
+                                                             int64_t ldo, int64_t pad) {
+    __shared__ T tile[kT][kT + 2];
+    const int64_t r0 = int64_t(blockIdx.x) * kT, c0 = int64_t(blockIdx.y) * kT;
+    const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
+    for (int i = y; i < kT; i += kThreads / 64)
+        tile[i][x] = r0 + i < R && c0 + x < C ? in[(r0 + i) * ldi + c0 + x] : T{};
+    __syncthreads();
+    for (int i = y; i < kT; i += kThreads / 64)
+        if (c0 + i < C && r0 + x < pad) out[(c0 + i) * ldo + r0 + x] = tile[x][i];
+}
+
+// D[t][f] = dH U act'(G), D[t][Fp + f] = dH act(G), the transpose Dt[f][t], Dt[F + f][t], and the
+// sums of their columns over the tile's tokens.
 template <class T, int ACT>
 __global__ __launch_bounds__(kThreads) void gated_slope_kernel(
     const T *__restrict__ dH, int64_t lddh, const float *__restrict__ G,
-    const float *__restrict__ U, int64_t ldp, int64_t T_, int64_t F, T *__restrict__ D,
-    float *__restrict__ partial) {
-    const int64_t f = int64_t(blockIdx.x) * kThreads + threadIdx.x;
-    if (f >= F) return;
-    const int64_t t0 = int64_t(blockIdx.y) * kGatedRowsPerPartial;
-    const int64_t t1 = min(t0 + kGatedRowsPerPartial, T_);
-    float sg = 0.0f, su = 0.0f;
-    for (int64_t t = t0; t < t1; ++t) {
-        float a, da;
-        activate_slope<ACT>(G[t * ldp + f], a, da);
-        const float dh = to_float(dH[t * lddh + f]);
-        const float dg = dh * U[t * ldp + f] * da, du = dh * a;
-        D[t * 2 * F + f] = from_float<T>(dg);
-        D[t * 2 * F + F + f] = from_float<T>(du);
-        sg += dg;
-        su += du;
+    const float *__restrict__ U, int64_t ldp, int64_t T_, int64_t F, T *__restrict__ D, int64_t Fp,
+    T *__restrict__ Dt, int64_t Tp, float *__restrict__ partial) {
+    __shared__ T tg[kT][kT + 2], tu[kT][kT + 2];
+    __shared__ float sg[kThreads / 64][kT], su[kThreads / 64][kT];
+    const int64_t t0 = int64_t(blockIdx.x) * kT, f0 = int64_t(blockIdx.y) * kT;
+    const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
+    const int64_t f = f0 + x;
+    float pg = 0.0f, pu = 0.0f;
+    for (int i = y; i < kT; i += kThreads / 64) {
+        const int64_t t = t0 + i;
+        float dg = 0.0f, du = 0.0f;
+        if (t < T_ && f < F) {
+            float a, da;
+            activate_slope<ACT>(G[t * ldp + f], a, da);
+            const float dh = to_float(dH[t * lddh + f]);
+            dg = dh * U[t * ldp + f] * da;
+            du = dh * a;
+        }
+        pg += dg;
+        pu += du;
+        tg[i][x] = from_float<T>(dg);
+        tu[i][x] = from_float<T>(du);
+        if (t < T_ && f < Fp) {
+            D[t * 2 * Fp + f] = tg[i][x];
+            D[t * 2 * Fp + Fp + f] = tu[i][x];
+        }
     }
-    partial[int64_t(blockIdx.y) * 2 * F + f] = sg;
-    partial[int64_t(blockIdx.y) * 2 * F + F + f] = su;
+    sg[y][x] = pg;
+    su[y][x] = pu;
+    __syncthreads();
+    for (int i = y; i < kT; i += kThreads / 64)
+        if (f0 + i < F && t0 + x < Tp) {
+            Dt[(f0 + i) * Tp + t0 + x] = tg[x][i];
+            Dt[(F + f0 + i) * Tp + t0 + x] = tu[x][i];
+        }
+    if (y == 0 && f < F) {
+        partial[int64_t(blockIdx.x) * 2 * F + f] = (sg[0][x] + sg[1][x]) + (sg[2][x] + sg[3][x]);
+        partial[int64_t(blockIdx.x) * 2 * F + F + f] = (su[0][x] + su[1][x]) + (su[2][x] + su[3][x]);
+    }
 }
 
 template <class T>
@@ -183,39 +167,85 @@ __global__ __launch_bounds__(kThreads) void bias_grad_kernel(const float *__rest
     }
 }
 
+// rows x cols elements of zeros.
+template <class T>
+__global__ __launch_bounds__(kThreads) void zero_rows_kernel(T *__restrict__ p, int64_t rows,
+                                                             int64_t cols, int64_t ld) {
+    const int64_t n = rows * cols;
+    for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; i < n;
+         i += int64_t(gridDim.x) * kThreads)
+        p[i / cols * ld + i % cols] = T{};
+}
+
+unsigned cover(int64_t n, int64_t tile) { return unsigned((n + tile - 1) / tile); }
+
+template <class T>
+void transpose(const void *in, int64_t ldi, int64_t R, int64_t C, T *out, int64_t ldo, int64_t pad,
+               void *stream) {
+    hipLaunchKernelGGL(transpose_kernel<T>, dim3(cover(pad, kT), cover(C, kT)), dim3(kThreads), 0,
+                       as_stream(stream), static_cast<const T *>(in), ldi, R, C, out, ldo, pad);
+}
+
 template <class T, class TG>
 void backward(const void *dH, int64_t lddh, const void *X, int64_t T_, int64_t ldx,
               const bsr_gated_t &W, const float *G, const float *U, int64_t ldp, void *dX,
               int64_t lddx, void *dWg, void *dWu, int64_t lddw, void *dbg, void *dbu, void *ws,
               void *stream) {
     const int64_t K = W.K, F = W.F;
-    const GatedWorkspace lay = gated_workspace_layout(T_, K, F, raw_enum(W.dtype));
-    T *D = reinterpret_cast<T *>(static_cast<char *>(ws) + lay.grad_offset);
-    float *partial = reinterpret_cast<float *>(static_cast<char *>(ws) + lay.partial_offset);
-    const int64_t blocks = (T_ + kGatedRowsPerPartial - 1) / kGatedRowsPerPartial;
+    const GatedWorkspace l = gated_workspace_layout(T_, K, F, raw_enum(W.dtype));
+    char *base = static_cast<char *>(ws);
+    T *D = reinterpret_cast<T *>(base + l.grad_offset);
+    T *Dt = reinterpret_cast<T *>(base + l.gradt_offset);
+    T *Xt = reinterpret_cast<T *>(base + l.xt_offset);
+    T *Wt = reinterpret_cast<T *>(base + l.wt_offset);
+    float *partial = reinterpret_cast<float *>(base + l.partial_offset);
     if (T_ > 0)
         with_act(W.act, [&](auto act) {
             hipLaunchKernelGGL((gated_slope_kernel<T, decltype(act)::value>),
-                               dim3(unsigned((F + kThreads - 1) / kThreads), unsigned(blocks)),
-                               dim3(kThreads), 0, as_stream(stream), static_cast<const T *>(dH),
-                               lddh, G, U, ldp, T_, F, D, partial);
+                               dim3(cover(l.Tp, kT), cover(l.Fp, kT)), dim3(kThreads), 0,
+                               as_stream(stream), static_cast<const T *>(dH), lddh, G, U, ldp, T_, F,
+                               D, l.Fp, Dt, l.Tp, partial);
         });
     if (dbg || dbu)
-        hipLaunchKernelGGL(bias_grad_kernel<TG>, dim3(unsigned((2 * F + kThreads - 1) / kThreads)),
-                           dim3(kThreads), 0, as_stream(stream), partial, blocks, F,
+        hipLaunchKernelGGL(bias_grad_kernel<TG>, dim3(cover(2 * F, kThreads)), dim3(kThreads), 0,
+                           as_stream(stream), partial, int64_t(cover(T_, kT)), F,
                            static_cast<TG *>(dbg), static_cast<TG *>(dbu));
-    const Operand<T> none{nullptr, 0, 0, 0};
-    if (dX && T_ > 0)
-        launch<T, false>(Operand<T>{D, 2 * F, 1, T_},
-                         Operand<T>{static_cast<const T *>(W.Wg), 1, W.ldg, K},
-                         Operand<T>{D + F, 2 * F, 1, T_},
-                         Operand<T>{static_cast<const T *>(W.Wu), 1, W.ldu, K}, F,
-                         StoreEpi<T>{static_cast<T *>(dX), nullptr, lddx, T_}, stream);
-    if (dWg)
-        launch<T, false>(Operand<T>{D, 1, 2 * F, 2 * F},
-                         Operand<T>{static_cast<const T *>(X), 1, ldx, K}, none, none, T_,
-                         StoreEpi<TG>{static_cast<TG *>(dWg), static_cast<TG *>(dWu), lddw, F},
-                         stream);
+    if (dX && T_ > 0) {
+        transpose<T>(W.Wg, W.ldg, F, K, Wt, 2 * l.Fp, l.Fp, stream);
+        transpose<T>(W.Wu, W.ldu, F, K, Wt + l.Fp, 2 * l.Fp, l.Fp, stream);
+        ProductArgs a{};
+        a.A = reinterpret_cast<const char *>(D);
+        a.B0 = reinterpret_cast<const char *>(Wt);
+        a.lda = a.ldb0 = 2 * l.Fp * kSize<T>;
+        a.Kb = int(2 * l.Fp * kSize<T>);
+        a.M = T_;
+        a.N = K;
+        a.out = dX;
+        a.ldo = lddx;
+        a.split = T_;
+        a.out_bf16 = std::is_same<T, bf16>::value;
+        launch_product<T, false, Out::kStore>(a, stream);
+    }
+    if (dWg && T_ > 0) {
+        transpose<T>(X, ldx, T_, K, Xt, l.Tp, l.Tp, stream);
+        ProductArgs a{};
+        a.A = reinterpret_cast<const char *>(Dt);
+        a.B0 = reinterpret_cast<const char *>(Xt);
+        a.lda = a.ldb0 = l.Tp * kSize<T>;
+        a.Kb = int(l.Tp * kSize<T>);
+        a.M = 2 * F;
+        a.N = K;
+        a.out = dWg;
+        a.out2 = dWu;
+        a.ldo = lddw;
+        a.split = F;
+        a.out_bf16 = std::is_same<TG, bf16>::value;
+        launch_product<T, false, Out::kStore>(a, stream);
+    } else if (dWg) {
+        for (void *p : {dWg, dWu})
+            hipLaunchKernelGGL(zero_rows_kernel<TG>, dim3(grid_for(F * K, kThreads, 4096)),
+                               dim3(kThreads), 0, as_stream(stream), static_cast<TG *>(p), F, K, lddw);
+    }
 }
 
 }  // namespace
@@ -223,31 +253,35 @@ void backward(const void *dH, int64_t lddh, const void *X, int64_t T_, int64_t l
 bsr_status launch_matmul_i8(const int8_t *Xq, int64_t T, int64_t K, int64_t ldx, const float *sx,
                             const int8_t *Wq, int64_t N, int64_t ldw, const float *sw,
                             const float *bias, void *Y, int y_dtype, int64_t ldy, void *stream) {
-    const Operand<int8_t> A{Xq, ldx, 1, T}, B{Wq, ldw, 1, N}, none{nullptr, 0, 0, 0};
-    if (y_dtype == BSR_BF16)
-        launch<int8_t, false>(A, B, none, none, K,
-                              ScaleEpi<bf16>{sx, sw, bias, static_cast<bf16 *>(Y), ldy}, stream);
-    else
-        launch<int8_t, false>(A, B, none, none, K,
-                              ScaleEpi<float>{sx, sw, bias, static_cast<float *>(Y), ldy}, stream);
+    ProductArgs a{};
+    a.A = reinterpret_cast<const char *>(Xq);
+    a.B0 = reinterpret_cast<const char *>(Wq);
+    a.lda = ldx;
+    a.ldb0 = ldw;
+    a.M = T;
+    a.N = N;
+    a.Kb = int(K);
+    a.sx = sx;
+    a.s0 = sw;
+    a.b0 = bias;
+    a.out = Y;
+    a.ldo = ldy;
+    a.out_bf16 = y_dtype == BSR_BF16;
+    launch_product<int8_t, false, Out::kScale>(a, stream);
     return launch_status();
 }
 
 bsr_status launch_gated(const void *X, int64_t T, int64_t ldx, const bsr_gated_t &W, void *H,
                         int64_t ldh, float *G, float *U, int64_t ldp, void *stream) {
-    if (raw_enum(W.dtype) == BSR_BF16)
-        gated<bf16, bf16>(X, T, ldx, nullptr, W, H, ldh, G, U, ldp, stream);
-    else
-        gated<float, float>(X, T, ldx, nullptr, W, H, ldh, G, U, ldp, stream);
+    const int dt = raw_enum(W.dtype);
+    const auto f = dt == BSR_BF16 ? gated<bf16> : gated<float>;
+    f(X, T, ldx, nullptr, W, H, dt, ldh, G, U, ldp, stream);
     return launch_status();
 }
 
 bsr_status launch_gated_i8(const int8_t *Xq, int64_t T, int64_t ldx, const float *sx,
                            const bsr_gated_t &W, void *H, int h_dtype, int64_t ldh, void *stream) {
-    if (h_dtype == BSR_BF16)
-        gated<int8_t, bf16>(Xq, T, ldx, sx, W, H, ldh, nullptr, nullptr, 0, stream);
-    else
-        gated<int8_t, float>(Xq, T, ldx, sx, W, H, ldh, nullptr, nullptr, 0, stream);
+    gated<int8_t>(Xq, T, ldx, sx, W, H, h_dtype, ldh, nullptr, nullptr, 0, stream);
     return launch_status();
 }
 

@@ -385,13 +385,17 @@ bsr_status check_gated_i8(const int8_t *Xq, int64_t T, int64_t ldx, const float 
 }
 
 GatedWorkspace gated_workspace_layout(int64_t T, int64_t K, int64_t F, int32_t dtype) {
-    (void)K;
     GatedWorkspace w{};
-    const size_t e = size_t(dtype_size(dtype));
+    const int64_t e = dtype_size(dtype), per = 16 / e;
     const int64_t blocks = (T + kGatedRowsPerPartial - 1) / kGatedRowsPerPartial;
+    w.Fp = (F + per - 1) / per * per;
+    w.Tp = (T + per - 1) / per * per;
     w.grad_offset = 0;
-    w.partial_offset = align256(size_t(T) * 2 * size_t(F) * e);
-    w.total = align256(w.partial_offset + size_t(blocks) * 2 * size_t(F) * 4);
+    w.gradt_offset = align256(size_t(T * 2 * w.Fp * e));
+    w.xt_offset = align256(w.gradt_offset + size_t(2 * F * w.Tp * e));
+    w.wt_offset = align256(w.xt_offset + size_t(K * w.Tp * e));
+    w.partial_offset = align256(w.wt_offset + size_t(K * 2 * w.Fp * e));
+    w.total = align256(w.partial_offset + size_t(blocks * 2 * F * 4));
     if (w.total == 0) w.total = 256;
     return w;
 }
