@@ -800,11 +800,22 @@ def bsr_cast_f32_bf16(src: torch.Tensor, dst: torch.Tensor | None = None,
     return dst
 
 
+_I8_DTYPES = (torch.int8,)
+_F32_DTYPES = (torch.float32,)
 _DTYPE_CODE = {torch.float32: BSR_F32, torch.bfloat16: BSR_BF16, torch.int8: BSR_I8}
 
 
 def _matrix_arg(t, name: str, rows: int | None, cols: int | None, dtypes) -> int:
     """Check a 2-D argument of the dense products (None: any size); returns its row pitch."""
+    # One pass over the conditions; anything unexpected goes through them one by one below, for the
+    # error that names it.
+    if isinstance(t, torch.Tensor) and t.dtype in dtypes:
+        shape = t.shape
+        if (len(shape) == 2 and (rows is None or shape[0] == rows)
+                and (cols is None or shape[1] == cols)):
+            row, col = t.stride()
+            if col == 1 and row >= shape[1]:
+                return row if shape[0] > 1 else shape[1]
     if (not isinstance(t, torch.Tensor) or t.dim() != 2
             or (rows is not None and t.shape[0] != rows)
             or (cols is not None and t.shape[1] != cols)):
@@ -830,28 +841,27 @@ def _vector_arg(t, name: str, n: int, dtype=torch.float32):
 
 def _one_device(*tensors) -> None:
     """Every given tensor is on the current GPU, whose stream the work is enqueued on."""
-    dev = None
+    now = -1
     for t in tensors:
         if t is None:
             continue
         if not t.is_cuda:
             raise TypeError("every tensor must be a CUDA (HIP) tensor")
-        if dev is None:
-            dev = t.device
+        if now < 0:
             now = _cur_device() if _cur_device is not None else torch.cuda.current_device()
-            if dev.index != now:
-                raise ValueError(f"the tensors are on {dev}, the current device is cuda:{now}: "
-                                 "make theirs current (torch.cuda.device)")
-        elif t.device != dev:
-            raise ValueError(f"tensors on {dev} and on {t.device} in one call")
+        if t.get_device() != now:
+            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{now}: keep a "
+                             "call's tensors on one device and make it current (torch.cuda.device)")
 
 
 def _on_stream(stream, *tensors) -> int | None:
     """The call's raw stream.  Tensors that the binding allocated (on torch's current stream) are
     recorded on it when it is another one, so that torch keeps their memory until it has run."""
     st = _stream(stream)
+    if stream is None:
+        return st
     made = [t for t in tensors if t is not None]
-    if stream is not None and made and st != torch.cuda.current_stream().cuda_stream:
+    if made and st != torch.cuda.current_stream().cuda_stream:
         side = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(st)
         side.wait_stream(torch.cuda.current_stream())   # memory the allocator reuses is free there
         for t in made:
@@ -868,13 +878,14 @@ def bsr_quantize_rows(X: torch.Tensor, Q: torch.Tensor | None = None,
     T, K = X.shape
     made = []
     if Q is None:
-        Q = torch.empty((T, K), dtype=torch.int8, device=X.device)
+        Q = torch.empty(T, K, dtype=torch.int8, device=X.device)
         made.append(Q)
     if scale is None:
-        scale = torch.empty((T,), dtype=_F32, device=X.device)
+        scale = torch.empty(T, dtype=_F32, device=X.device)
         made.append(scale)
-    ldq = _matrix_arg(Q, "Q", T, K, (torch.int8,))
-    _vector_arg(scale, "scale", T)
+    else:
+        _vector_arg(scale, "scale", T)
+    ldq = _matrix_arg(Q, "Q", T, K, _I8_DTYPES)
     _one_device(X, Q, scale)
     _check(_lib().bsr_quantize_rows(_ptr(X), _DTYPE_CODE[X.dtype], T, K, ldx, _ptr(Q), ldq,
                                     _ptr(scale), _on_stream(stream, *made)), "bsr_quantize_rows")
@@ -886,9 +897,9 @@ def bsr_matmul_i8(Xq: torch.Tensor, sx: torch.Tensor, Wq: torch.Tensor, sw: torc
                   out_dtype: torch.dtype = torch.float32, stream=None) -> torch.Tensor:
     """Y = diag(sx) Xq Wq^T diag(sw) + bias from 8-bit rows (bsr_matmul_i8): Xq int8 [T, K], Wq int8
     [N, K], scales and bias fp32; Y float32 or bfloat16 (out_dtype, when Y is None)."""
-    ldx = _matrix_arg(Xq, "Xq", None, None, (torch.int8,))
+    ldx = _matrix_arg(Xq, "Xq", None, None, _I8_DTYPES)
     T, K = Xq.shape
-    ldw = _matrix_arg(Wq, "Wq", None, K, (torch.int8,))
+    ldw = _matrix_arg(Wq, "Wq", None, K, _I8_DTYPES)
     N = Wq.shape[0]
     _vector_arg(sx, "sx", T)
     _vector_arg(sw, "sw", N)
@@ -897,7 +908,7 @@ def bsr_matmul_i8(Xq: torch.Tensor, sx: torch.Tensor, Wq: torch.Tensor, sw: torc
         raise ValueError("give both scales")
     made = None
     if Y is None:
-        Y = made = torch.empty((T, N), dtype=out_dtype, device=Xq.device)
+        Y = made = torch.empty(T, N, dtype=out_dtype, device=Xq.device)
     ldy = _matrix_arg(Y, "Y", T, N, _DATA_DTYPES)
     _one_device(Xq, sx, Wq, sw, bias, Y)
     _check(_lib().bsr_matmul_i8(_ptr(Xq), T, K, ldx, _ptr(sx), _ptr(Wq), N, ldw, _ptr(sw),
@@ -936,17 +947,17 @@ def bsr_gated(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor,
         raise ValueError("give both G and U, or neither")
     made = []
     if H is None:
-        H = torch.empty((T, F), dtype=X.dtype, device=X.device)
+        H = torch.empty(T, F, dtype=X.dtype, device=X.device)
         made.append(H)
     ldp = 0
     if save and G is None:
-        G = torch.empty((T, F), dtype=_F32, device=X.device)
-        U = torch.empty((T, F), dtype=_F32, device=X.device)
+        G = torch.empty(T, F, dtype=_F32, device=X.device)
+        U = torch.empty(T, F, dtype=_F32, device=X.device)
         made += [G, U]
     ldh = _matrix_arg(H, "H", T, F, (X.dtype,))
     if G is not None:
-        ldp = _matrix_arg(G, "G", T, F, (_F32,))
-        if _matrix_arg(U, "U", T, F, (_F32,)) != ldp:
+        ldp = _matrix_arg(G, "G", T, F, _F32_DTYPES)
+        if _matrix_arg(U, "U", T, F, _F32_DTYPES) != ldp:
             raise ValueError("G and U must have the same row pitch")
     _one_device(X, Wg, Wu, bg, bu, H, G, U)
     _check(_lib().bsr_gated(_ptr(X), T, _pitch(X, "X"), ctypes.byref(block), _ptr(H), ldh, _ptr(G),
@@ -980,8 +991,8 @@ def bsr_gated_backward(dH: torch.Tensor, X: torch.Tensor, Wg: torch.Tensor, Wu: 
     if (dWg is None) != (dWu is None):
         raise ValueError("give both dWg and dWu, or neither")
     lddh = _matrix_arg(dH, "dH", T, F, (X.dtype,))
-    ldp = _matrix_arg(G, "G", T, F, (_F32,))
-    if _matrix_arg(U, "U", T, F, (_F32,)) != ldp:
+    ldp = _matrix_arg(G, "G", T, F, _F32_DTYPES)
+    if _matrix_arg(U, "U", T, F, _F32_DTYPES) != ldp:
         raise ValueError("G and U must have the same row pitch")
     given = next((t for t in (dWg, dbg, dbu) if t is not None), None)
     if grad_dtype is None:
@@ -991,7 +1002,7 @@ def bsr_gated_backward(dH: torch.Tensor, X: torch.Tensor, Wg: torch.Tensor, Wu: 
     made = []
 
     def make(*shape, dtype):
-        made.append(torch.empty(shape, dtype=dtype, device=X.device))
+        made.append(torch.empty(*shape, dtype=dtype, device=X.device))
         return made[-1]
 
     if "X" in need and dX is None:
@@ -1035,12 +1046,12 @@ def bsr_gated_i8(Xq: torch.Tensor, sx: torch.Tensor, Wgq: torch.Tensor, sg: torc
     int8 [F, K] with sg and su fp32 [F]; H float32 or bfloat16 (out_dtype, when H is None)."""
     if sg is None or su is None or sx is None:
         raise ValueError("give every scale")
-    block = _gated_block(Xq, Wgq, Wuq, sg, su, bg, bu, act, (torch.int8,))
+    block = _gated_block(Xq, Wgq, Wuq, sg, su, bg, bu, act, _I8_DTYPES)
     T, F = Xq.shape[0], block.F
     _vector_arg(sx, "sx", T)
     made = None
     if H is None:
-        H = made = torch.empty((T, F), dtype=out_dtype, device=Xq.device)
+        H = made = torch.empty(T, F, dtype=out_dtype, device=Xq.device)
     ldh = _matrix_arg(H, "H", T, F, _DATA_DTYPES)
     _one_device(Xq, sx, Wgq, sg, Wuq, su, bg, bu, H)
     _check(_lib().bsr_gated_i8(_ptr(Xq), T, _pitch(Xq, "Xq"), _ptr(sx), ctypes.byref(block),

@@ -2,6 +2,8 @@
 // gradients, on the tiled matrix-core kernel (dense_tile.h).
 #include <type_traits>
 
+#include "dense_ring.h"
+#include "dense_rows.h"
 #include "dense_tile.h"
 
 namespace bsr {
@@ -12,37 +14,75 @@ constexpr int kThreads = 256;
 
 template <class T> constexpr int64_t kSize = sizeof(T);
 
-template <class E, int BM, int BN, int WM, int WN, int MF, bool DUAL, Out OUT>
+template <class E, int BM, int BN, int WM, int WN, Out OUT>
 void launch_tile(ProductArgs a, bool aligned, void *stream) {
-    using K = TileKernel<E, BM, BN, WM, WN, MF, DUAL, true, OUT>;
+    using K = TileKernel<E, BM, BN, WM, WN, true, OUT>;
     a.tiles_m = int((a.M + BM - 1) / BM);
     a.tiles_n = int((a.N + K::kTileN - 1) / K::kTileN);
     const dim3 grid(unsigned(a.tiles_m) * unsigned(a.tiles_n)), block(K::kThreads);
-    if (aligned)
-        hipLaunchKernelGGL((dense_tile_kernel<E, BM, BN, WM, WN, MF, DUAL, true, OUT>), grid, block,
-                           0, as_stream(stream), a);
-    else if constexpr (OUT != Out::kStore)   // the gradients' operands are laid out by the library
-        hipLaunchKernelGGL((dense_tile_kernel<E, BM, BN, WM, WN, MF, DUAL, false, OUT>), grid,
-                           block, 0, as_stream(stream), a);
+    constexpr bool ring = sizeof(E) < 4;      // aligned bf16 and int8 rows never come here
+    if (!ring && aligned)
+        hipLaunchKernelGGL((dense_tile_kernel<E, BM, BN, WM, WN, !ring, OUT>), grid, block, 0,
+                           as_stream(stream), a);
+    else if constexpr (OUT != Out::kStore)    // the gradients' operands are laid out by the library
+        hipLaunchKernelGGL((dense_tile_kernel<E, BM, BN, WM, WN, false, OUT>), grid, block, 0,
+                           as_stream(stream), a);
+}
+
+template <class E, int BM, int BN, int WM, int WN, Out OUT>
+void launch_ring(ProductArgs a, void *stream) {
+    using K = RingKernel<E, BM, BN, WM, WN, OUT>;
+    a.tiles_m = int((a.M + BM - 1) / BM);
+    a.tiles_n = int((a.N + K::kTileN - 1) / K::kTileN);
+    hipLaunchKernelGGL((dense_ring_kernel<E, BM, BN, WM, WN, OUT>),
+                       dim3(unsigned(a.tiles_m) * unsigned(a.tiles_n)), dim3(K::kThreads), 0,
+                       as_stream(stream), a);
+}
+
+template <class E, int NT, Out OUT>
+void launch_rows(const ProductArgs &a, bool aligned, void *stream) {
+    using K = RowsKernel<E, NT, true, OUT>;
+    const auto kernel = aligned ? dense_rows_kernel<E, NT, true, OUT>
+                                : dense_rows_kernel<E, NT, false, OUT>;
+    hipLaunchKernelGGL(kernel, dim3(unsigned((a.N + K::kChannels - 1) / K::kChannels)),
+                       dim3(64 * K::kWaves), 0, as_stream(stream), a);
 }
 
 bool rows_aligned(const void *p, int64_t ld) {
     return ((reinterpret_cast<uintptr_t>(p) | uintptr_t(ld)) & 15) == 0;
 }
 
-// The tile for a product of M tokens and `rows` channels (both matrices' together where there are
-// two).
-template <class E, bool DUAL, Out OUT> void launch_product(const ProductArgs &a, void *stream) {
+template <class E, Out OUT> void launch_product(const ProductArgs &a, void *stream) {
+    constexpr bool dual = OUT == Out::kGated;
     const bool aligned = a.Kb % 16 == 0 && rows_aligned(a.A, a.lda) && rows_aligned(a.B0, a.ldb0) &&
-                         (!DUAL || rows_aligned(a.B1, a.ldb1));
-    const int64_t rows = DUAL ? 2 * a.N : a.N;
+                         (!dual || rows_aligned(a.B1, a.ldb1));
+    if constexpr (OUT != Out::kStore) {
+        if (a.M <= 16) return launch_rows<E, 1, OUT>(a, aligned, stream);
+        if (a.M <= 32) return launch_rows<E, 2, OUT>(a, aligned, stream);
+        if (a.M <= 64) return launch_rows<E, 4, OUT>(a, aligned, stream);
+    }
+    const int64_t rows = dual ? 2 * a.N : a.N;
     auto tiles = [&](int bm, int bn) { return ((a.M + bm - 1) / bm) * ((rows + bn - 1) / bn); };
-    if (tiles(256, 256) >= 192)
-        launch_tile<E, 256, 256, 2, 4, 32, DUAL, OUT>(a, aligned, stream);
-    else if (tiles(128, 128) >= 192)
-        launch_tile<E, 128, 128, 2, 2, 32, DUAL, OUT>(a, aligned, stream);
-    else
-        launch_tile<E, 64, 64, 2, 2, 16, DUAL, OUT>(a, aligned, stream);
+    if constexpr (sizeof(E) == 4) {
+        if (tiles(128, 128) >= 160)
+            launch_tile<E, 128, 128, 4, 2, OUT>(a, aligned, stream);
+        else
+            launch_tile<E, 64, 64, 2, 2, OUT>(a, aligned, stream);
+    } else if (aligned) {
+        if (tiles(256, 256) >= 192)
+            launch_ring<E, 256, 256, 2, 4, OUT>(a, stream);
+        else if (tiles(128, 128) >= 192)
+            launch_ring<E, 128, 128, 2, 2, OUT>(a, stream);
+        else
+            launch_ring<E, 64, 64, 2, 2, OUT>(a, stream);
+    } else {
+        if (tiles(256, 256) >= 192)
+            launch_tile<E, 256, 256, 2, 4, OUT>(a, false, stream);
+        else if (tiles(128, 128) >= 192)
+            launch_tile<E, 128, 128, 2, 2, OUT>(a, false, stream);
+        else
+            launch_tile<E, 64, 64, 2, 2, OUT>(a, false, stream);
+    }
 }
 
 // f(constant activation) for the block's activation.
@@ -80,7 +120,7 @@ void gated(const void *X, int64_t T_, int64_t ldx, const float *sx, const bsr_ga
     a.G = G;
     a.U = U;
     a.ldp = ldp;
-    launch_product<T, true, Out::kGated>(a, stream);
+    launch_product<T, Out::kGated>(a, stream);
 }
 
 // --- gradients ----------------------------------------------------------------------------------
@@ -224,7 +264,7 @@ void backward(const void *dH, int64_t lddh, const void *X, int64_t T_, int64_t l
         a.ldo = lddx;
         a.split = T_;
         a.out_bf16 = std::is_same<T, bf16>::value;
-        launch_product<T, false, Out::kStore>(a, stream);
+        launch_product<T, Out::kStore>(a, stream);
     }
     if (dWg && T_ > 0) {
         transpose<T>(X, ldx, T_, K, Xt, l.Tp, l.Tp, stream);
@@ -240,7 +280,7 @@ void backward(const void *dH, int64_t lddh, const void *X, int64_t T_, int64_t l
         a.ldo = lddw;
         a.split = F;
         a.out_bf16 = std::is_same<TG, bf16>::value;
-        launch_product<T, false, Out::kStore>(a, stream);
+        launch_product<T, Out::kStore>(a, stream);
     } else if (dWg) {
         for (void *p : {dWg, dWu})
             hipLaunchKernelGGL(zero_rows_kernel<TG>, dim3(grid_for(F * K, kThreads, 4096)),
@@ -267,7 +307,7 @@ bsr_status launch_matmul_i8(const int8_t *Xq, int64_t T, int64_t K, int64_t ldx,
     a.out = Y;
     a.ldo = ldy;
     a.out_bf16 = y_dtype == BSR_BF16;
-    launch_product<int8_t, false, Out::kScale>(a, stream);
+    launch_product<int8_t, Out::kScale>(a, stream);
     return launch_status();
 }
 

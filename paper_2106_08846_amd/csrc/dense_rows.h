@@ -1,0 +1,86 @@
+// The dense products of few tokens (at most 64): the weights are read once, straight into the
+// operand registers of the matrix instructions, and that read is the whole cost.
+//
+// A workgroup makes 16 channels (gated: of each matrix) for every token.  Its eight waves split the
+// contraction: wave w takes every eighth block of kBlock bytes of the rows, loads a block's chunks
+// all at once, and keeps its own sums; they are added over the waves, in order, through LDS.  What
+// bounds a single token is latency: 16 rows of 4096 bytes are one block per wave, so that everything
+// a workgroup needs is in flight together.  The tokens come from the L2 (every workgroup reads all
+// of them), which is why the tile kernel takes over beyond 64.
+#pragma once
+
+#include "dense_tile.h"
+
+namespace bsr {
+
+// NT: groups of 16 tokens.
+template <class E, int NT, bool ALIGNED, Out OUT> struct RowsKernel {
+    static constexpr bool kDual = OUT == Out::kGated;
+    static constexpr int kWaves = 8;
+    static constexpr int kChannels = 16;
+    static constexpr int NW = kDual ? 2 : 1;
+    // Chunks of 64 bytes per row that a wave loads at once: 16 bytes a lane and operand each.
+    static constexpr int kHeld = NT == 4 ? 2 : NT == 2 ? 4 : kDual ? 4 : 8;
+    static constexpr int kBlock = 64 * kHeld;
+    using M_ = Mma<E>;
+    using Acc = typename M_::Acc;
+    static constexpr int kLds = kWaves * NW * NT * 64 * 16;
+
+    static __device__ __forceinline__ void run(const ProductArgs &a, char *lds) {
+        const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+        const int64_t n0 = int64_t(blockIdx.x) * kChannels;
+        const int rows = int(a.N - n0 < kChannels ? a.N - n0 : kChannels);
+        const Source sx{a.A, a.lda, int(a.M)};
+        const Source sw[2] = {{a.B0 + n0 * a.ldb0, a.ldb0, rows},
+                              {kDual ? a.B1 + n0 * a.ldb1 : nullptr, a.ldb1, rows}};
+        const int fr = lane & 15, fc = lane >> 4;
+        Acc acc[NW][NT] = {};
+        for (int kb = wave * kBlock; kb < a.Kb; kb += kWaves * kBlock) {
+            i32x4 w[kHeld][NW], x[kHeld][NT];
+#pragma unroll
+            for (int s = 0; s < kHeld; ++s) {
+                const int at = kb + s * 64 + fc * kChunk;
+#pragma unroll
+                for (int j = 0; j < NW; ++j) w[s][j] = load_chunk<E, ALIGNED>(sw[j], fr, at, a.Kb);
+            }
+#pragma unroll
+            for (int s = 0; s < kHeld; ++s) {
+                const int at = kb + s * 64 + fc * kChunk;
+#pragma unroll
+                for (int i = 0; i < NT; ++i) x[s][i] = load_chunk<E, ALIGNED>(sx, 16 * i + fr, at, a.Kb);
+            }
+#pragma unroll
+            for (int s = 0; s < kHeld; ++s)
+#pragma unroll
+                for (int j = 0; j < NW; ++j)
+#pragma unroll
+                    for (int i = 0; i < NT; ++i) acc[j][i] = M_::step(w[s][j], x[s][i], acc[j][i]);
+        }
+        Acc *part = reinterpret_cast<Acc *>(lds);
+#pragma unroll
+        for (int j = 0; j < NW; ++j)
+#pragma unroll
+            for (int i = 0; i < NT; ++i) part[((wave * NW + j) * NT + i) * 64 + lane] = acc[j][i];
+        __syncthreads();
+        // Wave i joins token group i: token 16 i + fr, channels n0 + 4 fc .. + 3.
+        if (wave >= NT) return;
+        Acc sum[2] = {};
+#pragma unroll
+        for (int v = 0; v < kWaves; ++v)
+#pragma unroll
+            for (int j = 0; j < NW; ++j) sum[j] += part[((v * NW + j) * NT + wave) * 64 + lane];
+        const int64_t m = 16 * wave + fr, n = n0 + 4 * fc;
+        if (m < a.M && n < a.N)
+            finish4<E, OUT>(a, m, n, int(a.N - n < 4 ? a.N - n : 4),
+                            __builtin_bit_cast(i32x4, sum[0]), __builtin_bit_cast(i32x4, sum[1]));
+    }
+};
+
+template <class E, int NT, bool ALIGNED, Out OUT>
+__global__ __launch_bounds__(512) void dense_rows_kernel(ProductArgs a) {
+    using K = RowsKernel<E, NT, ALIGNED, OUT>;
+    __shared__ __align__(16) char lds[K::kLds];
+    K::run(a, lds);
+}
+
+}  // namespace bsr

@@ -1,66 +1,47 @@
-// The tiled matrix-core product behind the dense entry points:
+// The tiled matrix-core products behind the dense entry points:
 //   P[m][n] = sum over k of A[m][k] B[n][k],
 // rows of A ("tokens") and of B ("channels") contiguous along k.  With DUAL, B is two matrices of
 // the same shape and every token meets both (the gate and up projections).
 //
-// A workgroup makes a BM x BN tile of P; DUAL interleaves MF rows of either matrix in the tile's BN
-// rows, so that one lane holds the gate and the up value of the same outputs.  Every step of the
-// contraction takes 128 bytes of each row (64 bf16, 128 int8 or 32 fp32) through LDS.  All three
-// types use the same layout: a lane's operand of one matrix instruction is 16 consecutive bytes of
-// one row (8 bf16 for 32x32x16 / 16x16x32, 16 int8 for 32x32x32 / 16x16x64); for fp32 the four
-// values of such a chunk go to four 32x32x2 / 16x16x4 instructions, which is the same sum with its
-// terms in another order.
+// A workgroup makes a BM x BN tile of P; DUAL interleaves 16 rows of either matrix in the tile's BN
+// rows, so that one lane holds the gate and the up value of the same outputs.  A lane's operand of
+// one matrix instruction is 16 consecutive bytes of one row: 8 bf16 for 16x16x32 or 16 int8 for
+// 16x16x64.  (32x32 instructions move the same bytes per product and ran the 8192^3 product 5%
+// slower.)  fp32 operands are split into three bf16 pieces on their way into LDS, see Pieces.
+//
+// Here: what the tile kernels share, and the kernel that takes its operands through registers into
+// LDS: for rows that start on no 16-byte boundary, and for fp32.  Rows on 16-byte boundaries go
+// straight into LDS in dense_ring.h.
 #pragma once
+
+#include <type_traits>
 
 #include "dense_math.h"
 
 namespace bsr {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
-typedef int i32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
-// One matrix-instruction step over a 16-byte chunk of MF rows each.
-template <class E, int MF> struct Mma;
-template <> struct Mma<bf16, 32> {
-    using Acc = f32x16;
-    static __device__ __forceinline__ Acc step(i32x4 a, i32x4 b, Acc c) {
-        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
-                                                       __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-    }
-};
-template <> struct Mma<bf16, 16> {
+// One matrix-instruction step over a 16-byte chunk of 16 rows each.  fp32: the four values of a
+// chunk go to four 16x16x4 instructions, which is the same sum with its terms in another order.
+template <class E> struct Mma;
+template <> struct Mma<bf16> {
     using Acc = f32x4;
     static __device__ __forceinline__ Acc step(i32x4 a, i32x4 b, Acc c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
                                                        __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
     }
 };
-template <> struct Mma<int8_t, 32> {
-    using Acc = i32x16;
-    static __device__ __forceinline__ Acc step(i32x4 a, i32x4 b, Acc c) {
-        return __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, c, 0, 0, 0);
-    }
-};
-template <> struct Mma<int8_t, 16> {
+template <> struct Mma<int8_t> {
     using Acc = i32x4;
     static __device__ __forceinline__ Acc step(i32x4 a, i32x4 b, Acc c) {
         return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0);
     }
 };
-template <> struct Mma<float, 32> {
-    using Acc = f32x16;
-    static __device__ __forceinline__ Acc step(i32x4 a, i32x4 b, Acc c) {
-        const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, b);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(x[i], y[i], c, 0, 0, 0);
-        return c;
-    }
-};
-template <> struct Mma<float, 16> {
+template <> struct Mma<float> {
     using Acc = f32x4;
     static __device__ __forceinline__ Acc step(i32x4 a, i32x4 b, Acc c) {
         const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, b);
@@ -69,6 +50,28 @@ template <> struct Mma<float, 16> {
         return c;
     }
 };
+
+// fp32 values as sums of three bf16 pieces, x = h + m + l: h is x rounded to bf16, m the remainder
+// rounded, l what is left, which has 8 significant bits (|m| <= 2^-9 |x|, |l| <= 2^-18 |x|; exact
+// while l does not underflow, |x| >= 2^-100).  A product x y is formed from the six cross terms down
+// to 2^-18 |x y| (hh, hm, mh, hl, lh, mm), each exact in fp32; the three left out are together below
+// 2^-25.9 |x y|, a quarter of fp32's own rounding.  Six bf16 instructions take 96 cycles for what
+// the fp32 instructions need 256 for.  An infinite operand (or one that rounds to infinity in bf16,
+// from 2^128 (1 - 2^-9) on) gives NaN.
+struct Pieces {
+    bf16x4 h, m, l;
+};
+__device__ __forceinline__ Pieces split(f32x4 x) {
+    Pieces p;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        p.h[i] = static_cast<__bf16>(x[i]);
+        const float r = x[i] - static_cast<float>(p.h[i]);
+        p.m[i] = static_cast<__bf16>(r);
+        p.l[i] = static_cast<__bf16>(r - static_cast<float>(p.m[i]));
+    }
+    return p;
+}
 
 // What becomes of the product.
 enum class Out { kStore, kScale, kGated };
@@ -174,72 +177,155 @@ __device__ __forceinline__ void finish4(const ProductArgs &a, int64_t m, int64_t
     }
 }
 
-constexpr int kStepBytes = 128;   // of every row, per step of the contraction
-constexpr int kChunk = 16;
-constexpr int kRowChunks = kStepBytes / kChunk;
+constexpr int kMF = 16;           // rows and columns of a matrix instruction
+constexpr int kChunk = 16;        // bytes of a row per lane and instruction
 
-// LDS position of chunk c of a row: the chunks of a row are permuted by its number, so that a
-// wave's 16-byte reads of one chunk column spread over the banks.
-__device__ __forceinline__ int swizzled(int row, int c) { return c ^ ((row >> 1) & 7); }
+struct Source {   // one operand's rows as a workgroup reads them
+    const char *base;     // first row of the tile
+    int64_t pitch;
+    int rows;             // rows that exist, at least 1
+};
 
-// BM x BN tile, WM x WN waves, MF x MF matrix instructions.  ALIGNED: rows start on 16-byte
-// boundaries and Kb is a multiple of 16, so 16-byte chunks are loaded whole through range-checked
-// buffer loads; otherwise byte-aligned loads, with the last chunk of a row put together from what
-// it has.
-template <class E, int BM, int BN, int WM, int WN, int MF, bool DUAL, bool ALIGNED, Out OUT>
-struct TileKernel {
+// The 16 bytes at byte kb of row `row`, those from Kb on and those of a row that does not exist
+// being zero.  ALIGNED: rows start on 16-byte boundaries and Kb is a multiple of 16, so chunks are
+// loaded whole through a range-checked buffer load; otherwise byte-aligned loads, with the last
+// chunk of a row put together from what it has.
+template <class E, bool ALIGNED>
+__device__ __forceinline__ i32x4 load_chunk(const Source &s, int row, int kb, int Kb) {
+    if constexpr (ALIGNED) {
+        // Every existing row ends at or before byte (rows - 1) * pitch + Kb; a row past the end is
+        // out of that range by itself, a chunk past Kb is sent there.
+        const unsigned bytes = unsigned((s.rows - 1) * s.pitch) + unsigned(Kb);
+        const unsigned off = kb < Kb ? unsigned(row) * unsigned(s.pitch) + unsigned(kb) : 0x80000000u;
+        return __builtin_bit_cast(
+            i32x4, __builtin_amdgcn_raw_buffer_load_b128(buffer_rsrc(s.base, bytes), off, 0, 0));
+    } else {
+        i32x4 v = {0, 0, 0, 0};
+        if (row >= s.rows || kb >= Kb) return v;
+        const char *p = s.base + row * s.pitch + kb;
+        if (Kb - kb >= kChunk) {
+            __builtin_memcpy(&v, p, kChunk);
+        } else {
+            const E *e = reinterpret_cast<const E *>(p);
+            const int n = (Kb - kb) / int(sizeof(E));
+            E tail[kChunk / sizeof(E)] = {};
+#pragma unroll
+            for (int i = 0; i < int(kChunk / sizeof(E)); ++i)
+                if (i < n) tail[i] = e[i];
+            __builtin_memcpy(&v, tail, kChunk);
+        }
+        return v;
+    }
+}
+
+// The tile of this workgroup.  Workgroups go round robin over the 8 XCDs: XCD x takes a contiguous
+// run of the tile order, and that order walks bands of 8 token tiles, so the tiles an XCD works on
+// at one time share rows of both operands in its L2.
+__device__ __forceinline__ void tile_of(const ProductArgs &a, int &tm, int &tn) {
+    const int total = a.tiles_m * a.tiles_n, id = blockIdx.x;
+    const int per = total / 8, extra = total % 8, x = id % 8;
+    const int t = x * per + (x < extra ? x : extra) + id / 8;
+    constexpr int kBand = 8;
+    const int band = t / (kBand * a.tiles_n), first = band * kBand;
+    const int height = a.tiles_m - first < kBand ? a.tiles_m - first : kBand;
+    const int in = t - first * a.tiles_n;
+    tm = first + in % height;
+    tn = in / height;
+}
+
+// Order LDS accesses of one wave's lanes among themselves.
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// A wave's NN x NM accumulators (channels x tokens, 16 x 16 each) to the outputs, 16 tokens at a time
+// through the wave's own LDS, so that consecutive lanes finish consecutive channels of a token.
+// m0, n0: the wave's first token and channel.
+constexpr int epilogue_bytes(int NN) { return kMF * (NN * kMF + 4) * 4; }
+template <class E, Out OUT, int NN, int NM, class Acc>
+__device__ __forceinline__ void epilogue(const ProductArgs &a, const Acc (&acc)[NN][NM], float *mine,
+                                         int64_t m0, int64_t n0) {
+    constexpr bool kDual = OUT == Out::kGated;
+    constexpr int kPitch = NN * kMF + 4;
+    constexpr int kQuads = NN * kMF / (kDual ? 8 : 4);
+    const int lane = threadIdx.x & 63, fr = lane % kMF, fc = lane / kMF;
+#pragma unroll
+    for (int i = 0; i < NM; ++i) {
+#pragma unroll
+        for (int j = 0; j < NN; ++j) {      // lane: token fr, channels 4 fc .. + 3
+            i32x4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const auto x = acc[j][i][e];
+                v[e] = __builtin_bit_cast(int, x);
+            }
+            *reinterpret_cast<i32x4 *>(mine + fr * kPitch + j * kMF + 4 * fc) = v;
+        }
+        wave_sync();
+#pragma unroll 1
+        for (int e = lane; e < kMF * kQuads; e += 64) {
+            const int t = e / kQuads, quad = e % kQuads;
+            const int64_t m = m0 + i * kMF + t, n = n0 + quad * 4;
+            const float *p = mine + t * kPitch;
+            i32x4 x, y = {0, 0, 0, 0};
+            if constexpr (kDual) {
+                const int pair = quad / (kMF / 4), r = quad % (kMF / 4) * 4;
+                x = *reinterpret_cast<const i32x4 *>(p + pair * 2 * kMF + r);
+                y = *reinterpret_cast<const i32x4 *>(p + pair * 2 * kMF + kMF + r);
+            } else {
+                x = *reinterpret_cast<const i32x4 *>(p + quad * 4);
+            }
+            if (m < a.M && n < a.N)
+                finish4<E, OUT>(a, m, n, int(a.N - n < 4 ? a.N - n : 4), x, y);
+        }
+        wave_sync();
+    }
+}
+
+// BM x BN tile, WM x WN waves, operands through registers.  A step of the contraction takes 128
+// bytes of every row (64 bf16, 128 int8, 32 fp32): its chunks are loaded one step before they are
+// written into LDS and two before they are used, and written between the halves of a step's matrix
+// instructions (10% faster at 8192^3 than loading and writing the next step around all of them).
+template <class E, int BM, int BN, int WM, int WN, bool ALIGNED, Out OUT> struct TileKernel {
+    static constexpr bool kDual = OUT == Out::kGated;
+    static constexpr bool kSplit = sizeof(E) == 4;       // fp32 in three pieces
+    static constexpr int kPlanes = kSplit ? 3 : 1;
     static constexpr int kThreads = 64 * WM * WN;
     static constexpr int TM = BM / WM, TN = BN / WN;     // a wave's tokens and channels
-    static constexpr int NM = TM / MF, NN = TN / MF;
+    static constexpr int NM = TM / kMF, NN = TN / kMF;
+    static constexpr int kStepBytes = 128;
+    static constexpr int kRowChunks = kStepBytes / kChunk;
+    static constexpr int kRowBytes = kSplit ? 64 : 128;  // of a row (and piece) in LDS
+    static constexpr int kSteps = kRowBytes / 64;        // matrix-instruction steps
     static constexpr int kRowsPerPass = kThreads / kRowChunks;
     static constexpr int LA = BM / kRowsPerPass, LB = BN / kRowsPerPass;   // chunks per thread
-    static constexpr int kStageBytes = (BM + BN) * kStepBytes;
-    static constexpr int kPitch = TN + 4;                // epilogue: floats per token in LDS
-    static constexpr int kEpiBytes = MF * kPitch * 4;    // per wave
-    static constexpr int kLds = 2 * kStageBytes > WM * WN * kEpiBytes ? 2 * kStageBytes
-                                                                     : WM * WN * kEpiBytes;
-    static constexpr int kSteps = MF == 32 ? 4 : 2;      // matrix-instruction steps per stage
-    static constexpr int kLaneChunks = 64 / MF;          // chunks of a row in one step
-    static constexpr int kTileN = DUAL ? BN / 2 : BN;    // channels per tile
-    using M_ = Mma<E, MF>;
+    static constexpr int kPlaneBytes = (BM + BN) * kRowBytes;
+    static constexpr int kStageBytes = kPlanes * kPlaneBytes;
+    static constexpr int kEpiBytes = WM * WN * epilogue_bytes(NN);
+    static constexpr int kLds = 2 * kStageBytes > kEpiBytes ? 2 * kStageBytes : kEpiBytes;
+    static constexpr int kTileN = kDual ? BN / 2 : BN;   // channels per tile
+    using M_ = Mma<typename std::conditional<kSplit, bf16, E>::type>;
     using Acc = typename M_::Acc;
     static_assert(BM % kRowsPerPass == 0 && BN % kRowsPerPass == 0, "whole passes");
-    static_assert(!DUAL || NN % 2 == 0, "gate and up blocks in pairs");
+    static_assert(!kDual || NN % 2 == 0, "gate and up blocks in pairs");
     static_assert(kLds <= 160 * 1024, "LDS of a CU");
 
-    struct Source {   // one operand's rows as this workgroup reads them
-        const char *base;     // first row of the tile
-        int64_t pitch;
-        int rows;             // rows that exist (0: none; never read)
-    };
-
-    // The chunk at byte kb of row `row`; rows that do not exist may hold anything, bytes from Kb on
-    // are zero.
-    static __device__ __forceinline__ i32x4 load_chunk(const Source &s, int row, int kb, int Kb) {
-        if constexpr (ALIGNED) {
-            // Every existing row ends at or before byte (rows - 1) * pitch + Kb; a chunk past Kb or
-            // a row past the end is sent out of range, which loads zeros.
-            const unsigned bytes = s.rows > 0 ? unsigned((s.rows - 1) * s.pitch) + unsigned(Kb) : 0u;
-            const unsigned off = kb < Kb ? unsigned(row) * unsigned(s.pitch) + unsigned(kb)
-                                         : 0x80000000u;
-            return __builtin_bit_cast(
-                i32x4, __builtin_amdgcn_raw_buffer_load_b128(buffer_rsrc(s.base, bytes), off, 0, 0));
+    // LDS position of 16-byte chunk c of a row: the chunks of a row are permuted by its number, so
+    // that a wave's reads of 16 rows spread over all banks (no conflicts counted).
+    static __device__ __forceinline__ int swizzled(int row, int c) {
+        return kRowBytes == 128 ? c ^ ((row >> 1) & 7) : c ^ ((row >> 2) & 3);
+    }
+    // Chunk c (of the source row) of row `row` into the stage at p.
+    static __device__ __forceinline__ void put_chunk(char *p, int row, int c, i32x4 v) {
+        if constexpr (kSplit) {
+            const Pieces s = split(__builtin_bit_cast(f32x4, v));
+            char *q = p + row * kRowBytes + swizzled(row, c >> 1) * kChunk + (c & 1) * 8;
+            *reinterpret_cast<bf16x4 *>(q) = s.h;
+            *reinterpret_cast<bf16x4 *>(q + kPlaneBytes) = s.m;
+            *reinterpret_cast<bf16x4 *>(q + 2 * kPlaneBytes) = s.l;
         } else {
-            i32x4 v = {0, 0, 0, 0};
-            if (row >= s.rows || kb >= Kb) return v;
-            const char *p = s.base + row * s.pitch + kb;
-            if (Kb - kb >= kChunk) {
-                __builtin_memcpy(&v, p, kChunk);
-            } else {
-                const E *e = reinterpret_cast<const E *>(p);
-                const int n = (Kb - kb) / int(sizeof(E));
-                E tail[kChunk / sizeof(E)] = {};
-#pragma unroll
-                for (int i = 0; i < int(kChunk / sizeof(E)); ++i)
-                    if (i < n) tail[i] = e[i];
-                __builtin_memcpy(&v, tail, kChunk);
-            }
-            return v;
+            *reinterpret_cast<i32x4 *>(p + row * kRowBytes + swizzled(row, c) * kChunk) = v;
         }
     }
 
@@ -253,7 +339,7 @@ struct TileKernel {
         const Source sa{a.A + m0 * a.lda, a.lda, int(left_m < BM ? left_m : BM)};
         const int rows_n = int(left_n < kTileN ? left_n : kTileN);
         const Source sb0{a.B0 + n0 * a.ldb0, a.ldb0, rows_n};
-        const Source sb1{DUAL ? a.B1 + n0 * a.ldb1 : nullptr, a.ldb1, rows_n};
+        const Source sb1{kDual ? a.B1 + n0 * a.ldb1 : nullptr, a.ldb1, rows_n};
 
         const int c = tid & (kRowChunks - 1), r0 = tid / kRowChunks;
         const int wave_row = wave * (64 / kRowChunks);      // first row of this wave in a pass
@@ -261,135 +347,91 @@ struct TileKernel {
         auto load = [&](int step) {
             const int kb = step * kStepBytes + c * kChunk;
 #pragma unroll
-            for (int i = 0; i < LA; ++i) ra[i] = load_chunk(sa, i * kRowsPerPass + r0, kb, a.Kb);
+            for (int i = 0; i < LA; ++i)
+                ra[i] = load_chunk<E, ALIGNED>(sa, i * kRowsPerPass + r0, kb, a.Kb);
 #pragma unroll
             for (int i = 0; i < LB; ++i) {
                 const int row = i * kRowsPerPass + r0;
-                if constexpr (DUAL) {
-                    // row = (pair * 2 + which) * MF + r stands for channel pair * MF + r
-                    const int first = i * kRowsPerPass + wave_row;      // uniform; MF % 8 == 0
-                    const int channel = row / (2 * MF) * MF + row % MF;
-                    const Source &s = (first / MF) & 1 ? sb1 : sb0;
-                    rb[i] = load_chunk(s, channel, kb, a.Kb);
+                if constexpr (kDual) {
+                    // row = (pair * 2 + which) * 16 + r stands for channel pair * 16 + r
+                    const int first = i * kRowsPerPass + wave_row;      // uniform
+                    const int channel = row / (2 * kMF) * kMF + row % kMF;
+                    const Source &s = (first / kMF) & 1 ? sb1 : sb0;
+                    rb[i] = load_chunk<E, ALIGNED>(s, channel, kb, a.Kb);
                 } else {
-                    rb[i] = load_chunk(sb0, row, kb, a.Kb);
+                    rb[i] = load_chunk<E, ALIGNED>(sb0, row, kb, a.Kb);
                 }
             }
         };
         auto put = [&](int buf) {
             char *p = lds + buf * kStageBytes;
 #pragma unroll
-            for (int i = 0; i < LA; ++i) {
-                const int row = i * kRowsPerPass + r0;
-                *reinterpret_cast<i32x4 *>(p + row * kStepBytes + swizzled(row, c) * kChunk) = ra[i];
-            }
-            p += BM * kStepBytes;
+            for (int i = 0; i < LA; ++i) put_chunk(p, i * kRowsPerPass + r0, c, ra[i]);
 #pragma unroll
-            for (int i = 0; i < LB; ++i) {
-                const int row = i * kRowsPerPass + r0;
-                *reinterpret_cast<i32x4 *>(p + row * kStepBytes + swizzled(row, c) * kChunk) = rb[i];
-            }
+            for (int i = 0; i < LB; ++i) put_chunk(p + BM * kRowBytes, i * kRowsPerPass + r0, c, rb[i]);
         };
 
         Acc acc[NN][NM] = {};
-        const int fr = lane % MF, fc = lane / MF;
+        const int fr = lane % kMF, fc = lane / kMF;
         const int steps = (a.Kb + kStepBytes - 1) / kStepBytes;
         load(0);
         put(0);
+        if (steps > 1) load(1);
         for (int s = 0; s < steps; ++s) {
             __syncthreads();
-            if (s + 1 < steps) load(s + 1);
-            const char *pa = lds + (s & 1) * kStageBytes + (wm * TM + fr) * kStepBytes;
-            const char *pb = lds + (s & 1) * kStageBytes + (BM + wn * TN + fr) * kStepBytes;
+            const char *pa = lds + (s & 1) * kStageBytes + (wm * TM + fr) * kRowBytes;
+            const char *pb = lds + (s & 1) * kStageBytes + (BM + wn * TN + fr) * kRowBytes;
+            i32x4 fa[kPlanes][NM], fb[kPlanes][NN];
+            auto fetch = [&](int k) {
+                const int at = swizzled(fr, k * 4 + fc) * kChunk;
 #pragma unroll
-            for (int k = 0; k < kSteps; ++k) {
-                const int at = swizzled(fr, k * kLaneChunks + fc) * kChunk;
-                i32x4 fa[NM], fb[NN];
+                for (int p = 0; p < kPlanes; ++p) {
 #pragma unroll
-                for (int i = 0; i < NM; ++i)
-                    fa[i] = *reinterpret_cast<const i32x4 *>(pa + i * MF * kStepBytes + at);
+                    for (int i = 0; i < NM; ++i)
+                        fa[p][i] = *reinterpret_cast<const i32x4 *>(pa + p * kPlaneBytes +
+                                                                   i * kMF * kRowBytes + at);
+#pragma unroll
+                    for (int j = 0; j < NN; ++j)
+                        fb[p][j] = *reinterpret_cast<const i32x4 *>(pb + p * kPlaneBytes +
+                                                                   j * kMF * kRowBytes + at);
+                }
+            };
+            // Piece x of B with piece y of A.
+            auto multiply = [&](int x, int y) {
 #pragma unroll
                 for (int j = 0; j < NN; ++j)
-                    fb[j] = *reinterpret_cast<const i32x4 *>(pb + j * MF * kStepBytes + at);
 #pragma unroll
-                for (int j = 0; j < NN; ++j)
-#pragma unroll
-                    for (int i = 0; i < NM; ++i) acc[j][i] = M_::step(fb[j], fa[i], acc[j][i]);
+                    for (int i = 0; i < NM; ++i) acc[j][i] = M_::step(fb[x][j], fa[y][i], acc[j][i]);
+            };
+            auto next = [&] {
+                if (s + 1 < steps) put((s + 1) & 1);
+                if (s + 2 < steps) load(s + 2);
+            };
+            fetch(0);
+            if constexpr (kSplit) {
+                multiply(0, 2);
+                multiply(2, 0);
+                next();
+                multiply(1, 1);
+                multiply(0, 1);
+                multiply(1, 0);
+                multiply(0, 0);
+            } else {
+                multiply(0, 0);
+                next();
+                fetch(1);
+                multiply(0, 0);
             }
-            if (s + 1 < steps) put((s + 1) & 1);
         }
         __syncthreads();
-
-        // Epilogue: MF tokens of the wave's tile at a time go through LDS, so that consecutive
-        // lanes finish consecutive channels of a token.
-        float *mine = reinterpret_cast<float *>(lds + wave * kEpiBytes);
-        constexpr int kQuads = (DUAL ? TN / 2 : TN) / 4;
-#pragma unroll
-        for (int i = 0; i < NM; ++i) {
-#pragma unroll
-            for (int j = 0; j < NN; ++j) {
-                // lane: token fr; register group g: channels 4 fc + g (* 8 for 32x32) .. + 3
-#pragma unroll
-                for (int g = 0; g < MF * MF / 256; ++g) {
-                    i32x4 v;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const auto x = acc[j][i][4 * g + e];
-                        v[e] = __builtin_bit_cast(int, x);
-                    }
-                    *reinterpret_cast<i32x4 *>(mine + fr * kPitch + j * MF + 8 * g + 4 * fc) = v;
-                }
-            }
-            wave_sync();
-            const int64_t mt = m0 + wm * TM + i * MF;
-#pragma unroll 1
-            for (int e = lane; e < MF * kQuads; e += 64) {
-                const int t = e / kQuads, quad = e % kQuads;
-                const int64_t m = mt + t;
-                int64_t n;
-                const float *p = mine + t * kPitch;
-                i32x4 x, y = {0, 0, 0, 0};
-                if constexpr (DUAL) {
-                    const int pair = quad / (MF / 4), r = quad % (MF / 4) * 4;
-                    n = n0 + wn * (TN / 2) + pair * MF + r;
-                    x = *reinterpret_cast<const i32x4 *>(p + pair * 2 * MF + r);
-                    y = *reinterpret_cast<const i32x4 *>(p + pair * 2 * MF + MF + r);
-                } else {
-                    n = n0 + wn * TN + quad * 4;
-                    x = *reinterpret_cast<const i32x4 *>(p + quad * 4);
-                }
-                if (m < a.M && n < a.N)
-                    finish4<E, OUT>(a, m, n, int(a.N - n < 4 ? a.N - n : 4), x, y);
-            }
-            wave_sync();
-        }
-    }
-
-    // Order LDS accesses of one wave's lanes among themselves.
-    static __device__ __forceinline__ void wave_sync() {
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-    }
-
-    // Workgroups go round robin over the 8 XCDs: XCD x takes a contiguous run of the tile order,
-    // and that order walks bands of 8 token tiles, so the tiles an XCD works on at one time share
-    // rows of both operands in its L2.
-    static __device__ __forceinline__ void tile_of(const ProductArgs &a, int &tm, int &tn) {
-        const int total = a.tiles_m * a.tiles_n, id = blockIdx.x;
-        const int per = total / 8, extra = total % 8, x = id % 8;
-        const int t = x * per + (x < extra ? x : extra) + id / 8;
-        constexpr int kBand = 8;
-        const int band = t / (kBand * a.tiles_n), first = band * kBand;
-        const int height = a.tiles_m - first < kBand ? a.tiles_m - first : kBand;
-        const int in = t - first * a.tiles_n;
-        tm = first + in % height;
-        tn = in / height;
+        epilogue<E, OUT, NN, NM>(a, acc, reinterpret_cast<float *>(lds + wave * epilogue_bytes(NN)),
+                                 m0 + wm * TM, n0 + wn * (kDual ? TN / 2 : TN));
     }
 };
 
-template <class E, int BM, int BN, int WM, int WN, int MF, bool DUAL, bool ALIGNED, Out OUT>
+template <class E, int BM, int BN, int WM, int WN, bool ALIGNED, Out OUT>
 __global__ __launch_bounds__(64 * WM * WN) void dense_tile_kernel(ProductArgs a) {
-    using K = TileKernel<E, BM, BN, WM, WN, MF, DUAL, ALIGNED, OUT>;
+    using K = TileKernel<E, BM, BN, WM, WN, ALIGNED, OUT>;
     __shared__ __align__(16) char lds[K::kLds];
     K::run(a, lds);
 }

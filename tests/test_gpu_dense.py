@@ -132,6 +132,53 @@ def test_matmul_i8(T, N, K, out, pad, shift):
     assert np.array_equal(host(y), exact.astype(np.float32))
 
 
+# Outputs large enough for the largest tiles: ragged in both directions, a depth that ends inside a
+# step, rows on and off 16-byte boundaries.
+LARGE = [(3330, 4100, 144), (3330, 4100, 130), (4000, 2900, 64), (6100, 2048, 200), (6100, 2048, 208)]
+
+
+@pytest.mark.parametrize("T,N,K", LARGE)
+def test_matmul_i8_large(T, N, K):
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(T + K)
+    xq, wq = (torch.randint(-128, 128, s, dtype=torch.int8, device=DEV, generator=gen)
+              for s in ((T, K), (N, K)))
+    one = torch.ones(max(T, N), device=DEV)
+    Y, clean = frame(T, N, torch.float32, 4, 0)
+    B.bsr_matmul_i8(xq, one[:T], wq, one[:N], Y=Y)
+    assert torch.equal(Y.double(), xq.double() @ wq.double().t())      # below 2^24: exact
+    assert clean()
+
+
+@pytest.mark.parametrize("T,F,K", [(t, n // 2, k) for t, n, k in LARGE])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "i8"])
+def test_gated_large(T, F, K, dtype):
+    """Whole numbers, exact in every type, through forward and backward."""
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(F + K)
+    x, wg, wu = (torch.randint(-2, 3, s, device=DEV, generator=gen).double()
+                 for s in ((T, K), (F, K), (F, K)))
+    g, u = x @ wg.t(), x @ wu.t()
+    h = torch.clamp(g, min=0) * u
+    if dtype == "i8":
+        one = torch.ones(max(T, F), device=DEV)
+        H = B.bsr_gated_i8(x.to(torch.int8), one[:T], wg.to(torch.int8), one[:F], wu.to(torch.int8),
+                           one[:F], act="relu", out_dtype=torch.float32)
+        assert torch.equal(H.double(), h)
+        return
+    dt = TORCH[dtype]
+    H, G, U = B.bsr_gated(x.to(dt), wg.to(dt), wu.to(dt), act="relu", save=True)
+    assert torch.equal(G.double(), g) and torch.equal(U.double(), u)
+    assert torch.equal(H, h.float().to(dt))
+    gi, ui = torch.clamp(g, -3, 3), torch.clamp(u, -3, 3)
+    dh = torch.randint(-1, 2, (T, F), device=DEV, generator=gen).double()
+    got = B.bsr_gated_backward(dh.to(dt), x.to(dt), wg.to(dt), wu.to(dt), gi.float(), ui.float(),
+                               act="relu", bias=True, grad_dtype=torch.float32)
+    dg, du = dh * ui * (gi > 0), dh * torch.clamp(gi, min=0)
+    for t, want in zip(got, (dg @ wg + du @ wu, dg.t() @ x, du.t() @ x, dg.sum(0), du.sum(0))):
+        assert torch.equal(t, want.float().to(t.dtype))
+
+
 def test_matmul_i8_longest_rows():
     """K = 131071 with every product at its largest: the sum comes to 2^31 - 2^14."""
     K = 131071
