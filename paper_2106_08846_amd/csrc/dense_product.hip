@@ -4,7 +4,7 @@
 
 #include "dense_ring.h"
 #include "dense_rows.h"
-#include "dense_tile.h"
+#include "dense_split.h"
 
 namespace bsr {
 
@@ -14,29 +14,31 @@ constexpr int kThreads = 256;
 
 template <class T> constexpr int64_t kSize = sizeof(T);
 
-template <class E, int BM, int BN, int WM, int WN, Out OUT>
-void launch_tile(ProductArgs a, bool aligned, void *stream) {
-    using K = TileKernel<E, BM, BN, WM, WN, true, OUT>;
+// Launch `kernel` over the tiles of K.
+template <class K, int BM>
+void launch_tiles(void (*kernel)(ProductArgs), ProductArgs a, void *stream) {
     a.tiles_m = int((a.M + BM - 1) / BM);
     a.tiles_n = int((a.N + K::kTileN - 1) / K::kTileN);
-    const dim3 grid(unsigned(a.tiles_m) * unsigned(a.tiles_n)), block(K::kThreads);
-    constexpr bool ring = sizeof(E) < 4;      // aligned bf16 and int8 rows never come here
-    if (!ring && aligned)
-        hipLaunchKernelGGL((dense_tile_kernel<E, BM, BN, WM, WN, !ring, OUT>), grid, block, 0,
-                           as_stream(stream), a);
-    else if constexpr (OUT != Out::kStore)    // the gradients' operands are laid out by the library
-        hipLaunchKernelGGL((dense_tile_kernel<E, BM, BN, WM, WN, false, OUT>), grid, block, 0,
-                           as_stream(stream), a);
-}
-
-template <class E, int BM, int BN, int WM, int WN, Out OUT>
-void launch_ring(ProductArgs a, void *stream) {
-    using K = RingKernel<E, BM, BN, WM, WN, OUT>;
-    a.tiles_m = int((a.M + BM - 1) / BM);
-    a.tiles_n = int((a.N + K::kTileN - 1) / K::kTileN);
-    hipLaunchKernelGGL((dense_ring_kernel<E, BM, BN, WM, WN, OUT>),
-                       dim3(unsigned(a.tiles_m) * unsigned(a.tiles_n)), dim3(K::kThreads), 0,
+    hipLaunchKernelGGL(kernel, dim3(unsigned(a.tiles_m) * unsigned(a.tiles_n)), dim3(K::kThreads), 0,
                        as_stream(stream), a);
+}
+template <class E, int BM, int BN, int WM, int WN, int RING, Out OUT>
+void launch_ring(const ProductArgs &a, void *stream) {
+    launch_tiles<RingKernel<E, BM, BN, WM, WN, RING, OUT>, BM>(
+        dense_ring_kernel<E, BM, BN, WM, WN, RING, OUT>, a, stream);
+}
+template <class E, int BM, int BN, int WM, int WN, int HELD, Out OUT>
+void launch_tile(const ProductArgs &a, void *stream) {
+    launch_tiles<TileKernel<E, BM, BN, WM, WN, HELD, OUT>, BM>(
+        dense_tile_kernel<E, BM, BN, WM, WN, HELD, OUT>, a, stream);
+}
+template <int BM, int BN, int WM, int WN, Out OUT>
+void launch_split(const ProductArgs &a, bool aligned, void *stream) {
+    using K = SplitKernel<BM, BN, WM, WN, true, OUT>;
+    if constexpr (OUT != Out::kStore)    // the gradients' operands are laid out by the library
+        if (!aligned)
+            return launch_tiles<K, BM>(dense_split_kernel<BM, BN, WM, WN, false, OUT>, a, stream);
+    launch_tiles<K, BM>(dense_split_kernel<BM, BN, WM, WN, true, OUT>, a, stream);
 }
 
 template <class E, int NT, Out OUT>
@@ -65,23 +67,28 @@ template <class E, Out OUT> void launch_product(const ProductArgs &a, void *stre
     auto tiles = [&](int bm, int bn) { return ((a.M + bm - 1) / bm) * ((rows + bn - 1) / bn); };
     if constexpr (sizeof(E) == 4) {
         if (tiles(128, 128) >= 160)
-            launch_tile<E, 128, 128, 4, 2, OUT>(a, aligned, stream);
+            launch_split<128, 128, 4, 2, OUT>(a, aligned, stream);
         else
-            launch_tile<E, 64, 64, 2, 2, OUT>(a, aligned, stream);
-    } else if (aligned) {
-        if (tiles(256, 256) >= 192)
-            launch_ring<E, 256, 256, 2, 4, OUT>(a, stream);
-        else if (tiles(128, 128) >= 192)
-            launch_ring<E, 128, 128, 2, 2, OUT>(a, stream);
-        else
-            launch_ring<E, 64, 64, 2, 2, OUT>(a, stream);
+            launch_split<64, 64, 4, 2, OUT>(a, aligned, stream);
+        return;
     } else {
+        if constexpr (OUT != Out::kStore) {
+            if (!aligned) {
+                if (tiles(256, 256) >= 192)
+                    launch_tile<E, 256, 256, 2, 4, 1, OUT>(a, stream);
+                else if (tiles(128, 128) >= 192)
+                    launch_tile<E, 128, 128, 2, 2, 1, OUT>(a, stream);
+                else
+                    launch_tile<E, 64, 64, 2, 2, 3, OUT>(a, stream);
+                return;
+            }
+        }
         if (tiles(256, 256) >= 192)
-            launch_tile<E, 256, 256, 2, 4, OUT>(a, false, stream);
+            launch_ring<E, 256, 256, 2, 4, 4, OUT>(a, stream);
         else if (tiles(128, 128) >= 192)
-            launch_tile<E, 128, 128, 2, 2, OUT>(a, false, stream);
+            launch_ring<E, 128, 128, 2, 2, 4, OUT>(a, stream);
         else
-            launch_tile<E, 64, 64, 2, 2, OUT>(a, false, stream);
+            launch_ring<E, 64, 64, 2, 2, 8, OUT>(a, stream);
     }
 }
 
@@ -129,65 +136,125 @@ void gated(const void *X, int64_t T_, int64_t ldx, const float *sx, const bsr_ga
 // weights are transposed.  Padding keeps every row 16-byte aligned and holds zeros.
 
 constexpr int kT = 64;   // tile of the transposing kernels
+template <class T> constexpr int kV = 16 / int(sizeof(T));      // elements of 16 bytes
+
+// A kT x kT tile in LDS, written by rows and read by columns, 16 bytes of the matrices at a time.
+// The pitch of 2 elements more puts the rows of a column that consecutive lanes read on different
+// banks.
+template <class T> struct TransposeTile {
+    T cell[kT][kT + 2];
+    __device__ __forceinline__ void put(int row, int col, const T (&v)[kV<T>]) {
+#pragma unroll
+        for (int i = 0; i < kV<T>; ++i) cell[row][col + i] = v[i];
+    }
+    // out[c][r] for the tile at rows r0 (a multiple of 64), columns c0: `C` columns exist, out's rows
+    // have `pad` elements (a multiple of 16 bytes).
+    __device__ __forceinline__ void store(T *out, int64_t ldo, int64_t r0, int64_t c0, int64_t C,
+                                          int64_t pad) const {
+        constexpr int per = kT / kV<T>;
+        for (int e = threadIdx.x; e < kT * per; e += kThreads) {
+            const int c = e / per, r = e % per * kV<T>;
+            if (c0 + c >= C || r0 + r >= pad) continue;
+            T v[kV<T>];
+#pragma unroll
+            for (int i = 0; i < kV<T>; ++i) v[i] = cell[r + i][c];
+            __builtin_memcpy(out + (c0 + c) * ldo + r0 + r, v, 16);
+        }
+    }
+};
+
+// kV elements p[0 .. n), the rest zero.
+template <class T> __device__ __forceinline__ void load_some(const T *p, int64_t n, T (&v)[kV<T>]) {
+    if (n >= kV<T>) {
+        __builtin_memcpy(v, p, 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kV<T>; ++i) v[i] = i < n ? p[i] : T{};
+    }
+}
 
 // out[c][r] = in[r][c] for r < R, c < C; out's rows are padded with zeros to `pad` columns.
 template <class T>
 __global__ __launch_bounds__(kThreads) void transpose_kernel(const T *__restrict__ in, int64_t ldi,
                                                              int64_t R, int64_t C, T *__restrict__ out,
                                                              int64_t ldo, int64_t pad) {
-    __shared__ T tile[kT][kT + 2];
+    __shared__ TransposeTile<T> tile;
     const int64_t r0 = int64_t(blockIdx.x) * kT, c0 = int64_t(blockIdx.y) * kT;
-    const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
-    for (int i = y; i < kT; i += kThreads / 64)
-        tile[i][x] = r0 + i < R && c0 + x < C ? in[(r0 + i) * ldi + c0 + x] : T{};
+    constexpr int per = kT / kV<T>;
+#pragma unroll
+    for (int e = threadIdx.x; e < kT * per; e += kThreads) {
+        const int r = e / per, c = e % per * kV<T>;
+        T v[kV<T>];
+        load_some(in + (r0 + r) * ldi + c0 + c, r0 + r < R ? C - c0 - c : 0, v);
+        tile.put(r, c, v);
+    }
     __syncthreads();
-    for (int i = y; i < kT; i += kThreads / 64)
-        if (c0 + i < C && r0 + x < pad) out[(c0 + i) * ldo + r0 + x] = tile[x][i];
+    tile.store(out, ldo, r0, c0, C, pad);
 }
 
 // D[t][f] = dH U act'(G), D[t][Fp + f] = dH act(G), the transpose Dt[f][t], Dt[F + f][t], and the
-// sums of their columns over the tile's tokens.
+// sums of their columns over the tile's tokens.  Memory bound: 16 bytes of D (4 or 8 hidden units of
+// a token) per thread and pass.
 template <class T, int ACT>
 __global__ __launch_bounds__(kThreads) void gated_slope_kernel(
     const T *__restrict__ dH, int64_t lddh, const float *__restrict__ G,
     const float *__restrict__ U, int64_t ldp, int64_t T_, int64_t F, T *__restrict__ D, int64_t Fp,
     T *__restrict__ Dt, int64_t Tp, float *__restrict__ partial) {
-    __shared__ T tg[kT][kT + 2], tu[kT][kT + 2];
-    __shared__ float sg[kThreads / 64][kT], su[kThreads / 64][kT];
+    constexpr int V = kV<T>, per = kT / V, kRows = kThreads / per;
+    __shared__ TransposeTile<T> tg, tu;
+    __shared__ float sums[2][kRows][kT + 1];
     const int64_t t0 = int64_t(blockIdx.x) * kT, f0 = int64_t(blockIdx.y) * kT;
-    const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
+    const int y = threadIdx.x / per, x = threadIdx.x % per * V;
     const int64_t f = f0 + x;
-    float pg = 0.0f, pu = 0.0f;
-    for (int i = y; i < kT; i += kThreads / 64) {
-        const int64_t t = t0 + i;
-        float dg = 0.0f, du = 0.0f;
-        if (t < T_ && f < F) {
-            float a, da;
-            activate_slope<ACT>(G[t * ldp + f], a, da);
-            const float dh = to_float(dH[t * lddh + f]);
-            dg = dh * U[t * ldp + f] * da;
-            du = dh * a;
+    float pg[V] = {}, pu[V] = {};
+#pragma unroll
+    for (int i = y; i < kT; i += kRows) {
+        const int64_t t = t0 + i, n = t < T_ ? F - f : 0;
+        T dh[V], dg[V], du[V];
+        float g[V], u[V];
+        load_some(dH + t * lddh + f, n, dh);
+        if (n >= V) {
+            __builtin_memcpy(g, G + t * ldp + f, sizeof g);
+            __builtin_memcpy(u, U + t * ldp + f, sizeof u);
+        } else {
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                g[j] = j < n ? G[t * ldp + f + j] : 0.0f;
+                u[j] = j < n ? U[t * ldp + f + j] : 0.0f;
+            }
         }
-        pg += dg;
-        pu += du;
-        tg[i][x] = from_float<T>(dg);
-        tu[i][x] = from_float<T>(du);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            float a, da;
+            activate_slope<ACT>(g[j], a, da);
+            const float h = to_float(dh[j]);
+            const float vg = j < n ? h * u[j] * da : 0.0f, vu = j < n ? h * a : 0.0f;
+            pg[j] += vg;
+            pu[j] += vu;
+            dg[j] = from_float<T>(vg);
+            du[j] = from_float<T>(vu);
+        }
+        tg.put(i, x, dg);
+        tu.put(i, x, du);
         if (t < T_ && f < Fp) {
-            D[t * 2 * Fp + f] = tg[i][x];
-            D[t * 2 * Fp + Fp + f] = tu[i][x];
+            __builtin_memcpy(D + t * 2 * Fp + f, dg, 16);
+            __builtin_memcpy(D + t * 2 * Fp + Fp + f, du, 16);
         }
     }
-    sg[y][x] = pg;
-    su[y][x] = pu;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        sums[0][y][x + j] = pg[j];
+        sums[1][y][x + j] = pu[j];
+    }
     __syncthreads();
-    for (int i = y; i < kT; i += kThreads / 64)
-        if (f0 + i < F && t0 + x < Tp) {
-            Dt[(f0 + i) * Tp + t0 + x] = tg[x][i];
-            Dt[(F + f0 + i) * Tp + t0 + x] = tu[x][i];
-        }
-    if (y == 0 && f < F) {
-        partial[int64_t(blockIdx.x) * 2 * F + f] = (sg[0][x] + sg[1][x]) + (sg[2][x] + sg[3][x]);
-        partial[int64_t(blockIdx.x) * 2 * F + F + f] = (su[0][x] + su[1][x]) + (su[2][x] + su[3][x]);
+    tg.store(Dt, Tp, t0, f0, F, Tp);
+    tu.store(Dt + F * Tp, Tp, t0, f0, F, Tp);
+    if (threadIdx.x < 2 * kT) {
+        const int which = threadIdx.x / kT, c = threadIdx.x % kT;
+        float s = 0.0f;
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) s += sums[which][r][c];
+        if (f0 + c < F) partial[int64_t(blockIdx.x) * 2 * F + which * F + f0 + c] = s;
     }
 }
 

@@ -1,12 +1,13 @@
 // The tiled product (dense_tile.h) for bf16 and int8 rows on 16-byte boundaries: global memory goes
-// straight into LDS, four steps deep.
+// straight into LDS, several steps deep.
 //
 // A step of the contraction takes 64 bytes of every row: one 16-byte operand chunk per lane, one
-// matrix instruction per pair of fragments.  LDS holds a ring of four steps.  While the matrix
+// matrix instruction per pair of fragments.  LDS holds a ring of RING steps.  While the matrix
 // instructions of step s run, their operands for step s + 1 are read from the ring into the
-// registers that step s frees one by one, and step s + 3 is being written into the place of step
-// s - 1, which every wave had read by the last barrier.  So no wave waits for LDS after a barrier,
-// and a load has two whole steps (about 2000 cycles) to arrive.
+// registers that step s frees one by one, and step s + RING - 1 is being written into the place of
+// step s - 1, which every wave had read by the last barrier.  So no wave waits for LDS after a
+// barrier, and a load has RING - 2 whole steps to arrive: two of 1000 cycles for the largest tile,
+// more and shorter ones for the small tiles.
 //
 // One workgroup of 256 x 256 outputs fills a CU: 8 waves of 128 x 64, 128 KB of LDS.  At 8192^3
 // (MI355X) it runs at 1.23-1.27 Pflop/s in bf16 and 2.3 Pop/s in int8, within 6% of the library
@@ -18,7 +19,7 @@
 
 namespace bsr {
 
-template <class E, int BM, int BN, int WM, int WN, Out OUT> struct RingKernel {
+template <class E, int BM, int BN, int WM, int WN, int RING, Out OUT> struct RingKernel {
     static constexpr bool kDual = OUT == Out::kGated;
     static constexpr int kWaves = WM * WN;
     static constexpr int kThreads = 64 * kWaves;
@@ -30,16 +31,16 @@ template <class E, int BM, int BN, int WM, int WN, Out OUT> struct RingKernel {
     static constexpr int PA = (BM / 16 + kWaves - 1) / kWaves, PB = (BN / 16 + kWaves - 1) / kWaves;
     static constexpr int kRowsA = PA * kWaves * 16, kRowsB = PB * kWaves * 16;
     static constexpr int kStageBytes = (kRowsA + kRowsB) * kRowBytes;
-    static constexpr int kRing = 4;
     static constexpr int kEpiBytes = kWaves * epilogue_bytes(NN);
-    static constexpr int kLds = kRing * kStageBytes > kEpiBytes ? kRing * kStageBytes : kEpiBytes;
+    static constexpr int kLds = RING * kStageBytes > kEpiBytes ? RING * kStageBytes : kEpiBytes;
     static constexpr int kTileN = kDual ? BN / 2 : BN;
     using M_ = Mma<E>;
     using Acc = typename M_::Acc;
     static_assert(BM % 16 == 0 && BN % 16 == 0 && TM % kMF == 0 && TN % kMF == 0, "whole blocks");
     static_assert(!kDual || (NN % 2 == 0 && kWaves % 2 == 0), "gate and up blocks in pairs");
     static_assert(kLds <= 160 * 1024, "LDS of a CU");
-    static_assert(PA + PB < 16, "vmcnt fits the immediate's low bits");
+    static constexpr int kAhead = (RING - 3) * (PA + PB);   // loads in flight across a barrier
+    static_assert(RING >= 4 && kAhead < 64, "vmcnt");
 
     typedef __attribute__((address_space(3))) char lds_char;
     typedef __attribute__((address_space(3))) void lds_void;
@@ -49,46 +50,39 @@ template <class E, int BM, int BN, int WM, int WN, Out OUT> struct RingKernel {
     // All but this wave's last N loads into LDS have arrived.
     template <int N> static __device__ __forceinline__ void wait_loads() {
         pin();
-        __builtin_amdgcn_s_waitcnt(0x0f70 | N);   // vmcnt(N)
+        __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | (N >> 4) << 14);   // vmcnt(N)
     }
 
     static __device__ __forceinline__ void run(const ProductArgs &a, char *lds) {
         const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
         const int wm = wave % WM, wn = wave / WM;
-        int tm, tn;
-        tile_of(a, tm, tn);
-        const int64_t m0 = int64_t(tm) * BM, n0 = int64_t(tn) * kTileN;
-        const int64_t left_m = a.M - m0, left_n = a.N - n0;
-        const int rows_m = int(left_m < BM ? left_m : BM);
-        const int rows_n = int(left_n < kTileN ? left_n : kTileN);
-
+        const TileRows<BM, kTileN, kDual> rows(a);
         // Group g holds rows 16 g ..; DUAL: gate rows where g is even, up rows where it is odd.  A
         // wave's groups g = i * kWaves + wave are all of one kind.
         const bool up = kDual && (wave & 1);
-        const char *pb = up ? a.B1 + n0 * a.ldb1 : a.B0 + n0 * a.ldb0;
-        const int64_t ldb = up ? a.ldb1 : a.ldb0;
-        const auto rsa = buffer_rsrc(a.A + m0 * a.lda, unsigned((rows_m - 1) * a.lda) + unsigned(a.Kb));
-        const auto rsb = buffer_rsrc(pb, unsigned((rows_n - 1) * ldb) + unsigned(a.Kb));
-        // Lane -> row lane / 4 of the group, 16 bytes at position lane % 4 of its 64, which holds
-        // chunk (lane % 4) ^ (row / 4) % 4: the permutation that spreads a fragment's reads over the
-        // banks, made on the way in.  Offsets from `kOut` on are out of every range and load zeros.
+        const Source &sa = rows.a, &sb = up ? rows.b1 : rows.b0;
+        const auto rsa = buffer_rsrc(sa.base, unsigned((sa.rows - 1) * sa.pitch) + unsigned(a.Kb));
+        const auto rsb = buffer_rsrc(sb.base, unsigned((sb.rows - 1) * sb.pitch) + unsigned(a.Kb));
+        // A group's 1024 bytes in LDS are written in lane order, so a lane loads what belongs in its
+        // place there: line lane / 8, position lane % 8 of half_row_at's layout.  Offsets from `kOut`
+        // on are out of every range and load zeros.
         constexpr unsigned kOut = 0x80000000u;
-        const int row = lane >> 2, c = (lane & 3) ^ ((lane >> 4) & 3);
+        const int place = (lane & 7) ^ (lane >> 3), row = (lane >> 3) * 2 + (place >> 2), c = place & 3;
         unsigned oa[PA], ob[PB];
 #pragma unroll
         for (int i = 0; i < PA; ++i) {
             const int r = (i * kWaves + wave) * 16 + row;
-            oa[i] = r < rows_m ? unsigned(r) * unsigned(a.lda) + c * kChunk : kOut;
+            oa[i] = r < sa.rows ? unsigned(r) * unsigned(sa.pitch) + c * kChunk : kOut;
         }
 #pragma unroll
         for (int i = 0; i < PB; ++i) {
             const int g = i * kWaves + wave, r = (kDual ? g >> 1 : g) * 16 + row;
-            ob[i] = r < rows_n ? unsigned(r) * unsigned(ldb) + c * kChunk : kOut;
+            ob[i] = r < sb.rows ? unsigned(r) * unsigned(sb.pitch) + c * kChunk : kOut;
         }
         auto load = [&](int s) {
             const int kb = s * kRowBytes;
             const bool in = kb + c * kChunk < a.Kb;      // chunks past the row's end: zeros
-            lds_char *to = (lds_char *)lds + (s % kRing) * kStageBytes + wave * 1024;
+            lds_char *to = (lds_char *)lds + (s % RING) * kStageBytes + wave * 1024;
 #pragma unroll
             for (int i = 0; i < PA; ++i)
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(rsa, (lds_void *)(to + i * kWaves * 1024), 16,
@@ -102,9 +96,8 @@ template <class E, int BM, int BN, int WM, int WN, Out OUT> struct RingKernel {
 
         Acc acc[NN][NM] = {};
         const int fr = lane % kMF, fc = lane / kMF;
-        const int at = (fc ^ ((fr >> 2) & 3)) * kChunk;
-        const int at_a = (wm * TM + fr) * kRowBytes + at;
-        const int at_b = (kRowsA + wn * TN + fr) * kRowBytes + at;
+        const int at_a = wm * TM * kRowBytes + half_row_at(fr, fc);
+        const int at_b = (kRowsA + wn * TN) * kRowBytes + half_row_at(fr, fc);
         auto fetch_a = [&](const char *p, int i) {
             return *reinterpret_cast<const i32x4 *>(p + at_a + i * kMF * kRowBytes);
         };
@@ -113,10 +106,9 @@ template <class E, int BM, int BN, int WM, int WN, Out OUT> struct RingKernel {
         };
         i32x4 fa[NM], fb[2][NN];
         const int steps = (a.Kb + kRowBytes - 1) / kRowBytes;
-        load(0);
-        load(1);
-        load(2);
-        wait_loads<PA + PB>();         // steps 0 and 1 are there
+#pragma unroll
+        for (int s = 0; s < RING - 1; ++s) load(s);
+        wait_loads<kAhead>();          // steps 0 and 1 are there
         __builtin_amdgcn_s_barrier();
         pin();
 #pragma unroll
@@ -124,20 +116,20 @@ template <class E, int BM, int BN, int WM, int WN, Out OUT> struct RingKernel {
 #pragma unroll
         for (int i = 0; i < NM; ++i) fa[i] = fetch_a(lds, i);
         auto step = [&](int s, const i32x4 (&now)[NN], i32x4 (&then)[NN]) {
-            const char *p = lds + ((s + 1) % kRing) * kStageBytes;
+            const char *p = lds + ((s + 1) % RING) * kStageBytes;
 #pragma unroll
             for (int i = 0; i < NM; ++i) {
 #pragma unroll
                 for (int j = 0; j < NN; ++j) acc[j][i] = M_::step(now[j], fa[i], acc[j][i]);
                 fa[i] = fetch_a(p, i);
-                if (i == 0) load(s + 3);
+                if (i == 0) load(s + RING - 1);
                 // the channels' fragments, spread over the rest of the step
 #pragma unroll
                 for (int j = 0; j < NN; ++j)
                     if (j * NM / NN == i) then[j] = fetch_b(p, j);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            wait_loads<PA + PB>();     // step s + 2 is there
+            wait_loads<kAhead>();      // step s + 2 is there
             __builtin_amdgcn_s_barrier();
             pin();
         };
@@ -150,13 +142,13 @@ template <class E, int BM, int BN, int WM, int WN, Out OUT> struct RingKernel {
         wait_loads<0>();               // what was loaded past the end, before LDS is used again
         __syncthreads();
         epilogue<E, OUT, NN, NM>(a, acc, reinterpret_cast<float *>(lds + wave * epilogue_bytes(NN)),
-                                 m0 + wm * TM, n0 + wn * (kDual ? TN / 2 : TN));
+                                 rows.m0 + wm * TM, rows.n0 + wn * (kDual ? TN / 2 : TN));
     }
 };
 
-template <class E, int BM, int BN, int WM, int WN, Out OUT>
+template <class E, int BM, int BN, int WM, int WN, int RING, Out OUT>
 __global__ __launch_bounds__(64 * WM * WN) void dense_ring_kernel(ProductArgs a) {
-    using K = RingKernel<E, BM, BN, WM, WN, OUT>;
+    using K = RingKernel<E, BM, BN, WM, WN, RING, OUT>;
     __shared__ __align__(16) char lds[K::kLds];
     K::run(a, lds);
 }

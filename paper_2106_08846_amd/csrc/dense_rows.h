@@ -35,20 +35,22 @@ template <class E, int NT, bool ALIGNED, Out OUT> struct RowsKernel {
                               {kDual ? a.B1 + n0 * a.ldb1 : nullptr, a.ldb1, rows}};
         const int fr = lane & 15, fc = lane >> 4;
         Acc acc[NW][NT] = {};
+        RowChunks<E, ALIGNED> cw[NW], cx[NT];
+#pragma unroll
+        for (int j = 0; j < NW; ++j) cw[j].set(sw[j], fr, fc * kChunk, a.Kb);
+#pragma unroll
+        for (int i = 0; i < NT; ++i) cx[i].set(sx, 16 * i + fr, fc * kChunk, a.Kb);
         for (int kb = wave * kBlock; kb < a.Kb; kb += kWaves * kBlock) {
+            const int left = a.Kb - fc * kChunk - kb;
             i32x4 w[kHeld][NW], x[kHeld][NT];
 #pragma unroll
-            for (int s = 0; s < kHeld; ++s) {
-                const int at = kb + s * 64 + fc * kChunk;
+            for (int s = 0; s < kHeld; ++s)
 #pragma unroll
-                for (int j = 0; j < NW; ++j) w[s][j] = load_chunk<E, ALIGNED>(sw[j], fr, at, a.Kb);
-            }
+                for (int j = 0; j < NW; ++j) w[s][j] = cw[j].load(kb + s * 64, left - s * 64);
 #pragma unroll
-            for (int s = 0; s < kHeld; ++s) {
-                const int at = kb + s * 64 + fc * kChunk;
+            for (int s = 0; s < kHeld; ++s)
 #pragma unroll
-                for (int i = 0; i < NT; ++i) x[s][i] = load_chunk<E, ALIGNED>(sx, 16 * i + fr, at, a.Kb);
-            }
+                for (int i = 0; i < NT; ++i) x[s][i] = cx[i].load(kb + s * 64, left - s * 64);
 #pragma unroll
             for (int s = 0; s < kHeld; ++s)
 #pragma unroll

@@ -7,14 +7,12 @@
 // rows, so that one lane holds the gate and the up value of the same outputs.  A lane's operand of
 // one matrix instruction is 16 consecutive bytes of one row: 8 bf16 for 16x16x32 or 16 int8 for
 // 16x16x64.  (32x32 instructions move the same bytes per product and ran the 8192^3 product 5%
-// slower.)  fp32 operands are split into three bf16 pieces on their way into LDS, see Pieces.
+// slower.)
 //
-// Here: what the tile kernels share, and the kernel that takes its operands through registers into
-// LDS: for rows that start on no 16-byte boundary, and for fp32.  Rows on 16-byte boundaries go
-// straight into LDS in dense_ring.h.
+// Here: what the tile kernels share, and the one for bf16 and int8 rows that start on no 16-byte
+// boundary.  Rows on 16-byte boundaries go straight into LDS in dense_ring.h; fp32 is in
+// dense_split.h.
 #pragma once
-
-#include <type_traits>
 
 #include "dense_math.h"
 
@@ -50,28 +48,6 @@ template <> struct Mma<float> {
         return c;
     }
 };
-
-// fp32 values as sums of three bf16 pieces, x = h + m + l: h is x rounded to bf16, m the remainder
-// rounded, l what is left, which has 8 significant bits (|m| <= 2^-9 |x|, |l| <= 2^-18 |x|; exact
-// while l does not underflow, |x| >= 2^-100).  A product x y is formed from the six cross terms down
-// to 2^-18 |x y| (hh, hm, mh, hl, lh, mm), each exact in fp32; the three left out are together below
-// 2^-25.9 |x y|, a quarter of fp32's own rounding.  Six bf16 instructions take 96 cycles for what
-// the fp32 instructions need 256 for.  An infinite operand (or one that rounds to infinity in bf16,
-// from 2^128 (1 - 2^-9) on) gives NaN.
-struct Pieces {
-    bf16x4 h, m, l;
-};
-__device__ __forceinline__ Pieces split(f32x4 x) {
-    Pieces p;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        p.h[i] = static_cast<__bf16>(x[i]);
-        const float r = x[i] - static_cast<float>(p.h[i]);
-        p.m[i] = static_cast<__bf16>(r);
-        p.l[i] = static_cast<__bf16>(r - static_cast<float>(p.m[i]));
-    }
-    return p;
-}
 
 // What becomes of the product.
 enum class Out { kStore, kScale, kGated };
@@ -186,37 +162,45 @@ struct Source {   // one operand's rows as a workgroup reads them
     int rows;             // rows that exist, at least 1
 };
 
-// The 16 bytes at byte kb of row `row`, those from Kb on and those of a row that does not exist
-// being zero.  ALIGNED: rows start on 16-byte boundaries and Kb is a multiple of 16, so chunks are
-// loaded whole through a range-checked buffer load; otherwise byte-aligned loads, with the last
-// chunk of a row put together from what it has.
-template <class E, bool ALIGNED>
-__device__ __forceinline__ i32x4 load_chunk(const Source &s, int row, int kb, int Kb) {
-    if constexpr (ALIGNED) {
-        // Every existing row ends at or before byte (rows - 1) * pitch + Kb; a row past the end is
-        // out of that range by itself, a chunk past Kb is sent there.
-        const unsigned bytes = unsigned((s.rows - 1) * s.pitch) + unsigned(Kb);
-        const unsigned off = kb < Kb ? unsigned(row) * unsigned(s.pitch) + unsigned(kb) : 0x80000000u;
-        return __builtin_bit_cast(
-            i32x4, __builtin_amdgcn_raw_buffer_load_b128(buffer_rsrc(s.base, bytes), off, 0, 0));
-    } else {
-        i32x4 v = {0, 0, 0, 0};
-        if (row >= s.rows || kb >= Kb) return v;
-        const char *p = s.base + row * s.pitch + kb;
-        if (Kb - kb >= kChunk) {
-            __builtin_memcpy(&v, p, kChunk);
-        } else {
-            const E *e = reinterpret_cast<const E *>(p);
-            const int n = (Kb - kb) / int(sizeof(E));
-            E tail[kChunk / sizeof(E)] = {};
-#pragma unroll
-            for (int i = 0; i < int(kChunk / sizeof(E)); ++i)
-                if (i < n) tail[i] = e[i];
-            __builtin_memcpy(&v, tail, kChunk);
-        }
-        return v;
+// One lane's view of a row: the 16-byte chunk at byte `col` of it, and those at `col` plus whole steps.
+// Rows past the end stand for the last one: what they give reaches only outputs that do not exist.
+// ALIGNED: rows start on 16-byte boundaries and Kb is a multiple of 16, so chunks are loaded whole
+// through a range-checked buffer load; otherwise byte-aligned loads, with the last chunk of a row put
+// together from what it has.
+template <class E, bool ALIGNED> struct RowChunks {
+    const char *base;     // uniform
+    unsigned bytes, off;
+
+    __device__ __forceinline__ void set(const Source &s, int row, int col, int Kb) {
+        base = s.base;
+        bytes = unsigned((s.rows - 1) * s.pitch) + unsigned(Kb);
+        off = unsigned(row < s.rows ? row : s.rows - 1) * unsigned(s.pitch) + unsigned(col);
     }
-}
+    // The chunk `kb` bytes further on, `left` = Kb - col - kb bytes of which are left in the row; zeros
+    // past its end.
+    __device__ __forceinline__ i32x4 load(int kb, int left) const {
+        if constexpr (ALIGNED) {
+            const unsigned at = left > 0 ? off + unsigned(kb) : 0x80000000u;    // out of range: zeros
+            return __builtin_bit_cast(
+                i32x4, __builtin_amdgcn_raw_buffer_load_b128(buffer_rsrc(base, bytes), at, 0, 0));
+        } else {
+            i32x4 v = {0, 0, 0, 0};
+            const char *p = base + (off + unsigned(kb));
+            if (left >= kChunk) {
+                __builtin_memcpy(&v, p, kChunk);
+            } else if (left > 0) {
+                const E *e = reinterpret_cast<const E *>(p);
+                const int n = left / int(sizeof(E));
+                E tail[kChunk / sizeof(E)] = {};
+#pragma unroll
+                for (int i = 0; i < int(kChunk / sizeof(E)); ++i)
+                    if (i < n) tail[i] = e[i];
+                __builtin_memcpy(&v, tail, kChunk);
+            }
+            return v;
+        }
+    }
+};
 
 // The tile of this workgroup.  Workgroups go round robin over the 8 XCDs: XCD x takes a contiguous
 // run of the tile order, and that order walks bands of 8 token tiles, so the tiles an XCD works on
@@ -231,6 +215,43 @@ __device__ __forceinline__ void tile_of(const ProductArgs &a, int &tm, int &tn) 
     const int in = t - first * a.tiles_n;
     tm = first + in % height;
     tn = in / height;
+}
+
+// The rows of both operands that a workgroup's tile takes: BM tokens, kTileN channels of each of B's
+// matrices.
+template <int BM, int kTileN, bool DUAL> struct TileRows {
+    int64_t m0, n0;
+    Source a, b0, b1;
+
+    __device__ __forceinline__ explicit TileRows(const ProductArgs &p) {
+        int tm, tn;
+        tile_of(p, tm, tn);
+        m0 = int64_t(tm) * BM;
+        n0 = int64_t(tn) * kTileN;
+        const int64_t left_m = p.M - m0, left_n = p.N - n0;
+        const int rows_n = int(left_n < kTileN ? left_n : kTileN);
+        a = Source{p.A + m0 * p.lda, p.lda, int(left_m < BM ? left_m : BM)};
+        b0 = Source{p.B0 + n0 * p.ldb0, p.ldb0, rows_n};
+        b1 = DUAL ? Source{p.B1 + n0 * p.ldb1, p.ldb1, rows_n} : b0;
+    }
+    // Row `row` of the tile's B is row `channel(row)` of this source; `first` is the first row that
+    // the wave's lanes ask for (uniform; at most 16 rows, from a multiple of their number on).  DUAL:
+    // row (pair * 2 + which) * 16 + r stands for channel pair * 16 + r.
+    __device__ __forceinline__ const Source &b(int first) const {
+        return DUAL && ((first / kMF) & 1) ? b1 : b0;
+    }
+    static __device__ __forceinline__ int channel(int row) {
+        return DUAL ? row / (2 * kMF) * kMF + row % kMF : row;
+    }
+};
+
+// LDS layout of rows of 64 bytes: two rows to a line of 128, whose 16-byte chunks are permuted by the
+// line's number.  A wave's read of 16 rows then meets every bank once in each of the groups of 16
+// lanes that a 16-byte read is served in (lanes 0-3, 12-15, 20-23, 24-27 and so on); permuting each
+// row's four chunks by row / 4 instead gave two-way conflicts, measured as twice the LDS cycles.
+__device__ __forceinline__ int half_row_at(int row, int c) {
+    const int line = row >> 1;
+    return line * 128 + ((((row & 1) << 2) | c) ^ (line & 7)) * kChunk;
 }
 
 // Order LDS accesses of one wave's lanes among themselves.
@@ -283,29 +304,25 @@ __device__ __forceinline__ void epilogue(const ProductArgs &a, const Acc (&acc)[
     }
 }
 
-// BM x BN tile, WM x WN waves, operands through registers.  A step of the contraction takes 128
-// bytes of every row (64 bf16, 128 int8, 32 fp32): its chunks are loaded one step before they are
-// written into LDS and two before they are used, and written between the halves of a step's matrix
-// instructions (10% faster at 8192^3 than loading and writing the next step around all of them).
-template <class E, int BM, int BN, int WM, int WN, bool ALIGNED, Out OUT> struct TileKernel {
+// BM x BN tile, WM x WN waves, for bf16 and int8 rows that start on no 16-byte boundary: operands go
+// through registers into LDS.  A step of the contraction takes 128 bytes of every row (64 bf16, 128
+// int8): its chunks are loaded HELD steps before they are written into LDS and HELD + 1 before they
+// are used (small tiles, whose steps are shorter than a load, hold three), and written between the
+// halves of a step's matrix instructions (10% faster at 8192^3 than around all of them).
+template <class E, int BM, int BN, int WM, int WN, int HELD, Out OUT> struct TileKernel {
     static constexpr bool kDual = OUT == Out::kGated;
-    static constexpr bool kSplit = sizeof(E) == 4;       // fp32 in three pieces
-    static constexpr int kPlanes = kSplit ? 3 : 1;
     static constexpr int kThreads = 64 * WM * WN;
     static constexpr int TM = BM / WM, TN = BN / WN;     // a wave's tokens and channels
     static constexpr int NM = TM / kMF, NN = TN / kMF;
-    static constexpr int kStepBytes = 128;
-    static constexpr int kRowChunks = kStepBytes / kChunk;
-    static constexpr int kRowBytes = kSplit ? 64 : 128;  // of a row (and piece) in LDS
-    static constexpr int kSteps = kRowBytes / 64;        // matrix-instruction steps
+    static constexpr int kRowBytes = 128;
+    static constexpr int kRowChunks = kRowBytes / kChunk;
     static constexpr int kRowsPerPass = kThreads / kRowChunks;
     static constexpr int LA = BM / kRowsPerPass, LB = BN / kRowsPerPass;   // chunks per thread
-    static constexpr int kPlaneBytes = (BM + BN) * kRowBytes;
-    static constexpr int kStageBytes = kPlanes * kPlaneBytes;
+    static constexpr int kStageBytes = (BM + BN) * kRowBytes;
     static constexpr int kEpiBytes = WM * WN * epilogue_bytes(NN);
     static constexpr int kLds = 2 * kStageBytes > kEpiBytes ? 2 * kStageBytes : kEpiBytes;
     static constexpr int kTileN = kDual ? BN / 2 : BN;   // channels per tile
-    using M_ = Mma<typename std::conditional<kSplit, bf16, E>::type>;
+    using M_ = Mma<E>;
     using Acc = typename M_::Acc;
     static_assert(BM % kRowsPerPass == 0 && BN % kRowsPerPass == 0, "whole passes");
     static_assert(!kDual || NN % 2 == 0, "gate and up blocks in pairs");
@@ -313,125 +330,90 @@ template <class E, int BM, int BN, int WM, int WN, bool ALIGNED, Out OUT> struct
 
     // LDS position of 16-byte chunk c of a row: the chunks of a row are permuted by its number, so
     // that a wave's reads of 16 rows spread over all banks (no conflicts counted).
-    static __device__ __forceinline__ int swizzled(int row, int c) {
-        return kRowBytes == 128 ? c ^ ((row >> 1) & 7) : c ^ ((row >> 2) & 3);
-    }
-    // Chunk c (of the source row) of row `row` into the stage at p.
-    static __device__ __forceinline__ void put_chunk(char *p, int row, int c, i32x4 v) {
-        if constexpr (kSplit) {
-            const Pieces s = split(__builtin_bit_cast(f32x4, v));
-            char *q = p + row * kRowBytes + swizzled(row, c >> 1) * kChunk + (c & 1) * 8;
-            *reinterpret_cast<bf16x4 *>(q) = s.h;
-            *reinterpret_cast<bf16x4 *>(q + kPlaneBytes) = s.m;
-            *reinterpret_cast<bf16x4 *>(q + 2 * kPlaneBytes) = s.l;
-        } else {
-            *reinterpret_cast<i32x4 *>(p + row * kRowBytes + swizzled(row, c) * kChunk) = v;
-        }
-    }
+    static __device__ __forceinline__ int swizzled(int row, int c) { return c ^ ((row >> 1) & 7); }
 
     static __device__ __forceinline__ void run(const ProductArgs &a, char *lds) {
         const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
         const int wm = wave % WM, wn = wave / WM;
-        int tm, tn;
-        tile_of(a, tm, tn);
-        const int64_t m0 = int64_t(tm) * BM, n0 = int64_t(tn) * kTileN;
-        const int64_t left_m = a.M - m0, left_n = a.N - n0;
-        const Source sa{a.A + m0 * a.lda, a.lda, int(left_m < BM ? left_m : BM)};
-        const int rows_n = int(left_n < kTileN ? left_n : kTileN);
-        const Source sb0{a.B0 + n0 * a.ldb0, a.ldb0, rows_n};
-        const Source sb1{kDual ? a.B1 + n0 * a.ldb1 : nullptr, a.ldb1, rows_n};
-
+        const TileRows<BM, kTileN, kDual> rows(a);
         const int c = tid & (kRowChunks - 1), r0 = tid / kRowChunks;
         const int wave_row = wave * (64 / kRowChunks);      // first row of this wave in a pass
-        i32x4 ra[LA], rb[LB];
-        auto load = [&](int step) {
-            const int kb = step * kStepBytes + c * kChunk;
-#pragma unroll
-            for (int i = 0; i < LA; ++i)
-                ra[i] = load_chunk<E, ALIGNED>(sa, i * kRowsPerPass + r0, kb, a.Kb);
-#pragma unroll
-            for (int i = 0; i < LB; ++i) {
-                const int row = i * kRowsPerPass + r0;
-                if constexpr (kDual) {
-                    // row = (pair * 2 + which) * 16 + r stands for channel pair * 16 + r
-                    const int first = i * kRowsPerPass + wave_row;      // uniform
-                    const int channel = row / (2 * kMF) * kMF + row % kMF;
-                    const Source &s = (first / kMF) & 1 ? sb1 : sb0;
-                    rb[i] = load_chunk<E, ALIGNED>(s, channel, kb, a.Kb);
-                } else {
-                    rb[i] = load_chunk<E, ALIGNED>(sb0, row, kb, a.Kb);
-                }
-            }
+        struct Held {                        // a step's chunks of this thread
+            i32x4 a[LA], b[LB];
         };
-        auto put = [&](int buf) {
+        Held held[HELD];                     // step k in held[k % HELD], its place in LDS k % 2
+        RowChunks<E, false> ca[LA], cb[LB];
+#pragma unroll
+        for (int i = 0; i < LA; ++i) ca[i].set(rows.a, i * kRowsPerPass + r0, c * kChunk, a.Kb);
+#pragma unroll
+        for (int i = 0; i < LB; ++i)
+            cb[i].set(rows.b(i * kRowsPerPass + wave_row), rows.channel(i * kRowsPerPass + r0),
+                      c * kChunk, a.Kb);
+        auto load = [&](int step, Held &h) { // zeros from Kb on
+            const int kb = step * kRowBytes, left = a.Kb - c * kChunk - kb;
+#pragma unroll
+            for (int i = 0; i < LA; ++i) h.a[i] = ca[i].load(kb, left);
+#pragma unroll
+            for (int i = 0; i < LB; ++i) h.b[i] = cb[i].load(kb, left);
+        };
+        auto put = [&](int buf, const Held &h) {
             char *p = lds + buf * kStageBytes;
 #pragma unroll
-            for (int i = 0; i < LA; ++i) put_chunk(p, i * kRowsPerPass + r0, c, ra[i]);
-#pragma unroll
-            for (int i = 0; i < LB; ++i) put_chunk(p + BM * kRowBytes, i * kRowsPerPass + r0, c, rb[i]);
+            for (int i = 0; i < LA + LB; ++i) {
+                const int row = (i < LA ? i : i - LA) * kRowsPerPass + r0;
+                *reinterpret_cast<i32x4 *>(p + (i < LA ? 0 : BM * kRowBytes) + row * kRowBytes +
+                                           swizzled(row, c) * kChunk) = i < LA ? h.a[i] : h.b[i - LA];
+            }
         };
 
         Acc acc[NN][NM] = {};
         const int fr = lane % kMF, fc = lane / kMF;
-        const int steps = (a.Kb + kStepBytes - 1) / kStepBytes;
-        load(0);
-        put(0);
-        if (steps > 1) load(1);
-        for (int s = 0; s < steps; ++s) {
+        const int steps = (a.Kb + kRowBytes - 1) / kRowBytes;
+#pragma unroll
+        for (int k = 0; k < HELD; ++k) load(k, held[k]);
+        put(0, held[0]);
+        load(HELD, held[0]);
+        // Step s, whose successor waits in h.
+        auto step = [&](int s, Held &h) {
             __syncthreads();
             const char *pa = lds + (s & 1) * kStageBytes + (wm * TM + fr) * kRowBytes;
             const char *pb = lds + (s & 1) * kStageBytes + (BM + wn * TN + fr) * kRowBytes;
-            i32x4 fa[kPlanes][NM], fb[kPlanes][NN];
-            auto fetch = [&](int k) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
                 const int at = swizzled(fr, k * 4 + fc) * kChunk;
+                i32x4 fa[NM], fb[NN];
 #pragma unroll
-                for (int p = 0; p < kPlanes; ++p) {
+                for (int i = 0; i < NM; ++i)
+                    fa[i] = *reinterpret_cast<const i32x4 *>(pa + i * kMF * kRowBytes + at);
 #pragma unroll
-                    for (int i = 0; i < NM; ++i)
-                        fa[p][i] = *reinterpret_cast<const i32x4 *>(pa + p * kPlaneBytes +
-                                                                   i * kMF * kRowBytes + at);
-#pragma unroll
-                    for (int j = 0; j < NN; ++j)
-                        fb[p][j] = *reinterpret_cast<const i32x4 *>(pb + p * kPlaneBytes +
-                                                                   j * kMF * kRowBytes + at);
-                }
-            };
-            // Piece x of B with piece y of A.
-            auto multiply = [&](int x, int y) {
+                for (int j = 0; j < NN; ++j)
+                    fb[j] = *reinterpret_cast<const i32x4 *>(pb + j * kMF * kRowBytes + at);
 #pragma unroll
                 for (int j = 0; j < NN; ++j)
 #pragma unroll
-                    for (int i = 0; i < NM; ++i) acc[j][i] = M_::step(fb[x][j], fa[y][i], acc[j][i]);
-            };
-            auto next = [&] {
-                if (s + 1 < steps) put((s + 1) & 1);
-                if (s + 2 < steps) load(s + 2);
-            };
-            fetch(0);
-            if constexpr (kSplit) {
-                multiply(0, 2);
-                multiply(2, 0);
-                next();
-                multiply(1, 1);
-                multiply(0, 1);
-                multiply(1, 0);
-                multiply(0, 0);
-            } else {
-                multiply(0, 0);
-                next();
-                fetch(1);
-                multiply(0, 0);
+                    for (int i = 0; i < NM; ++i) acc[j][i] = M_::step(fb[j], fa[i], acc[j][i]);
+                if (k == 0) {
+                    put((s + 1) & 1, h);
+                    load(s + 1 + HELD, h);
+                }
+            }
+        };
+        for (int s = 0; s < steps;) {
+#pragma unroll
+            for (int k = 0; k < HELD; ++k) {
+                step(s, held[(k + 1) % HELD]);
+                if (++s >= steps) break;
             }
         }
         __syncthreads();
         epilogue<E, OUT, NN, NM>(a, acc, reinterpret_cast<float *>(lds + wave * epilogue_bytes(NN)),
-                                 m0 + wm * TM, n0 + wn * (kDual ? TN / 2 : TN));
+                                 rows.m0 + wm * TM, rows.n0 + wn * (kDual ? TN / 2 : TN));
     }
 };
 
-template <class E, int BM, int BN, int WM, int WN, bool ALIGNED, Out OUT>
+template <class E, int BM, int BN, int WM, int WN, int HELD, Out OUT>
 __global__ __launch_bounds__(64 * WM * WN) void dense_tile_kernel(ProductArgs a) {
-    using K = TileKernel<E, BM, BN, WM, WN, ALIGNED, OUT>;
+    using K = TileKernel<E, BM, BN, WM, WN, HELD, OUT>;
     __shared__ __align__(16) char lds[K::kLds];
     K::run(a, lds);
 }
