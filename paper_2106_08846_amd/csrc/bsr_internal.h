@@ -94,14 +94,15 @@ bsr_status check_gated_backward(const void *dH, int64_t lddh, const void *X, int
                                 int64_t ldp, const void *dX, int64_t lddx, const void *dWg,
                                 const void *dWu, int64_t lddw, const void *dbg, const void *dbu,
                                 int32_t grad_dtype, const void *workspace, size_t ws_bytes);
-// Workspace of bsr_gated_backward: byte offsets of its regions, each on a 256-byte boundary.  Fp and
-// Tp are F and T rounded up to whole 16-byte chunks.
+// Workspace of bsr_gated_backward: byte offsets of its regions, each on a 256-byte boundary.
 struct GatedWorkspace {
-    int64_t Fp, Tp;
+    int64_t Fp;              // F rounded up to whole steps of 32 (bf16) or 16-byte chunks (fp32)
+    int64_t Kp;              // bf16: K rounded up to whole 16-byte chunks
+    int64_t Tp;              // fp32: T rounded up to whole 16-byte chunks
     size_t grad_offset;      // [T][2 Fp]: dG | dU, of the block's dtype
-    size_t gradt_offset;     // [2 F][Tp]: its transpose
-    size_t xt_offset;        // [K][Tp]: X's transpose
-    size_t wt_offset;        // [K][2 Fp]: the weights' transposes
+    size_t gradt_offset;     // fp32: [2 F][Tp], its transpose
+    size_t x_offset;         // bf16: [T][Kp], a copy of an unaligned X; fp32: [K][Tp], X's transpose
+    size_t w_offset;         // bf16: [2][F][Kp], copies; fp32: [K][2 Fp], the weights' transposes
     size_t partial_offset;   // fp32 [row blocks][2 F]: partial bias gradients
     size_t total;
 };

@@ -22,10 +22,10 @@ void launch_tiles(void (*kernel)(ProductArgs), ProductArgs a, void *stream) {
     hipLaunchKernelGGL(kernel, dim3(unsigned(a.tiles_m) * unsigned(a.tiles_n)), dim3(K::kThreads), 0,
                        as_stream(stream), a);
 }
-template <class E, int BM, int BN, int WM, int WN, int RING, Out OUT>
+template <class E, int BM, int BN, int WM, int WN, int RING, Out OUT, bool COLS_A, bool COLS_B>
 void launch_ring(const ProductArgs &a, void *stream) {
-    launch_tiles<RingKernel<E, BM, BN, WM, WN, RING, OUT>, BM>(
-        dense_ring_kernel<E, BM, BN, WM, WN, RING, OUT>, a, stream);
+    launch_tiles<RingKernel<E, BM, BN, WM, WN, RING, OUT, COLS_A, COLS_B>, BM>(
+        dense_ring_kernel<E, BM, BN, WM, WN, RING, OUT, COLS_A, COLS_B>, a, stream);
 }
 template <class E, int BM, int BN, int WM, int WN, int HELD, Out OUT>
 void launch_tile(const ProductArgs &a, void *stream) {
@@ -54,6 +54,35 @@ bool rows_aligned(const void *p, int64_t ld) {
     return ((reinterpret_cast<uintptr_t>(p) | uintptr_t(ld)) & 15) == 0;
 }
 
+// Rounds of workgroups that tiles of bm x bn take on the chip's CUs, times the cost of a round.
+int64_t rounds(const ProductArgs &a, bool dual, int bm, int bn, int cost) {
+    const int64_t rows = dual ? 2 * a.N : a.N;
+    const int64_t tiles = ((a.M + bm - 1) / bm) * ((rows + bn - 1) / bn), cus = device_cu_count();
+    return (tiles + cus - 1) / cus * cost;
+}
+
+// The tile by the rounds it takes: the costs are microseconds of one round of each at K = 4096 in bf16
+// (MI355X).  At 4096 x 4096 x 4096 256 x 256 tiles take 110 us, 128 x 128 ones 154 and 64 x 64 ones
+// 259; at 2048^3 51, 24 and 33; at 128 x 8192 x 4096 84, 33 and 20; at 6144 x 2048 x 16384, whose 192
+// tiles of 256 x 256 leave a quarter of the CUs idle, 438 against 368 in 192 x 256.
+template <class E, Out OUT, bool COLS_A = false, bool COLS_B = false>
+void launch_ring_product(const ProductArgs &a, void *stream) {
+    constexpr bool dual = OUT == Out::kGated;
+    const int64_t cost[5] = {rounds(a, dual, 256, 256, 110), rounds(a, dual, 192, 256, 85),
+                             rounds(a, dual, 128, 256, 65), rounds(a, dual, 128, 128, 42),
+                             rounds(a, dual, 64, 64, 18)};
+    int best = 0;
+    for (int i = 1; i < 5; ++i)
+        if (cost[i] < cost[best]) best = i;
+    switch (best) {
+        case 0: return launch_ring<E, 256, 256, 2, 4, 4, OUT, COLS_A, COLS_B>(a, stream);
+        case 1: return launch_ring<E, 192, 256, 2, 4, 4, OUT, COLS_A, COLS_B>(a, stream);
+        case 2: return launch_ring<E, 128, 256, 2, 4, 4, OUT, COLS_A, COLS_B>(a, stream);
+        case 3: return launch_ring<E, 128, 128, 2, 4, 4, OUT, COLS_A, COLS_B>(a, stream);
+        default: return launch_ring<E, 64, 64, 2, 2, 8, OUT, COLS_A, COLS_B>(a, stream);
+    }
+}
+
 template <class E, Out OUT> void launch_product(const ProductArgs &a, void *stream) {
     constexpr bool dual = OUT == Out::kGated;
     const bool aligned = a.Kb % 16 == 0 && rows_aligned(a.A, a.lda) && rows_aligned(a.B0, a.ldb0) &&
@@ -63,32 +92,24 @@ template <class E, Out OUT> void launch_product(const ProductArgs &a, void *stre
         if (a.M <= 32) return launch_rows<E, 2, OUT>(a, aligned, stream);
         if (a.M <= 64) return launch_rows<E, 4, OUT>(a, aligned, stream);
     }
-    const int64_t rows = dual ? 2 * a.N : a.N;
-    auto tiles = [&](int bm, int bn) { return ((a.M + bm - 1) / bm) * ((rows + bn - 1) / bn); };
     if constexpr (sizeof(E) == 4) {
-        if (tiles(128, 128) >= 160)
+        // Costs of a round at K = 4096, as above: 1000 x 768 x 3064 takes 102 us in 128 x 128 tiles and
+        // 49 in 64 x 64, 896 x 4096 x 768 36 and 45.
+        if (rounds(a, dual, 128, 128, 168) <= rounds(a, dual, 64, 64, 55))
             launch_split<128, 128, 4, 2, OUT>(a, aligned, stream);
         else
             launch_split<64, 64, 4, 2, OUT>(a, aligned, stream);
-        return;
+    } else if (aligned) {
+        launch_ring_product<E, OUT>(a, stream);
     } else {
-        if constexpr (OUT != Out::kStore) {
-            if (!aligned) {
-                if (tiles(256, 256) >= 192)
-                    launch_tile<E, 256, 256, 2, 4, 1, OUT>(a, stream);
-                else if (tiles(128, 128) >= 192)
-                    launch_tile<E, 128, 128, 2, 2, 1, OUT>(a, stream);
-                else
-                    launch_tile<E, 64, 64, 2, 2, 3, OUT>(a, stream);
-                return;
-            }
-        }
-        if (tiles(256, 256) >= 192)
-            launch_ring<E, 256, 256, 2, 4, 4, OUT>(a, stream);
-        else if (tiles(128, 128) >= 192)
-            launch_ring<E, 128, 128, 2, 2, 4, OUT>(a, stream);
+        const int64_t cost[3] = {rounds(a, dual, 256, 256, 130), rounds(a, dual, 128, 128, 50),
+                                 rounds(a, dual, 64, 64, 25)};
+        if (cost[0] <= cost[1] && cost[0] <= cost[2])
+            launch_tile<E, 256, 256, 2, 4, 1, OUT>(a, stream);
+        else if (cost[1] <= cost[2])
+            launch_tile<E, 128, 128, 2, 2, 1, OUT>(a, stream);
         else
-            launch_ring<E, 64, 64, 2, 2, 8, OUT>(a, stream);
+            launch_tile<E, 64, 64, 2, 2, 3, OUT>(a, stream);
     }
 }
 
@@ -132,8 +153,9 @@ void gated(const void *X, int64_t T_, int64_t ldx, const float *sx, const bsr_ga
 
 // --- gradients ----------------------------------------------------------------------------------
 // The two gradient products sum over the hidden width and over the tokens, along which their
-// operands are not contiguous.  dG and dU are written in both orders where they are made; X and the
-// weights are transposed.  Padding keeps every row 16-byte aligned and holds zeros.
+// operands are not contiguous.  bf16: the product kernel takes them as they are (column operands);
+// fp32: dG and dU are written in both orders where they are made, X and the weights are transposed.
+// Padding keeps every row 16-byte aligned and holds zeros.
 
 constexpr int kT = 64;   // tile of the transposing kernels
 template <class T> constexpr int kV = 16 / int(sizeof(T));      // elements of 16 bytes
@@ -192,16 +214,31 @@ __global__ __launch_bounds__(kThreads) void transpose_kernel(const T *__restrict
     tile.store(out, ldo, r0, c0, C, pad);
 }
 
-// D[t][f] = dH U act'(G), D[t][Fp + f] = dH act(G), the transpose Dt[f][t], Dt[F + f][t], and the
-// sums of their columns over the tile's tokens.  Memory bound: 16 bytes of D (4 or 8 hidden units of
-// a token) per thread and pass.
-template <class T, int ACT>
+// out[r][c] = in[r][c] for c < C, rows of `pad` elements (a multiple of 16 bytes) padded with zeros.
+template <class T>
+__global__ __launch_bounds__(kThreads) void copy_rows_kernel(const T *__restrict__ in, int64_t ldi,
+                                                             int64_t R, int64_t C, T *__restrict__ out,
+                                                             int64_t pad) {
+    const int64_t per = pad / kV<T>, n = R * per;
+    for (int64_t e = int64_t(blockIdx.x) * kThreads + threadIdx.x; e < n;
+         e += int64_t(gridDim.x) * kThreads) {
+        const int64_t r = e / per, c = e % per * kV<T>;
+        T v[kV<T>];
+        load_some(in + r * ldi + c, C - c, v);
+        __builtin_memcpy(out + r * pad + c, v, 16);
+    }
+}
+
+// D[t][f] = dH U act'(G), D[t][Fp + f] = dH act(G), zeros up to Fp, and the sums of their columns over
+// the tile's tokens; BOTH: also the transpose Dt[f][t], Dt[F + f][t].  Memory bound: 16 bytes of D (4
+// or 8 hidden units of a token) per thread and pass.
+template <class T, int ACT, bool BOTH>
 __global__ __launch_bounds__(kThreads) void gated_slope_kernel(
     const T *__restrict__ dH, int64_t lddh, const float *__restrict__ G,
     const float *__restrict__ U, int64_t ldp, int64_t T_, int64_t F, T *__restrict__ D, int64_t Fp,
     T *__restrict__ Dt, int64_t Tp, float *__restrict__ partial) {
     constexpr int V = kV<T>, per = kT / V, kRows = kThreads / per;
-    __shared__ TransposeTile<T> tg, tu;
+    __shared__ typename std::conditional<BOTH, TransposeTile<T>, char>::type tg, tu;
     __shared__ float sums[2][kRows][kT + 1];
     const int64_t t0 = int64_t(blockIdx.x) * kT, f0 = int64_t(blockIdx.y) * kT;
     const int y = threadIdx.x / per, x = threadIdx.x % per * V;
@@ -234,8 +271,10 @@ __global__ __launch_bounds__(kThreads) void gated_slope_kernel(
             dg[j] = from_float<T>(vg);
             du[j] = from_float<T>(vu);
         }
-        tg.put(i, x, dg);
-        tu.put(i, x, du);
+        if constexpr (BOTH) {
+            tg.put(i, x, dg);
+            tu.put(i, x, du);
+        }
         if (t < T_ && f < Fp) {
             __builtin_memcpy(D + t * 2 * Fp + f, dg, 16);
             __builtin_memcpy(D + t * 2 * Fp + Fp + f, du, 16);
@@ -247,8 +286,10 @@ __global__ __launch_bounds__(kThreads) void gated_slope_kernel(
         sums[1][y][x + j] = pu[j];
     }
     __syncthreads();
-    tg.store(Dt, Tp, t0, f0, F, Tp);
-    tu.store(Dt + F * Tp, Tp, t0, f0, F, Tp);
+    if constexpr (BOTH) {
+        tg.store(Dt, Tp, t0, f0, F, Tp);
+        tu.store(Dt + F * Tp, Tp, t0, f0, F, Tp);
+    }
     if (threadIdx.x < 2 * kT) {
         const int which = threadIdx.x / kT, c = threadIdx.x % kT;
         float s = 0.0f;
@@ -293,61 +334,101 @@ void transpose(const void *in, int64_t ldi, int64_t R, int64_t C, T *out, int64_
                        as_stream(stream), static_cast<const T *>(in), ldi, R, C, out, ldo, pad);
 }
 
+// A matrix as a column operand: itself where its rows are whole 16-byte chunks on 16-byte boundaries,
+// else copied to `space` with rows of Kp elements.
+struct ColumnOperand {
+    const char *p;
+    int64_t ld;      // bytes
+};
+ColumnOperand as_columns(const void *in, int64_t ldi, int64_t R, int64_t C, char *space, int64_t Kp,
+                         void *stream) {
+    if (C % 8 == 0 && rows_aligned(in, ldi * 2)) return {static_cast<const char *>(in), ldi * 2};
+    hipLaunchKernelGGL(copy_rows_kernel<bf16>, dim3(grid_for(R * (Kp / 8), kThreads, 4096)),
+                       dim3(kThreads), 0, as_stream(stream), static_cast<const bf16 *>(in), ldi, R, C,
+                       reinterpret_cast<bf16 *>(space), Kp);
+    return {space, Kp * 2};
+}
+
 template <class T, class TG>
 void backward(const void *dH, int64_t lddh, const void *X, int64_t T_, int64_t ldx,
               const bsr_gated_t &W, const float *G, const float *U, int64_t ldp, void *dX,
               int64_t lddx, void *dWg, void *dWu, int64_t lddw, void *dbg, void *dbu, void *ws,
               void *stream) {
+    constexpr bool columns = sizeof(T) == 2;
     const int64_t K = W.K, F = W.F;
     const GatedWorkspace l = gated_workspace_layout(T_, K, F, raw_enum(W.dtype));
     char *base = static_cast<char *>(ws);
     T *D = reinterpret_cast<T *>(base + l.grad_offset);
     T *Dt = reinterpret_cast<T *>(base + l.gradt_offset);
-    T *Xt = reinterpret_cast<T *>(base + l.xt_offset);
-    T *Wt = reinterpret_cast<T *>(base + l.wt_offset);
+    char *x_space = base + l.x_offset, *w_space = base + l.w_offset;
     float *partial = reinterpret_cast<float *>(base + l.partial_offset);
     if (T_ > 0)
         with_act(W.act, [&](auto act) {
-            hipLaunchKernelGGL((gated_slope_kernel<T, decltype(act)::value>),
-                               dim3(cover(l.Tp, kT), cover(l.Fp, kT)), dim3(kThreads), 0,
-                               as_stream(stream), static_cast<const T *>(dH), lddh, G, U, ldp, T_, F,
-                               D, l.Fp, Dt, l.Tp, partial);
+            hipLaunchKernelGGL((gated_slope_kernel<T, decltype(act)::value, !columns>),
+                               dim3(cover(columns ? T_ : l.Tp, kT), cover(l.Fp, kT)), dim3(kThreads),
+                               0, as_stream(stream), static_cast<const T *>(dH), lddh, G, U, ldp, T_,
+                               F, D, l.Fp, Dt, l.Tp, partial);
         });
     if (dbg || dbu)
         hipLaunchKernelGGL(bias_grad_kernel<TG>, dim3(cover(2 * F, kThreads)), dim3(kThreads), 0,
                            as_stream(stream), partial, int64_t(cover(T_, kT)), F,
                            static_cast<TG *>(dbg), static_cast<TG *>(dbu));
-    if (dX && T_ > 0) {
-        transpose<T>(W.Wg, W.ldg, F, K, Wt, 2 * l.Fp, l.Fp, stream);
-        transpose<T>(W.Wu, W.ldu, F, K, Wt + l.Fp, 2 * l.Fp, l.Fp, stream);
-        ProductArgs a{};
-        a.A = reinterpret_cast<const char *>(D);
-        a.B0 = reinterpret_cast<const char *>(Wt);
-        a.lda = a.ldb0 = 2 * l.Fp * kSize<T>;
+    ProductArgs a{};
+    a.A = reinterpret_cast<const char *>(D);
+    a.lda = 2 * l.Fp * kSize<T>;
+    if (dX && T_ > 0) {           // D (T x 2 Fp) times (Wg; Wu)
         a.Kb = int(2 * l.Fp * kSize<T>);
-        a.M = T_;
+        a.M = a.split = a.limit = T_;
         a.N = K;
         a.out = dX;
         a.ldo = lddx;
-        a.split = T_;
         a.out_bf16 = std::is_same<T, bf16>::value;
-        launch_product<T, Out::kStore>(a, stream);
+        if constexpr (columns) {
+            const ColumnOperand g = as_columns(W.Wg, W.ldg, F, K, w_space, l.Kp, stream);
+            const ColumnOperand u = as_columns(W.Wu, W.ldu, F, K, w_space + F * l.Kp * 2, l.Kp, stream);
+            a.B0 = g.p;
+            a.B1 = u.p;
+            a.ldb0 = g.ld;
+            a.ldb1 = u.ld;
+            a.rows_k = int(F);
+            a.half = int(l.Fp / 32);
+            launch_ring_product<T, Out::kStore, false, true>(a, stream);
+        } else {
+            T *Wt = reinterpret_cast<T *>(w_space);
+            transpose<T>(W.Wg, W.ldg, F, K, Wt, 2 * l.Fp, l.Fp, stream);
+            transpose<T>(W.Wu, W.ldu, F, K, Wt + l.Fp, 2 * l.Fp, l.Fp, stream);
+            a.B0 = w_space;
+            a.ldb0 = a.lda;
+            launch_product<T, Out::kStore>(a, stream);
+        }
     }
-    if (dWg && T_ > 0) {
-        transpose<T>(X, ldx, T_, K, Xt, l.Tp, l.Tp, stream);
-        ProductArgs a{};
-        a.A = reinterpret_cast<const char *>(Dt);
-        a.B0 = reinterpret_cast<const char *>(Xt);
-        a.lda = a.ldb0 = l.Tp * kSize<T>;
-        a.Kb = int(l.Tp * kSize<T>);
-        a.M = 2 * F;
+    if (dWg && T_ > 0) {          // D^T (2 F x T) times X
         a.N = K;
         a.out = dWg;
         a.out2 = dWu;
         a.ldo = lddw;
-        a.split = F;
+        a.limit = F;
         a.out_bf16 = std::is_same<TG, bf16>::value;
-        launch_product<T, Out::kStore>(a, stream);
+        if constexpr (columns) {
+            const ColumnOperand x = as_columns(X, ldx, T_, K, x_space, l.Kp, stream);
+            a.B0 = a.B1 = x.p;
+            a.ldb0 = a.ldb1 = x.ld;
+            a.rows_k = int(T_);
+            a.half = cover(T_, 32);
+            a.Kb = a.half * 64;
+            a.M = 2 * l.Fp;
+            a.split = l.Fp;
+            launch_ring_product<T, Out::kStore, true, true>(a, stream);
+        } else {
+            transpose<T>(X, ldx, T_, K, reinterpret_cast<T *>(x_space), l.Tp, l.Tp, stream);
+            a.A = reinterpret_cast<const char *>(Dt);
+            a.B0 = x_space;
+            a.lda = a.ldb0 = l.Tp * kSize<T>;
+            a.Kb = int(l.Tp * kSize<T>);
+            a.M = 2 * F;
+            a.split = F;
+            launch_product<T, Out::kStore>(a, stream);
+        }
     } else if (dWg) {
         for (void *p : {dWg, dWu})
             hipLaunchKernelGGL(zero_rows_kernel<TG>, dim3(grid_for(F * K, kThreads, 4096)),

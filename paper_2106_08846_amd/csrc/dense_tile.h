@@ -57,13 +57,15 @@ struct ProductArgs {
     int64_t lda, ldb0, ldb1;      // row pitches in bytes
     int64_t M, N;                 // tokens; channels (of each matrix)
     int Kb;                       // bytes of a row that are summed over
+    int rows_k, half;             // column operands: rows of each matrix, and the step from which on
+                                  // the second one (B1) is taken
     int tiles_m, tiles_n;
     // epilogue
     const float *sx, *s0, *s1;    // scales of tokens and channels (int8)
     const float *b0, *b1;         // biases or NULL
-    void *out, *out2;             // kStore: rows from `split` on go to out2
+    void *out, *out2;             // kStore: rows from `split` on go to out2; `limit` of each exist
     float *G, *U;                 // kGated: pre-activations or NULL
-    int64_t ldo, ldp, split;
+    int64_t ldo, ldp, split, limit;
     int out_bf16, act;
 };
 
@@ -126,10 +128,8 @@ __device__ __forceinline__ void finish4(const ProductArgs &a, int64_t m, int64_t
         y = __builtin_bit_cast(f32x4, q);
     }
     if constexpr (OUT == Out::kStore) {
-        if (m < a.split)
-            store4(a.out, m * a.ldo + n, a.out_bf16, x, cnt);
-        else
-            store4(a.out2, (m - a.split) * a.ldo + n, a.out_bf16, x, cnt);
+        const int64_t row = m < a.split ? m : m - a.split;
+        if (row < a.limit) store4(m < a.split ? a.out : a.out2, row * a.ldo + n, a.out_bf16, x, cnt);
         return;
     }
     if constexpr (sizeof(E) == 1) {

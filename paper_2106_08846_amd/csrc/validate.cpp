@@ -388,13 +388,16 @@ GatedWorkspace gated_workspace_layout(int64_t T, int64_t K, int64_t F, int32_t d
     GatedWorkspace w{};
     const int64_t e = dtype_size(dtype), per = 16 / e;
     const int64_t blocks = (T + kGatedRowsPerPartial - 1) / kGatedRowsPerPartial;
-    w.Fp = (F + per - 1) / per * per;
-    w.Tp = (T + per - 1) / per * per;
+    const bool bf16 = dtype == BSR_BF16;
+    auto up = [](int64_t n, int64_t m) { return (n + m - 1) / m * m; };
+    w.Fp = up(F, bf16 ? 32 : per);
+    w.Kp = up(K, per);
+    w.Tp = up(T, per);
     w.grad_offset = 0;
     w.gradt_offset = align256(size_t(T * 2 * w.Fp * e));
-    w.xt_offset = align256(w.gradt_offset + size_t(2 * F * w.Tp * e));
-    w.wt_offset = align256(w.xt_offset + size_t(K * w.Tp * e));
-    w.partial_offset = align256(w.wt_offset + size_t(K * 2 * w.Fp * e));
+    w.x_offset = align256(w.gradt_offset + (bf16 ? 0 : size_t(2 * F * w.Tp * e)));
+    w.w_offset = align256(w.x_offset + size_t(bf16 ? T * w.Kp * e : K * w.Tp * e));
+    w.partial_offset = align256(w.w_offset + size_t(bf16 ? 2 * F * w.Kp * e : K * 2 * w.Fp * e));
     w.total = align256(w.partial_offset + size_t(blocks * 2 * F * 4));
     if (w.total == 0) w.total = 256;
     return w;
@@ -414,7 +417,7 @@ bsr_status check_gated_backward(const void *dH, int64_t lddh, const void *X, int
     if (lddh < F || ldp < F || (dX && lddx < K) || (dw && lddw < K)) return BSR_ERR_SHAPE;
     if (T > kGatedMaxBackwardTokens || lddh > kDenseMaxWidth || ldp > kDenseMaxWidth ||
         (dX && lddx > kDenseMaxWidth) || (dw && lddw > kDenseMaxWidth) ||
-        2 * F > kDenseMaxWidth || F * K > kDenseMaxOut / 2 || T * K > kDenseMaxOut)
+        2 * F > kDenseMaxWidth - 64 || F * K > kDenseMaxOut / 2 || T * K > kDenseMaxOut)
         return BSR_ERR_UNSUPPORTED;
     if (dw && (!dWg || !dWu)) return BSR_ERR_NULL;
     if (T > 0 && (!dH || !X || !G || !U)) return BSR_ERR_NULL;
@@ -439,7 +442,7 @@ extern "C" {
 size_t bsr_gated_workspace_bytes(int64_t T, int64_t K, int64_t F, bsr_dtype dtype) {
     const int32_t dt = bsr::raw_enum(dtype);
     if (T < 0 || K < 1 || F < 1 || T > bsr::kGatedMaxBackwardTokens ||
-        K > bsr::kDenseMaxWidth || 2 * F > bsr::kDenseMaxWidth ||
+        K > bsr::kDenseMaxWidth || 2 * F > bsr::kDenseMaxWidth - 64 ||
         (dt != BSR_F32 && dt != BSR_BF16))
         return 0;
     return bsr::gated_workspace_layout(T, K, F, dt).total;
