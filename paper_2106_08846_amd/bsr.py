@@ -841,15 +841,18 @@ def _vector_arg(t, name: str, n: int, dtype=torch.float32):
 
 def _one_device(*tensors) -> None:
     """Every given tensor is on the current GPU, whose stream the work is enqueued on."""
-    now = -1
+    now = None
     for t in tensors:
         if t is None:
             continue
+        dev = t.get_device()
+        if dev == now:
+            continue
         if not t.is_cuda:
             raise TypeError("every tensor must be a CUDA (HIP) tensor")
-        if now < 0:
+        if now is None:
             now = _cur_device() if _cur_device is not None else torch.cuda.current_device()
-        if t.get_device() != now:
+        if dev != now:
             raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{now}: keep a "
                              "call's tensors on one device and make it current (torch.cuda.device)")
 
@@ -880,12 +883,14 @@ def bsr_quantize_rows(X: torch.Tensor, Q: torch.Tensor | None = None,
     if Q is None:
         Q = torch.empty(T, K, dtype=torch.int8, device=X.device)
         made.append(Q)
+        ldq = K
+    else:
+        ldq = _matrix_arg(Q, "Q", T, K, _I8_DTYPES)
     if scale is None:
         scale = torch.empty(T, dtype=_F32, device=X.device)
         made.append(scale)
     else:
         _vector_arg(scale, "scale", T)
-    ldq = _matrix_arg(Q, "Q", T, K, _I8_DTYPES)
     _one_device(X, Q, scale)
     _check(_lib().bsr_quantize_rows(_ptr(X), _DTYPE_CODE[X.dtype], T, K, ldx, _ptr(Q), ldq,
                                     _ptr(scale), _on_stream(stream, *made)), "bsr_quantize_rows")
@@ -908,8 +913,12 @@ def bsr_matmul_i8(Xq: torch.Tensor, sx: torch.Tensor, Wq: torch.Tensor, sw: torc
         raise ValueError("give both scales")
     made = None
     if Y is None:
+        if out_dtype not in _DATA_DTYPES:
+            raise TypeError("out_dtype must be float32 or bfloat16")
         Y = made = torch.empty(T, N, dtype=out_dtype, device=Xq.device)
-    ldy = _matrix_arg(Y, "Y", T, N, _DATA_DTYPES)
+        ldy = N
+    else:
+        ldy = _matrix_arg(Y, "Y", T, N, _DATA_DTYPES)
     _one_device(Xq, sx, Wq, sw, bias, Y)
     _check(_lib().bsr_matmul_i8(_ptr(Xq), T, K, ldx, _ptr(sx), _ptr(Wq), N, ldw, _ptr(sw),
                                 _ptr(bias), _ptr(Y), _DTYPE_CODE[Y.dtype], ldy,
@@ -917,19 +926,20 @@ def bsr_matmul_i8(Xq: torch.Tensor, sx: torch.Tensor, Wq: torch.Tensor, sw: torc
     return Y
 
 
-def _gated_block(X, Wg, Wu, sg, su, bg, bu, act: str, dtypes) -> bsr_gated_t:
-    """Check a gated block's weights against X and describe them for the C side (the caller checks
-    the devices)."""
+def _gated_block(X, Wg, Wu, sg, su, bg, bu, act: str, dtypes) -> tuple[int, bsr_gated_t]:
+    """Check a gated block's weights against X (the caller checks the devices); returns X's row pitch
+    and the block's description for the C side."""
     if act not in ACTS:
         raise ValueError(f"act must be one of {', '.join(ACTS)}")
-    _matrix_arg(X, "X", None, None, dtypes)
+    ldx = _matrix_arg(X, "X", None, None, dtypes)
     K = X.shape[1]
     ldg = _matrix_arg(Wg, "Wg", None, K, (X.dtype,))
     F = Wg.shape[0]
     ldu = _matrix_arg(Wu, "Wu", F, K, (X.dtype,))
     for t, name in ((sg, "sg"), (su, "su"), (bg, "bg"), (bu, "bu")):
-        _vector_arg(t, name, F)
-    return bsr_gated_t(K, F, _ptr(Wg), _ptr(Wu), ldg, ldu, _ptr(sg), _ptr(su), _ptr(bg), _ptr(bu),
+        if t is not None:
+            _vector_arg(t, name, F)
+    return ldx, bsr_gated_t(K, F, _ptr(Wg), _ptr(Wu), ldg, ldu, _ptr(sg), _ptr(su), _ptr(bg), _ptr(bu),
                        _DTYPE_CODE[X.dtype], ACTS[act])
 
 
@@ -941,7 +951,7 @@ def bsr_gated(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor,
     X [T, K], Wg and Wu [F, K], all float32 or all bfloat16, biases fp32; H [T, F] of X's type.
     act: "silu", "gelu", "gelu_tanh" or "relu".  With save (or G and U given) returns (H, G, U), G and
     U the fp32 pre-activations that bsr_gated_backward reads; otherwise H."""
-    block = _gated_block(X, Wg, Wu, None, None, bg, bu, act, _DATA_DTYPES)
+    ldx, block = _gated_block(X, Wg, Wu, None, None, bg, bu, act, _DATA_DTYPES)
     T, F = X.shape[0], block.F
     if (G is None) != (U is None):
         raise ValueError("give both G and U, or neither")
@@ -949,18 +959,20 @@ def bsr_gated(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor,
     if H is None:
         H = torch.empty(T, F, dtype=X.dtype, device=X.device)
         made.append(H)
+        ldh = F
+    else:
+        ldh = _matrix_arg(H, "H", T, F, (X.dtype,))
     ldp = 0
     if save and G is None:
         G = torch.empty(T, F, dtype=_F32, device=X.device)
         U = torch.empty(T, F, dtype=_F32, device=X.device)
         made += [G, U]
-    ldh = _matrix_arg(H, "H", T, F, (X.dtype,))
     if G is not None:
         ldp = _matrix_arg(G, "G", T, F, _F32_DTYPES)
         if _matrix_arg(U, "U", T, F, _F32_DTYPES) != ldp:
             raise ValueError("G and U must have the same row pitch")
     _one_device(X, Wg, Wu, bg, bu, H, G, U)
-    _check(_lib().bsr_gated(_ptr(X), T, _pitch(X, "X"), ctypes.byref(block), _ptr(H), ldh, _ptr(G),
+    _check(_lib().bsr_gated(_ptr(X), T, ldx, ctypes.byref(block), _ptr(H), ldh, _ptr(G),
                             _ptr(U), ldp, _on_stream(stream, *made)), "bsr_gated")
     return H if G is None else (H, G, U)
 
@@ -984,7 +996,7 @@ def bsr_gated_backward(dH: torch.Tensor, X: torch.Tensor, Wg: torch.Tensor, Wu: 
     float32 suits bsr_iht_update and fp32 master weights), allocated here unless given.  `workspace`
     is a uint8 device tensor of bsr_gated_workspace_bytes, allocated here when None; calls that may
     overlap in time need one each."""
-    block = _gated_block(X, Wg, Wu, None, None, None, None, act, _DATA_DTYPES)
+    ldx, block = _gated_block(X, Wg, Wu, None, None, None, None, act, _DATA_DTYPES)
     T, K, F = X.shape[0], block.K, block.F
     if any(n not in ("X", "W") for n in need):
         raise ValueError('need may name "X" and "W"')
@@ -1029,7 +1041,7 @@ def bsr_gated_backward(dH: torch.Tensor, X: torch.Tensor, Wg: torch.Tensor, Wu: 
             or workspace.dim() != 1 or not workspace.is_contiguous()):
         raise ValueError("workspace must be a contiguous uint8 tensor")
     _one_device(dH, X, Wg, Wu, G, U, dX, dWg, dWu, dbg, dbu, workspace)
-    _check(_lib().bsr_gated_backward(_ptr(dH), lddh, _ptr(X), T, _pitch(X, "X"),
+    _check(_lib().bsr_gated_backward(_ptr(dH), lddh, _ptr(X), T, ldx,
                                      ctypes.byref(block), _ptr(G), _ptr(U), ldp, _ptr(dX), lddx,
                                      _ptr(dWg), _ptr(dWu), lddw, _ptr(dbg), _ptr(dbu),
                                      _DTYPE_CODE[grad_dtype], _ptr(workspace), workspace.numel(),
@@ -1046,15 +1058,19 @@ def bsr_gated_i8(Xq: torch.Tensor, sx: torch.Tensor, Wgq: torch.Tensor, sg: torc
     int8 [F, K] with sg and su fp32 [F]; H float32 or bfloat16 (out_dtype, when H is None)."""
     if sg is None or su is None or sx is None:
         raise ValueError("give every scale")
-    block = _gated_block(Xq, Wgq, Wuq, sg, su, bg, bu, act, _I8_DTYPES)
+    ldx, block = _gated_block(Xq, Wgq, Wuq, sg, su, bg, bu, act, _I8_DTYPES)
     T, F = Xq.shape[0], block.F
     _vector_arg(sx, "sx", T)
     made = None
     if H is None:
+        if out_dtype not in _DATA_DTYPES:
+            raise TypeError("out_dtype must be float32 or bfloat16")
         H = made = torch.empty(T, F, dtype=out_dtype, device=Xq.device)
-    ldh = _matrix_arg(H, "H", T, F, _DATA_DTYPES)
+        ldh = F
+    else:
+        ldh = _matrix_arg(H, "H", T, F, _DATA_DTYPES)
     _one_device(Xq, sx, Wgq, sg, Wuq, su, bg, bu, H)
-    _check(_lib().bsr_gated_i8(_ptr(Xq), T, _pitch(Xq, "Xq"), _ptr(sx), ctypes.byref(block),
+    _check(_lib().bsr_gated_i8(_ptr(Xq), T, ldx, _ptr(sx), ctypes.byref(block),
                                _ptr(H), _DTYPE_CODE[H.dtype], ldh, _on_stream(stream, made)),
            "bsr_gated_i8")
     return H

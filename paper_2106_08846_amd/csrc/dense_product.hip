@@ -61,16 +61,18 @@ int64_t rounds(const ProductArgs &a, bool dual, int bm, int bn, int cost) {
     return (tiles + cus - 1) / cus * cost;
 }
 
-// The tile by the rounds it takes: the costs are microseconds of one round of each at K = 4096 in bf16
-// (MI355X).  At 4096 x 4096 x 4096 256 x 256 tiles take 110 us, 128 x 128 ones 154 and 64 x 64 ones
-// 259; at 2048^3 51, 24 and 33; at 128 x 8192 x 4096 84, 33 and 20; at 6144 x 2048 x 16384, whose 192
-// tiles of 256 x 256 leave a quarter of the CUs idle, 438 against 368 in 192 x 256.
+// The tile by the rounds it takes.  The costs are those of a round of each tile, measured (MI355X) in
+// bf16 and int8 over grids of 1 to 32 rounds, in hundredths of a round of 256 x 256, which takes 110 us
+// at K = 4096 in bf16 and 61 in int8.  So bf16 4096 x 4096 x 4096 takes 110 us in 256 x 256 tiles, 160
+// in 128 x 128 and 259 in 64 x 64; 2048^3 51, 24 and 33; 128 x 8192 x 4096 84, 35 and 20; and
+// 6144 x 2048 x 16384, whose 192 tiles of 256 x 256 leave a quarter of the CUs idle, 438 against 368
+// in 192 x 256; int8 2048 x 20480 x 4096 184 in 256 x 256 (2.5 rounds) and 196 in 192 x 256 (3.4).
 template <class E, Out OUT, bool COLS_A = false, bool COLS_B = false>
 void launch_ring_product(const ProductArgs &a, void *stream) {
     constexpr bool dual = OUT == Out::kGated;
-    const int64_t cost[5] = {rounds(a, dual, 256, 256, 110), rounds(a, dual, 192, 256, 85),
-                             rounds(a, dual, 128, 256, 65), rounds(a, dual, 128, 128, 42),
-                             rounds(a, dual, 64, 64, 18)};
+    const int64_t cost[5] = {rounds(a, dual, 256, 256, 100), rounds(a, dual, 192, 256, 78),
+                             rounds(a, dual, 128, 256, 62), rounds(a, dual, 128, 128, 38),
+                             rounds(a, dual, 64, 64, 16)};
     int best = 0;
     for (int i = 1; i < 5; ++i)
         if (cost[i] < cost[best]) best = i;
@@ -88,9 +90,10 @@ template <class E, Out OUT> void launch_product(const ProductArgs &a, void *stre
     const bool aligned = a.Kb % 16 == 0 && rows_aligned(a.A, a.lda) && rows_aligned(a.B0, a.ldb0) &&
                          (!dual || rows_aligned(a.B1, a.ldb1));
     if constexpr (OUT != Out::kStore) {
+        // Beyond 32 tokens the tiles are as fast or faster: 64 tokens through 11008 x 4096 int8 take 31
+        // us here and 20 in tiles, through 4096 x 4096 14 and 15.
         if (a.M <= 16) return launch_rows<E, 1, OUT>(a, aligned, stream);
         if (a.M <= 32) return launch_rows<E, 2, OUT>(a, aligned, stream);
-        if (a.M <= 64) return launch_rows<E, 4, OUT>(a, aligned, stream);
     }
     if constexpr (sizeof(E) == 4) {
         // Costs of a round at K = 4096, as above: 1000 x 768 x 3064 takes 102 us in 128 x 128 tiles and
@@ -102,14 +105,20 @@ template <class E, Out OUT> void launch_product(const ProductArgs &a, void *stre
     } else if (aligned) {
         launch_ring_product<E, OUT>(a, stream);
     } else {
-        const int64_t cost[3] = {rounds(a, dual, 256, 256, 130), rounds(a, dual, 128, 128, 50),
-                                 rounds(a, dual, 64, 64, 25)};
-        if (cost[0] <= cost[1] && cost[0] <= cost[2])
-            launch_tile<E, 256, 256, 2, 4, 1, OUT>(a, stream);
-        else if (cost[1] <= cost[2])
-            launch_tile<E, 128, 128, 2, 2, 1, OUT>(a, stream);
-        else
-            launch_tile<E, 64, 64, 2, 2, 3, OUT>(a, stream);
+        // As launch_ring_product: bf16 4096 x 4096 x 4095 takes 146 us in 256 x 256 tiles, 183 in
+        // 128 x 256, 194 in 128 x 128 and 368 in 64 x 64; 2048 x 2048 x 4095 136, 89, 68 and 100;
+        // int8 333 x 2304 x 770 28, 18, 12 and 9.
+        const int64_t cost[4] = {rounds(a, dual, 256, 256, 100), rounds(a, dual, 128, 256, 63),
+                                 rounds(a, dual, 128, 128, 38), rounds(a, dual, 64, 64, 17)};
+        int best = 0;
+        for (int i = 1; i < 4; ++i)
+            if (cost[i] < cost[best]) best = i;
+        switch (best) {
+            case 0: return launch_tile<E, 256, 256, 2, 4, 1, OUT>(a, stream);
+            case 1: return launch_tile<E, 128, 256, 2, 4, 1, OUT>(a, stream);
+            case 2: return launch_tile<E, 128, 128, 2, 4, 2, OUT>(a, stream);
+            default: return launch_tile<E, 64, 64, 2, 2, 3, OUT>(a, stream);
+        }
     }
 }
 

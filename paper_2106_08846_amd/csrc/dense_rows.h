@@ -1,4 +1,4 @@
-// The dense products of few tokens (at most 64): the weights are read once, straight into the
+// The dense products of few tokens (at most 32): the weights are read once, straight into the
 // operand registers of the matrix instructions, and that read is the whole cost.
 //
 // A workgroup makes 16 channels (gated: of each matrix) for every token.  Its eight waves split the
@@ -6,7 +6,7 @@
 // all at once, and keeps its own sums; they are added over the waves, in order, through LDS.  What
 // bounds a single token is latency: 16 rows of 4096 bytes are one block per wave, so that everything
 // a workgroup needs is in flight together.  The tokens come from the L2 (every workgroup reads all
-// of them), which is why the tile kernel takes over beyond 64.
+// of them), which is why the tile kernels take over beyond 32.
 #pragma once
 
 #include "dense_tile.h"
@@ -20,7 +20,7 @@ template <class E, int NT, bool ALIGNED, Out OUT> struct RowsKernel {
     static constexpr int kChannels = 16;
     static constexpr int NW = kDual ? 2 : 1;
     // Chunks of 64 bytes per row that a wave loads at once: 16 bytes a lane and operand each.
-    static constexpr int kHeld = NT == 4 ? 2 : NT == 2 ? 4 : kDual ? 4 : 8;
+    static constexpr int kHeld = NT == 2 || kDual ? 4 : 8;
     static constexpr int kBlock = 64 * kHeld;
     using M_ = Mma<E>;
     using Acc = typename M_::Acc;
@@ -35,7 +35,8 @@ template <class E, int NT, bool ALIGNED, Out OUT> struct RowsKernel {
                               {kDual ? a.B1 + n0 * a.ldb1 : nullptr, a.ldb1, rows}};
         const int fr = lane & 15, fc = lane >> 4;
         Acc acc[NW][NT] = {};
-        RowChunks<E, ALIGNED> cw[NW], cx[NT];
+        constexpr Load kLoad = ALIGNED ? Load::kAligned : sizeof(E) == 4 ? Load::kBytes : Load::kShifted;
+        RowChunks<E, kLoad> cw[NW], cx[NT];
 #pragma unroll
         for (int j = 0; j < NW; ++j) cw[j].set(sw[j], fr, fc * kChunk, a.Kb);
 #pragma unroll

@@ -77,7 +77,7 @@ template <int BM, int BN, int WM, int WN, bool ALIGNED, Out OUT> struct SplitKer
             f32x8 v[L];
         };
         Held held[3];                        // step k in held[k % 3], its place in LDS slot k % 3
-        RowChunks<float, ALIGNED> chunks[L];
+        RowChunks<float, ALIGNED ? Load::kAligned : Load::kBytes> chunks[L];
 #pragma unroll
         for (int i = 0; i < L; ++i) {
             const int first = i * kRowsPerPass + wave * 16, row = i * kRowsPerPass + r0;
