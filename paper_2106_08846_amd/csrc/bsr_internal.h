@@ -104,8 +104,21 @@ struct GatedWorkspace {
     size_t x_offset;         // bf16: [T][Kp], a copy of an unaligned X; fp32: [K][Tp], X's transpose
     size_t w_offset;         // bf16: [2][F][Kp], copies; fp32: [K][2 Fp], the weights' transposes
     size_t partial_offset;   // fp32 [row blocks][2 F]: partial bias gradients
+    int x_slices, w_slices;  // of dX's and of the weight gradients' product
+    size_t slice_offset;     // fp32: the slices' sums, of one product at a time
     size_t total;
 };
+// Slices that a gradient product of M x N outputs and `steps` steps of its contraction (32 of it each)
+// is cut into where 64 x 64 tiles leave CUs idle (of 256; bf16: where they do not give two workgroups
+// to each, fp32 gains nothing from the second); a slice keeps at least 64 steps in bf16 (10 us) and 16
+// in fp32 (8 us).  Each writes fp32 sums, which are added in order.
+inline int gated_slices(int64_t M, int64_t N, int64_t steps, bool bf16) {
+    const int64_t tiles = ((M + 63) / 64) * ((N + 63) / 64);
+    int64_t n = (bf16 ? 512 : 256) / (tiles > 0 ? tiles : 1);
+    if (n > steps / (bf16 ? 64 : 16)) n = steps / (bf16 ? 64 : 16);
+    if (n > 16) n = 16;
+    return n > 1 ? int(n) : 1;
+}
 constexpr int kGatedRowsPerPartial = 64;
 GatedWorkspace gated_workspace_layout(int64_t T, int64_t K, int64_t F, int32_t dtype);
 

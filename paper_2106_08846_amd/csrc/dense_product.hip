@@ -16,11 +16,11 @@ template <class T> constexpr int64_t kSize = sizeof(T);
 
 // Launch `kernel` over the tiles of K.
 template <class K, int BM>
-void launch_tiles(void (*kernel)(ProductArgs), ProductArgs a, void *stream) {
+void launch_tiles(void (*kernel)(ProductArgs), ProductArgs a, void *stream, unsigned slices = 1) {
     a.tiles_m = int((a.M + BM - 1) / BM);
     a.tiles_n = int((a.N + K::kTileN - 1) / K::kTileN);
-    hipLaunchKernelGGL(kernel, dim3(unsigned(a.tiles_m) * unsigned(a.tiles_n)), dim3(K::kThreads), 0,
-                       as_stream(stream), a);
+    hipLaunchKernelGGL(kernel, dim3(unsigned(a.tiles_m) * unsigned(a.tiles_n), slices),
+                       dim3(K::kThreads), 0, as_stream(stream), a);
 }
 template <class E, int BM, int BN, int WM, int WN, int RING, Out OUT, bool COLS_A, bool COLS_B>
 void launch_ring(const ProductArgs &a, void *stream) {
@@ -46,8 +46,9 @@ void launch_rows(const ProductArgs &a, bool aligned, void *stream) {
     using K = RowsKernel<E, NT, true, OUT>;
     const auto kernel = aligned ? dense_rows_kernel<E, NT, true, OUT>
                                 : dense_rows_kernel<E, NT, false, OUT>;
-    hipLaunchKernelGGL(kernel, dim3(unsigned((a.N + K::kChannels - 1) / K::kChannels)),
-                       dim3(64 * K::kWaves), 0, as_stream(stream), a);
+    const unsigned groups_n = unsigned((a.N + K::kChannels - 1) / K::kChannels);
+    const unsigned groups_m = unsigned((a.M + 16 * NT - 1) / (16 * NT));
+    hipLaunchKernelGGL(kernel, dim3(groups_n, groups_m), dim3(64 * K::kWaves), 0, as_stream(stream), a);
 }
 
 bool rows_aligned(const void *p, int64_t ld) {
@@ -90,10 +91,12 @@ template <class E, Out OUT> void launch_product(const ProductArgs &a, void *stre
     const bool aligned = a.Kb % 16 == 0 && rows_aligned(a.A, a.lda) && rows_aligned(a.B0, a.ldb0) &&
                          (!dual || rows_aligned(a.B1, a.ldb1));
     if constexpr (OUT != Out::kStore) {
-        // Beyond 32 tokens the tiles are as fast or faster: 64 tokens through 11008 x 4096 int8 take 31
-        // us here and 20 in tiles, through 4096 x 4096 14 and 15.
+        // Beyond one group of 32 only where its workgroups, each with a whole contraction to itself, fit
+        // the chip in one round: bf16 64 x 1024 x 4096 takes 12 us here and 19 in tiles, 128 x 1024 x
+        // 8192 23 and 34, 64 x 4096 x 4096 (two rounds) 24 and 19.
         if (a.M <= 16) return launch_rows<E, 1, OUT>(a, aligned, stream);
-        if (a.M <= 32) return launch_rows<E, 2, OUT>(a, aligned, stream);
+        if (a.M <= 32 || ((a.M + 31) / 32) * ((a.N + 15) / 16) <= device_cu_count())
+            return launch_rows<E, 2, OUT>(a, aligned, stream);
     }
     if constexpr (sizeof(E) == 4) {
         // Costs of a round at K = 4096, as above: 1000 x 768 x 3064 takes 102 us in 128 x 128 tiles and
@@ -205,11 +208,18 @@ template <class T> __device__ __forceinline__ void load_some(const T *p, int64_t
 }
 
 // out[c][r] = in[r][c] for r < R, c < C; out's rows are padded with zeros to `pad` columns.
+// blockIdx.z counts the matrices.
+template <class T> struct Transposes {
+    const T *in[2];
+    int64_t ldi[2];
+    T *out[2];
+};
 template <class T>
-__global__ __launch_bounds__(kThreads) void transpose_kernel(const T *__restrict__ in, int64_t ldi,
-                                                             int64_t R, int64_t C, T *__restrict__ out,
+__global__ __launch_bounds__(kThreads) void transpose_kernel(Transposes<T> of, int64_t R, int64_t C,
                                                              int64_t ldo, int64_t pad) {
     __shared__ TransposeTile<T> tile;
+    const T *in = blockIdx.z == 0 ? of.in[0] : of.in[1];
+    const int64_t ldi = blockIdx.z == 0 ? of.ldi[0] : of.ldi[1];
     const int64_t r0 = int64_t(blockIdx.x) * kT, c0 = int64_t(blockIdx.y) * kT;
     constexpr int per = kT / kV<T>;
 #pragma unroll
@@ -220,7 +230,7 @@ __global__ __launch_bounds__(kThreads) void transpose_kernel(const T *__restrict
         tile.put(r, c, v);
     }
     __syncthreads();
-    tile.store(out, ldo, r0, c0, C, pad);
+    tile.store(blockIdx.z == 0 ? of.out[0] : of.out[1], ldo, r0, c0, C, pad);
 }
 
 // out[r][c] = in[r][c] for c < C, rows of `pad` elements (a multiple of 16 bytes) padded with zeros.
@@ -337,10 +347,10 @@ __global__ __launch_bounds__(kThreads) void zero_rows_kernel(T *__restrict__ p, 
 unsigned cover(int64_t n, int64_t tile) { return unsigned((n + tile - 1) / tile); }
 
 template <class T>
-void transpose(const void *in, int64_t ldi, int64_t R, int64_t C, T *out, int64_t ldo, int64_t pad,
-               void *stream) {
-    hipLaunchKernelGGL(transpose_kernel<T>, dim3(cover(pad, kT), cover(C, kT)), dim3(kThreads), 0,
-                       as_stream(stream), static_cast<const T *>(in), ldi, R, C, out, ldo, pad);
+void transpose(const Transposes<T> &of, unsigned matrices, int64_t R, int64_t C, int64_t ldo,
+               int64_t pad, void *stream) {
+    hipLaunchKernelGGL(transpose_kernel<T>, dim3(cover(pad, kT), cover(C, kT), matrices),
+                       dim3(kThreads), 0, as_stream(stream), of, R, C, ldo, pad);
 }
 
 // A matrix as a column operand: itself where its rows are whole 16-byte chunks on 16-byte boundaries,
@@ -358,6 +368,54 @@ ColumnOperand as_columns(const void *in, int64_t ldi, int64_t R, int64_t C, char
     return {space, Kp * 2};
 }
 
+// The slices' sums, in order, to where the product goes.
+template <class TG>
+__global__ __launch_bounds__(kThreads) void join_slices_kernel(ProductArgs a,
+                                                               const float *__restrict__ sums,
+                                                               int slices) {
+    const int64_t per = (a.N + 3) / 4, n = a.M * per;
+    for (int64_t e = int64_t(blockIdx.x) * kThreads + threadIdx.x; e < n;
+         e += int64_t(gridDim.x) * kThreads) {
+        const int64_t m = e / per, c = e % per * 4;
+        const int cnt = int(a.N - c < 4 ? a.N - c : 4);
+        f32x4 v = load4(sums, m * a.N + c, cnt, 0.0f);
+        for (int z = 1; z < slices; ++z) v += load4(sums, (z * a.M + m) * a.N + c, cnt, 0.0f);
+        const int64_t row = m < a.split ? m : m - a.split;
+        if (row < a.limit)
+            store4(m < a.split ? a.out : a.out2, row * a.ldo + c, sizeof(TG) == 2, v, cnt);
+    }
+}
+
+// A gradient product, cut into slices of its contraction where its outputs are too few to fill the
+// chip: with them a training step of 100 x 1000 x 4000 (dX: 32 tiles, 250 steps) takes 55 us in bf16,
+// 80 without.
+template <class T, class TG, bool COLS_A>
+void gradient_product(const ProductArgs &a, int slices, float *sums, void *stream) {
+    constexpr bool columns = sizeof(T) == 2;
+    if (slices == 1) {
+        if constexpr (columns)
+            launch_ring_product<T, Out::kStore, COLS_A, true>(a, stream);
+        else
+            launch_product<T, Out::kStore>(a, stream);
+        return;
+    }
+    ProductArgs part = a;
+    const int steps = (a.Kb + 32 * int(sizeof(T)) - 1) / (32 * int(sizeof(T)));
+    part.slice = (steps + slices - 1) / slices;
+    part.out = sums;
+    const unsigned used = unsigned((steps + part.slice - 1) / part.slice);
+    if constexpr (columns) {
+        using K = RingKernel<T, 64, 64, 2, 2, 8, Out::kStore, COLS_A, true>;
+        launch_tiles<K, 64>(dense_ring_kernel<T, 64, 64, 2, 2, 8, Out::kStore, COLS_A, true>, part,
+                            stream, used);
+    } else {
+        using K = SplitKernel<64, 64, 4, 2, true, Out::kStore>;
+        launch_tiles<K, 64>(dense_split_kernel<64, 64, 4, 2, true, Out::kStore>, part, stream, used);
+    }
+    hipLaunchKernelGGL(join_slices_kernel<TG>, dim3(grid_for(a.M * ((a.N + 3) / 4), kThreads, 2048)),
+                       dim3(kThreads), 0, as_stream(stream), a, sums, int(used));
+}
+
 template <class T, class TG>
 void backward(const void *dH, int64_t lddh, const void *X, int64_t T_, int64_t ldx,
               const bsr_gated_t &W, const float *G, const float *U, int64_t ldp, void *dX,
@@ -371,6 +429,7 @@ void backward(const void *dH, int64_t lddh, const void *X, int64_t T_, int64_t l
     T *Dt = reinterpret_cast<T *>(base + l.gradt_offset);
     char *x_space = base + l.x_offset, *w_space = base + l.w_offset;
     float *partial = reinterpret_cast<float *>(base + l.partial_offset);
+    float *sums = reinterpret_cast<float *>(base + l.slice_offset);
     if (T_ > 0)
         with_act(W.act, [&](auto act) {
             hipLaunchKernelGGL((gated_slope_kernel<T, decltype(act)::value, !columns>),
@@ -401,15 +460,16 @@ void backward(const void *dH, int64_t lddh, const void *X, int64_t T_, int64_t l
             a.ldb1 = u.ld;
             a.rows_k = int(F);
             a.half = int(l.Fp / 32);
-            launch_ring_product<T, Out::kStore, false, true>(a, stream);
         } else {
             T *Wt = reinterpret_cast<T *>(w_space);
-            transpose<T>(W.Wg, W.ldg, F, K, Wt, 2 * l.Fp, l.Fp, stream);
-            transpose<T>(W.Wu, W.ldu, F, K, Wt + l.Fp, 2 * l.Fp, l.Fp, stream);
+            transpose<T>({{static_cast<const T *>(W.Wg), static_cast<const T *>(W.Wu)},
+                          {W.ldg, W.ldu},
+                          {Wt, Wt + l.Fp}},
+                         2, F, K, 2 * l.Fp, l.Fp, stream);
             a.B0 = w_space;
             a.ldb0 = a.lda;
-            launch_product<T, Out::kStore>(a, stream);
         }
+        gradient_product<T, T, false>(a, l.x_slices, sums, stream);
     }
     if (dWg && T_ > 0) {          // D^T (2 F x T) times X
         a.N = K;
@@ -427,17 +487,17 @@ void backward(const void *dH, int64_t lddh, const void *X, int64_t T_, int64_t l
             a.Kb = a.half * 64;
             a.M = 2 * l.Fp;
             a.split = l.Fp;
-            launch_ring_product<T, Out::kStore, true, true>(a, stream);
         } else {
-            transpose<T>(X, ldx, T_, K, reinterpret_cast<T *>(x_space), l.Tp, l.Tp, stream);
+            transpose<T>({{static_cast<const T *>(X)}, {ldx}, {reinterpret_cast<T *>(x_space)}}, 1, T_, K,
+                         l.Tp, l.Tp, stream);
             a.A = reinterpret_cast<const char *>(Dt);
             a.B0 = x_space;
             a.lda = a.ldb0 = l.Tp * kSize<T>;
             a.Kb = int(l.Tp * kSize<T>);
             a.M = 2 * F;
             a.split = F;
-            launch_product<T, Out::kStore>(a, stream);
         }
+        gradient_product<T, TG, columns>(a, l.w_slices, sums, stream);
     } else if (dWg) {
         for (void *p : {dWg, dWu})
             hipLaunchKernelGGL(zero_rows_kernel<TG>, dim3(grid_for(F * K, kThreads, 4096)),

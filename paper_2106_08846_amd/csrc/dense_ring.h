@@ -161,10 +161,12 @@ struct RingKernel {
         using ColsA = Columns<kRowsA>;
         using ColsB = Columns<kRowsB>;
 
-        auto load = [&](int s) {
+        const Slice slice(a, (a.Kb + kRowBytes - 1) / kRowBytes);
+        auto load = [&](int step) {
+            const int s = slice.first + step;
             const int kb = s * kRowBytes;
             const bool in = kb + c * kChunk < a.Kb;      // chunks past the row's end: zeros
-            lds_char *to = (lds_char *)lds + (s % RING) * kStageBytes + wave * 1024;
+            lds_char *to = (lds_char *)lds + (step % RING) * kStageBytes + wave * 1024;
             auto columns = [&](auto cols, const ColumnSource &src, lds_char *at, int tile, int groups) {
                 unsigned ld;
                 const i32x4 rsrc = src.rsrc(s, ld);
@@ -173,7 +175,7 @@ struct RingKernel {
                     int k, chunk;
                     cols.place((i * kWaves + wave) * 64 + lane, k, chunk);
                     load_unseen(rsrc, at + i * kWaves * 1024,
-                                chunk * 8 < tile ? unsigned(k) * ld + unsigned(chunk) * kChunk : kOut);
+                                chunk * 8 < tile ? __umul24(unsigned(k), ld) + unsigned(chunk) * kChunk : kOut);
                 }
             };
             if constexpr (COLS_A) {
@@ -213,7 +215,7 @@ struct RingKernel {
             return *reinterpret_cast<const i32x4 *>(p + at_b + j * kMF * kRowBytes);
         };
         i32x4 fa[NM], fb[2][NN];
-        const int steps = (a.Kb + kRowBytes - 1) / kRowBytes;
+        const int steps = slice.steps;
 #pragma unroll
         for (int s = 0; s < RING - 1; ++s) load(s);
         wait_loads<kAhead>();          // steps 0 and 1 are there

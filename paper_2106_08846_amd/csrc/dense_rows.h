@@ -1,8 +1,8 @@
 // The dense products of few tokens (at most 32): the weights are read once, straight into the
 // operand registers of the matrix instructions, and that read is the whole cost.
 //
-// A workgroup makes 16 channels (gated: of each matrix) for every token.  Its eight waves split the
-// contraction: wave w takes every eighth block of kBlock bytes of the rows, loads a block's chunks
+// A workgroup makes 16 channels (gated: of each matrix) for 16 NT tokens (blockIdx.y counts groups of
+// them).  Its eight waves split the contraction: wave w takes every eighth block of kBlock bytes of the rows, loads a block's chunks
 // all at once, and keeps its own sums; they are added over the waves, in order, through LDS.  What
 // bounds a single token is latency: 16 rows of 4096 bytes are one block per wave, so that everything
 // a workgroup needs is in flight together.  The tokens come from the L2 (every workgroup reads all
@@ -30,7 +30,8 @@ template <class E, int NT, bool ALIGNED, Out OUT> struct RowsKernel {
         const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
         const int64_t n0 = int64_t(blockIdx.x) * kChannels;
         const int rows = int(a.N - n0 < kChannels ? a.N - n0 : kChannels);
-        const Source sx{a.A, a.lda, int(a.M)};
+        const int64_t m0 = int64_t(blockIdx.y) * (16 * NT), left_m = a.M - m0;
+        const Source sx{a.A + m0 * a.lda, a.lda, int(left_m < 16 * NT ? left_m : 16 * NT)};
         const Source sw[2] = {{a.B0 + n0 * a.ldb0, a.ldb0, rows},
                               {kDual ? a.B1 + n0 * a.ldb1 : nullptr, a.ldb1, rows}};
         const int fr = lane & 15, fc = lane >> 4;
@@ -72,7 +73,7 @@ template <class E, int NT, bool ALIGNED, Out OUT> struct RowsKernel {
         for (int v = 0; v < kWaves; ++v)
 #pragma unroll
             for (int j = 0; j < NW; ++j) sum[j] += part[((v * NW + j) * NT + wave) * 64 + lane];
-        const int64_t m = 16 * wave + fr, n = n0 + 4 * fc;
+        const int64_t m = m0 + 16 * wave + fr, n = n0 + 4 * fc;
         if (m < a.M && n < a.N)
             finish4<E, OUT>(a, m, n, int(a.N - n < 4 ? a.N - n : 4),
                             __builtin_bit_cast(i32x4, sum[0]), __builtin_bit_cast(i32x4, sum[1]));

@@ -86,8 +86,10 @@ template <int BM, int BN, int WM, int WN, bool ALIGNED, Out OUT> struct SplitKer
             else
                 chunks[i].set(rows.b(first - BM), rows.channel(row - BM), c * 2 * kChunk, a.Kb);
         }
-        auto load = [&](int step, Held &h) { // zeros from Kb on
-            const int kb = step * kStepBytes, left = a.Kb - c * 2 * kChunk - kb;
+        const Slice slice(a, (a.Kb + kStepBytes - 1) / kStepBytes);
+        const int end = min(a.Kb, (slice.first + slice.steps) * kStepBytes);
+        auto load = [&](int step, Held &h) { // zeros from the slice's end on
+            const int kb = (slice.first + step) * kStepBytes, left = end - c * 2 * kChunk - kb;
 #pragma unroll
             for (int i = 0; i < L; ++i) {
                 i32x4 v[2];
@@ -125,7 +127,7 @@ template <int BM, int BN, int WM, int WN, bool ALIGNED, Out OUT> struct SplitKer
                 fb[x][j] = *reinterpret_cast<const i32x4 *>(p + x * kPlaneBytes + at_b +
                                                            j * kMF * kRowBytes);
         };
-        const int steps = (a.Kb + kStepBytes - 1) / kStepBytes;
+        const int steps = slice.steps;
         load(0, held[0]);
         load(1, held[1]);
         load(2, held[2]);

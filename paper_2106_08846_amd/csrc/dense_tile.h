@@ -60,6 +60,8 @@ struct ProductArgs {
     int rows_k, half;             // column operands: rows of each matrix, and the step from which on
                                   // the second one (B1) is taken
     int tiles_m, tiles_n;
+    int slice;                    // kStore: steps of the contraction per workgroup, blockIdx.y counting
+                                  // slices whose sums go to out + blockIdx.y * M * N; 0: all of them
     // epilogue
     const float *sx, *s0, *s1;    // scales of tokens and channels (int8)
     const float *b0, *b1;         // biases or NULL
@@ -128,6 +130,10 @@ __device__ __forceinline__ void finish4(const ProductArgs &a, int64_t m, int64_t
         y = __builtin_bit_cast(f32x4, q);
     }
     if constexpr (OUT == Out::kStore) {
+        if (a.slice > 0) {
+            store4(a.out, (blockIdx.y * a.M + m) * a.N + n, false, x, cnt);
+            return;
+        }
         const int64_t row = m < a.split ? m : m - a.split;
         if (row < a.limit) store4(m < a.split ? a.out : a.out2, row * a.ldo + n, a.out_bf16, x, cnt);
         return;
@@ -239,6 +245,15 @@ __device__ __forceinline__ void tile_of(const ProductArgs &a, int &tm, int &tn) 
     tm = first + in % height;
     tn = in / height;
 }
+
+// The steps of the contraction that this workgroup sums: `steps` from `first` on, of `total`.
+struct Slice {
+    int first, steps;
+    __device__ __forceinline__ Slice(const ProductArgs &a, int total) {
+        first = a.slice > 0 ? int(blockIdx.y) * a.slice : 0;
+        steps = a.slice > 0 && total - first > a.slice ? a.slice : total - first;
+    }
+};
 
 // The rows of both operands that a workgroup's tile takes: BM tokens, kTileN channels of each of B's
 // matrices.

@@ -398,7 +398,13 @@ GatedWorkspace gated_workspace_layout(int64_t T, int64_t K, int64_t F, int32_t d
     w.x_offset = align256(w.gradt_offset + (bf16 ? 0 : size_t(2 * F * w.Tp * e)));
     w.w_offset = align256(w.x_offset + size_t(bf16 ? T * w.Kp * e : K * w.Tp * e));
     w.partial_offset = align256(w.w_offset + size_t(bf16 ? 2 * F * w.Kp * e : K * 2 * w.Fp * e));
-    w.total = align256(w.partial_offset + size_t(blocks * 2 * F * 4));
+    w.slice_offset = align256(w.partial_offset + size_t(blocks * 2 * F * 4));
+    const int64_t dw_rows = bf16 ? 2 * w.Fp : 2 * F;
+    w.x_slices = gated_slices(T, K, (2 * w.Fp + 31) / 32, bf16);
+    w.w_slices = gated_slices(dw_rows, K, (T + 31) / 32, bf16);
+    const int64_t xs = w.x_slices > 1 ? w.x_slices * T * K : 0;
+    const int64_t ws = w.w_slices > 1 ? w.w_slices * dw_rows * K : 0;
+    w.total = align256(w.slice_offset + size_t(xs > ws ? xs : ws) * 4);
     if (w.total == 0) w.total = 256;
     return w;
 }
