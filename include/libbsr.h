@@ -496,7 +496,7 @@ LIBBSR_API bsr_status bsr_quantize_rows(const void *X, bsr_dtype x_dtype, int64_
  * T = 0 is a no-op; N, K >= 1.  Y must not overlap an input.
  * Errors: BSR_ERR_NULL, BSR_ERR_SHAPE, BSR_ERR_ARG (unknown dtype, overlap), BSR_ERR_DTYPE (y_dtype
  *   BSR_I8), BSR_ERR_UNSUPPORTED (K above 131071, where the 32-bit sum could overflow; N or a pitch
- *   above 2^20, T above 2^24, T * N above 2^37), BSR_ERR_ARCH, BSR_ERR_HIP.
+ *   above 2^20, T above 2^24, T * N above 2^36), BSR_ERR_ARCH, BSR_ERR_HIP.
  */
 LIBBSR_API bsr_status bsr_matmul_i8(const int8_t *Xq, int64_t T, int64_t K, int64_t ldx,
                                     const float *sx, const int8_t *Wq, int64_t N, int64_t ldw,
@@ -532,11 +532,15 @@ typedef struct {
  * G, U: device fp32, T x F with row pitch ldp, or both NULL: the pre-activations, kept for
  *   bsr_gated_backward (fp32 also for bf16 blocks, so that the gradients are not those of rounded
  *   pre-activations).
- * fp32 blocks form their products in fp32 arithmetic.
+ * bf16 products are exact in fp32.  fp32 products of more than a few tokens are formed from three bf16
+ *   pieces of each operand (six exact cross terms; what is left out is below 2^-25.9 of the product,
+ *   a quarter of fp32's rounding, for operands of 2^-100 or more), otherwise by fp32 instructions: an
+ *   infinite operand, or one from 2^128 (1 - 2^-9) on, may give NaN where fp32 arithmetic gives an
+ *   infinity; it reaches the outputs of its token, or of its channel, only.
  * T = 0 is a no-op.  H, G and U must not overlap an input or each other.
  * Errors: BSR_ERR_NULL (also: one of G and U without the other), BSR_ERR_SHAPE, BSR_ERR_ARG (unknown
  *   dtype or activation, overlap), BSR_ERR_DTYPE (BSR_I8), BSR_ERR_UNSUPPORTED (K, F or a pitch
- *   above 2^20, T above 2^24, T * F above 2^36), BSR_ERR_ARCH, BSR_ERR_HIP.
+ *   above 2^20, T above 2^24, T * F above 2^35), BSR_ERR_ARCH, BSR_ERR_HIP.
  */
 LIBBSR_API bsr_status bsr_gated(const void *X, int64_t T, int64_t ldx, const bsr_gated_t *W,
                                 void *H, int64_t ldh, float *G, float *U, int64_t ldp,
@@ -552,7 +556,8 @@ LIBBSR_API size_t bsr_gated_workspace_bytes(int64_t T, int64_t K, int64_t F, bsr
  *   of the products below),
  *   dX = dG Wg + dU Wu,  dWg = dG^T X,  dWu = dU^T X,
  *   dbg[f] = sum over t of dG[t][f],  dbu[f] = sum over t of dU[t][f]  (of the unrounded values).
- * Sums are fp32 in a fixed order: repeated calls are bitwise reproducible.
+ * Sums are fp32 in an order fixed by the sizes, products as in bsr_gated: repeated calls are bitwise
+ * reproducible.
  * dH: device, T x F of W->dtype, row pitch lddh.  X, W as in the forward call (biases are not
  *   read).  G, U: device fp32, T x F, row pitch ldp, as bsr_gated wrote them.
  * dX: device, T x K of W->dtype, row pitch lddx, or NULL (not wanted).
@@ -564,7 +569,7 @@ LIBBSR_API size_t bsr_gated_workspace_bytes(int64_t T, int64_t K, int64_t F, bsr
  * T = 0 sets the weight and bias gradients to zero.  Outputs and workspace must not overlap an input
  * or each other.
  * Errors: those of bsr_gated, BSR_ERR_NULL (one of dWg and dWu without the other), BSR_ERR_WORKSPACE
- *   (missing, too small or misaligned), BSR_ERR_UNSUPPORTED (T above 2^20).
+ *   (missing, too small or misaligned), BSR_ERR_UNSUPPORTED (T above 2^20, F above 2^19 - 32).
  */
 LIBBSR_API bsr_status bsr_gated_backward(const void *dH, int64_t lddh, const void *X, int64_t T,
                                          int64_t ldx, const bsr_gated_t *W, const float *G,

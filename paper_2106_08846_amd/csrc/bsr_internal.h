@@ -77,8 +77,9 @@ bsr_status check_attention(const float *Q, int64_t ldq, const float *K, int64_t 
 // tile spans at most 256 rows of at most 4 MiB) and every grid below 2^22 workgroups.
 constexpr int64_t kDenseMaxWidth = int64_t(1) << 20;    // columns and pitches, elements
 constexpr int64_t kDenseMaxTokens = int64_t(1) << 24;
-constexpr int64_t kDenseMaxOut = int64_t(1) << 37;      // elements of all outputs of one tile grid
-constexpr int64_t kGatedMaxBackwardTokens = int64_t(1) << 20;   // T is a pitch of the transposes
+constexpr int64_t kDenseMaxOut = int64_t(1) << 36;      // elements of all outputs of one tile grid
+constexpr int64_t kGatedMaxBackwardTokens = int64_t(1) << 20;   // T is a pitch (fp32 transposes)
+constexpr int64_t kGatedMaxBackwardWidth = kDenseMaxWidth / 2 - 32;   // F: 2 F, padded, is a pitch
 constexpr int64_t kI8MaxK = 131071;                     // 2^14 * K stays below 2^31
 bsr_status check_quantize_rows(const void *X, int32_t x_dtype, int64_t T, int64_t K, int64_t ldx,
                                const int8_t *Q, int64_t ldq, const float *scale);

@@ -112,24 +112,29 @@ __global__ __launch_bounds__(64 * WAVES * ROWS) void quantize_rows_kernel(
 }
 
 template <class T, int WAVES, int ROWS>
-void launch(const void *X, int64_t T_, int64_t K, int64_t ldx, int8_t *Q, int64_t ldq, float *scale,
+void launch(const T *X, int64_t T_, int64_t K, int64_t ldx, int8_t *Q, int64_t ldq, float *scale,
             void *stream) {
     const auto kernel = K % (64 * WAVES * kVec) == 0 ? quantize_rows_kernel<T, WAVES, ROWS, true>
                                                      : quantize_rows_kernel<T, WAVES, ROWS, false>;
-    hipLaunchKernelGGL(kernel, dim3(unsigned((T_ + ROWS - 1) / ROWS)), dim3(64 * WAVES * ROWS), 0,
-                       as_stream(stream), static_cast<const T *>(X), T_, int(K), ldx, Q, ldq, scale);
+    constexpr int64_t most = int64_t(1) << 21;     // rows of a launch: a grid has under 2^32 threads
+    for (int64_t t = 0; t < T_; t += most) {
+        const int64_t n = T_ - t < most ? T_ - t : most;
+        hipLaunchKernelGGL(kernel, dim3(unsigned((n + ROWS - 1) / ROWS)), dim3(64 * WAVES * ROWS), 0,
+                           as_stream(stream), X + t * ldx, n, int(K), ldx, Q + t * ldq, ldq, scale + t);
+    }
 }
 
 template <class T>
 void quantize(const void *X, int64_t T_, int64_t K, int64_t ldx, int8_t *Q, int64_t ldq,
               float *scale, void *stream) {
+    const T *x = static_cast<const T *>(X);
     constexpr int64_t held = 64 * kVec * kHeld;   // elements of a row that a wave holds
     if (K <= held)
-        launch<T, 1, 4>(X, T_, K, ldx, Q, ldq, scale, stream);
+        launch<T, 1, 4>(x, T_, K, ldx, Q, ldq, scale, stream);
     else if (K <= 4 * held)
-        launch<T, 4, 1>(X, T_, K, ldx, Q, ldq, scale, stream);
+        launch<T, 4, 1>(x, T_, K, ldx, Q, ldq, scale, stream);
     else
-        launch<T, 16, 1>(X, T_, K, ldx, Q, ldq, scale, stream);
+        launch<T, 16, 1>(x, T_, K, ldx, Q, ldq, scale, stream);
 }
 
 }  // namespace

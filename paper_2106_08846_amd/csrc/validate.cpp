@@ -279,9 +279,10 @@ struct Span {
     int64_t bytes;
 };
 
-// `rows` rows of `width` elements of `size` bytes at pitch ld (sizes checked before).
+// `rows` rows of `width` elements of `size` bytes at pitch ld: sizes that are checked before, except
+// the pitch of an array that is not given.
 Span span(const void *p, int64_t rows, int64_t ld, int64_t width, int64_t size) {
-    return Span{p, rows > 0 ? ((rows - 1) * ld + width) * size : 0};
+    return Span{p, p && rows > 0 ? ((rows - 1) * ld + width) * size : 0};
 }
 
 // No output overlaps an input or another output.
@@ -423,7 +424,7 @@ bsr_status check_gated_backward(const void *dH, int64_t lddh, const void *X, int
     if (lddh < F || ldp < F || (dX && lddx < K) || (dw && lddw < K)) return BSR_ERR_SHAPE;
     if (T > kGatedMaxBackwardTokens || lddh > kDenseMaxWidth || ldp > kDenseMaxWidth ||
         (dX && lddx > kDenseMaxWidth) || (dw && lddw > kDenseMaxWidth) ||
-        2 * F > kDenseMaxWidth - 64 || F * K > kDenseMaxOut / 2 || T * K > kDenseMaxOut)
+        F > kGatedMaxBackwardWidth || F * K > kDenseMaxOut / 2 || T * K > kDenseMaxOut)
         return BSR_ERR_UNSUPPORTED;
     if (dw && (!dWg || !dWu)) return BSR_ERR_NULL;
     if (T > 0 && (!dH || !X || !G || !U)) return BSR_ERR_NULL;
@@ -448,7 +449,7 @@ extern "C" {
 size_t bsr_gated_workspace_bytes(int64_t T, int64_t K, int64_t F, bsr_dtype dtype) {
     const int32_t dt = bsr::raw_enum(dtype);
     if (T < 0 || K < 1 || F < 1 || T > bsr::kGatedMaxBackwardTokens ||
-        K > bsr::kDenseMaxWidth || 2 * F > bsr::kDenseMaxWidth - 64 ||
+        K > bsr::kDenseMaxWidth || F > bsr::kGatedMaxBackwardWidth ||
         (dt != BSR_F32 && dt != BSR_BF16))
         return 0;
     return bsr::gated_workspace_layout(T, K, F, dt).total;

@@ -134,7 +134,9 @@ def test_matmul_i8(T, N, K, out, pad, shift):
 
 # Outputs large enough for the largest tiles: ragged in both directions, a depth that ends inside a
 # step, rows on and off 16-byte boundaries.
-LARGE = [(3330, 4100, 144), (3330, 4100, 130), (4000, 2900, 64), (6100, 2048, 200), (6100, 2048, 208)]
+LARGE = [(3330, 4100, 144), (3330, 4100, 130), (4000, 2900, 64), (6100, 2048, 200), (6100, 2048, 208),
+         (4090, 2040, 96), (4090, 2040, 99), (2040, 2044, 160), (2040, 2044, 167), (1020, 1024, 80),
+         (1020, 1024, 77), (100, 1000, 2064), (64, 512, 1000), (127, 256, 777)]
 
 
 @pytest.mark.parametrize("T,N,K", LARGE)
@@ -160,6 +162,7 @@ def test_gated_large(T, F, K, dtype):
                  for s in ((T, K), (F, K), (F, K)))
     g, u = x @ wg.t(), x @ wu.t()
     h = torch.clamp(g, min=0) * u
+    assert h.abs().max() < 2 ** 24          # exact in fp32
     if dtype == "i8":
         one = torch.ones(max(T, F), device=DEV)
         H = B.bsr_gated_i8(x.to(torch.int8), one[:T], wg.to(torch.int8), one[:F], wu.to(torch.int8),
@@ -170,13 +173,35 @@ def test_gated_large(T, F, K, dtype):
     H, G, U = B.bsr_gated(x.to(dt), wg.to(dt), wu.to(dt), act="relu", save=True)
     assert torch.equal(G.double(), g) and torch.equal(U.double(), u)
     assert torch.equal(H, h.float().to(dt))
-    gi, ui = torch.clamp(g, -3, 3), torch.clamp(u, -3, 3)
-    dh = torch.randint(-1, 2, (T, F), device=DEV, generator=gen).double()
-    got = B.bsr_gated_backward(dh.to(dt), x.to(dt), wg.to(dt), wu.to(dt), gi.float(), ui.float(),
-                               act="relu", bias=True, grad_dtype=torch.float32)
-    dg, du = dh * ui * (gi > 0), dh * torch.clamp(gi, min=0)
+
+
+# Gradients whose outputs meet every tile (dX: T x K, the weights' 2 F x K), and some whose outputs are
+# so few that their contraction is sliced (over F, or over T).
+GRADIENTS = [(4090, 4088, 33), (6100, 2048, 20), (4090, 2040, 33), (2040, 2040, 17), (40, 4090, 2040),
+             (50, 2040, 3050), (33, 2040, 2040), (70, 2040, 1020), (70, 40, 5000), (1, 264, 4100),
+             (5000, 48, 40), (9000, 33, 30), (300, 200, 2111)]
+
+
+@pytest.mark.parametrize("T,K,F", GRADIENTS)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gated_backward_large(T, K, F, dtype):
+    """Whole numbers small enough that every sum is exact."""
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(T + K + F)
+    dt = TORCH[dtype]
+
+    def ints(lo, hi, *shape):
+        return torch.randint(lo, hi + 1, shape, device=DEV, generator=gen).double()
+
+    x, wg, wu, dh = ints(-2, 2, T, K), ints(-2, 2, F, K), ints(-2, 2, F, K), ints(-1, 1, T, F)
+    g, u = ints(-3, 3, T, F), ints(-3, 3, T, F)
+    dX, clean = frame(T, K, dt, 8, 0)
+    got = B.bsr_gated_backward(dh.to(dt), x.to(dt), wg.to(dt), wu.to(dt), g.float(), u.float(),
+                               act="relu", bias=True, grad_dtype=torch.float32, dX=dX)
+    dg, du = dh * u * (g > 0), dh * torch.clamp(g, min=0)
     for t, want in zip(got, (dg @ wg + du @ wu, dg.t() @ x, du.t() @ x, dg.sum(0), du.sum(0))):
         assert torch.equal(t, want.float().to(t.dtype))
+    assert clean()
 
 
 def test_matmul_i8_longest_rows():
@@ -347,6 +372,55 @@ def test_gated_non_finite_values_stay_in_their_rows(dtype, T):
     assert torch.equal(H[keep], clean[keep])
     if T > 1:
         assert not torch.isfinite(G[T - 2]).any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [1, 40, 300])
+def test_gated_non_finite_weights_stay_in_their_channels(dtype, T):
+    rng = np.random.default_rng(12)
+    x = rand(rng, T, 100, dtype=dtype).to(DEV)
+    wg, wu = (rand(rng, 90, 100, dtype=dtype).to(DEV) for _ in range(2))
+    clean, G0, U0 = B.bsr_gated(x, wg, wu, save=True)
+    wg[7, 3], wu[50, 99], wu[89, 0] = float("inf"), float("nan"), -3.4e38
+    H, G, U = B.bsr_gated(x, wg, wu, save=True)
+    assert not torch.isfinite(G[:, 7]).any() and torch.isnan(U[:, 50]).all()
+    keep = [f for f in range(90) if f not in (7, 50, 89)]
+    assert torch.equal(H[:, keep], clean[:, keep])
+    assert torch.equal(G[:, 50], G0[:, 50]) and torch.equal(U[:, 7], U0[:, 7])
+
+
+def test_offsets_past_32_bits():
+    """Rows that start more than 2^31 and 2^32 bytes into their matrices."""
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 40 GB")
+    pitch, T, K, F = 1 << 20, 2200, 40, 48                # int8 rows a MiB apart; bf16 two
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(1)
+    ints = lambda *s: torch.randint(-2, 3, s, device=DEV, generator=gen)  # noqa: E731
+    small, w = ints(T, K), ints(F, K)
+    one = torch.ones(T, device=DEV)
+    want = small.double() @ w.double().t()
+    x8 = torch.empty(T, pitch, dtype=torch.int8, device=DEV)[:, :K]
+    x8.copy_(small)
+    y = torch.empty(T, pitch, dtype=torch.bfloat16, device=DEV)[:, :F]
+    B.bsr_matmul_i8(x8, one, w.to(torch.int8), one[:F], Y=y)
+    assert torch.equal(y.double(), want)
+    q, s = B.bsr_quantize_rows(y)
+    wq, ws = D.quantize_rows(y.float().cpu().numpy())
+    assert np.array_equal(host(q), wq) and np.array_equal(host(s), ws)
+    del x8
+    x = torch.empty(T, pitch, dtype=torch.bfloat16, device=DEV)[:, :K]
+    x.copy_(small)
+    wb = w.to(torch.bfloat16)
+    H, G, U = B.bsr_gated(x, wb, wb, act="relu", save=True, H=y)
+    assert torch.equal(G.double(), want) and torch.equal(U.double(), want)
+    assert torch.equal(H, (torch.clamp(want, min=0) * want).float().to(torch.bfloat16))
+    y.fill_(1)
+    grads = B.bsr_gated_backward(y, x, wb, wb, torch.ones_like(G), torch.ones_like(U), act="relu",
+                                 grad_dtype=torch.float32, dX=x.clone())
+    ones = torch.ones(T, F, dtype=torch.float64, device=DEV)
+    assert torch.equal(grads[0].double(), 2 * ones @ w.double())
+    assert torch.equal(grads[1].double(), ones.t() @ small.double())
 
 
 @pytest.mark.parametrize("T,K,F", GATED_SIZES + [(16, 2048, 512)])
