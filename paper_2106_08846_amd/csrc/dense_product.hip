@@ -68,22 +68,71 @@ int64_t rounds(const ProductArgs &a, bool dual, int bm, int bn, int cost) {
 // in 128 x 128 and 259 in 64 x 64; 2048^3 51, 24 and 33; 128 x 8192 x 4096 84, 35 and 20; and
 // 6144 x 2048 x 16384, whose 192 tiles of 256 x 256 leave a quarter of the CUs idle, 438 against 368
 // in 192 x 256; int8 2048 x 20480 x 4096 184 in 256 x 256 (2.5 rounds) and 196 in 192 x 256 (3.4).
-template <class E, Out OUT, bool COLS_A = false, bool COLS_B = false>
-void launch_ring_product(const ProductArgs &a, void *stream) {
-    constexpr bool dual = OUT == Out::kGated;
-    const int64_t cost[5] = {rounds(a, dual, 256, 256, 100), rounds(a, dual, 192, 256, 78),
-                             rounds(a, dual, 128, 256, 62), rounds(a, dual, 128, 128, 38),
-                             rounds(a, dual, 64, 64, 16)};
-    int best = 0;
-    for (int i = 1; i < 5; ++i)
+constexpr int kRingTiles = 5;
+int64_t ring_cost(const ProductArgs &a, bool dual, int &best) {
+    const int64_t cost[kRingTiles] = {rounds(a, dual, 256, 256, 100), rounds(a, dual, 192, 256, 78),
+                                      rounds(a, dual, 128, 256, 62), rounds(a, dual, 128, 128, 38),
+                                      rounds(a, dual, 64, 64, 16)};
+    best = 0;
+    for (int i = 1; i < kRingTiles; ++i)
         if (cost[i] < cost[best]) best = i;
-    switch (best) {
+    return cost[best];
+}
+
+template <class E, Out OUT, bool COLS_A, bool COLS_B>
+void launch_ring_tile(const ProductArgs &a, int tile, void *stream) {
+    switch (tile) {
         case 0: return launch_ring<E, 256, 256, 2, 4, 4, OUT, COLS_A, COLS_B>(a, stream);
         case 1: return launch_ring<E, 192, 256, 2, 4, 4, OUT, COLS_A, COLS_B>(a, stream);
         case 2: return launch_ring<E, 128, 256, 2, 4, 4, OUT, COLS_A, COLS_B>(a, stream);
         case 3: return launch_ring<E, 128, 128, 2, 4, 4, OUT, COLS_A, COLS_B>(a, stream);
         default: return launch_ring<E, 64, 64, 2, 2, 8, OUT, COLS_A, COLS_B>(a, stream);
     }
+}
+
+// The product's channels from n on, as a product of its own.
+ProductArgs channels_from(ProductArgs a, int64_t n, bool cols_b) {
+    const int64_t out_size = a.out_bf16 ? 2 : 4;
+    const auto skip = [&](const char *p, int64_t ld) { return p ? p + (cols_b ? 2 * n : n * ld) : p; };
+    const auto vec = [&](const float *p) { return p ? p + n : p; };
+    const auto out = [&](void *p) { return p ? static_cast<char *>(p) + n * out_size : nullptr; };
+    a.B0 = skip(a.B0, a.ldb0);
+    a.B1 = skip(a.B1, a.ldb1);
+    a.s0 = vec(a.s0);
+    a.s1 = vec(a.s1);
+    a.b0 = vec(a.b0);
+    a.b1 = vec(a.b1);
+    a.out = out(a.out);
+    a.out2 = out(a.out2);
+    a.G = a.G ? a.G + n : nullptr;
+    a.U = a.U ? a.U + n : nullptr;
+    a.N -= n;
+    return a;
+}
+
+// A product whose last round of 256 x 256 tiles is not full goes in two launches where that saves a
+// twentieth: as many channels as fill whole rounds, then the rest in the tile that suits it
+// (int8 2048 tokens through 2 x 10240 x 4096: 640 tiles in 2.5 rounds).
+template <class E, Out OUT, bool COLS_A = false, bool COLS_B = false>
+void launch_ring_product(const ProductArgs &a, void *stream) {
+    constexpr bool dual = OUT == Out::kGated;
+    constexpr int64_t kChannels = dual ? 128 : 256;
+    int tile, rest_tile;
+    const int64_t whole = ring_cost(a, dual, tile);
+    const int64_t cus = device_cu_count(), tiles_m = (a.M + 255) / 256;
+    const int64_t tiles_n = (a.N + kChannels - 1) / kChannels;
+    const int64_t columns = tiles_m * tiles_n / cus * cus / tiles_m;    // of tiles, in full rounds
+    if (columns > 0 && columns < tiles_n) {
+        ProductArgs first = a;
+        first.N = columns * kChannels;
+        const ProductArgs rest = channels_from(a, first.N, COLS_B);
+        const int64_t parts = rounds(first, dual, 256, 256, 100) + ring_cost(rest, dual, rest_tile);
+        if (parts * 20 <= whole * 19) {
+            launch_ring_tile<E, OUT, COLS_A, COLS_B>(first, 0, stream);
+            return launch_ring_tile<E, OUT, COLS_A, COLS_B>(rest, rest_tile, stream);
+        }
+    }
+    launch_ring_tile<E, OUT, COLS_A, COLS_B>(a, tile, stream);
 }
 
 template <class E, Out OUT> void launch_product(const ProductArgs &a, void *stream) {

@@ -136,7 +136,8 @@ def test_matmul_i8(T, N, K, out, pad, shift):
 # step, rows on and off 16-byte boundaries.
 LARGE = [(3330, 4100, 144), (3330, 4100, 130), (4000, 2900, 64), (6100, 2048, 200), (6100, 2048, 208),
          (4090, 2040, 96), (4090, 2040, 99), (2040, 2044, 160), (2040, 2044, 167), (1020, 1024, 80),
-         (1020, 1024, 77), (100, 1000, 2064), (64, 512, 1000), (127, 256, 777)]
+         (1020, 1024, 77), (100, 1000, 2064), (64, 512, 1000), (127, 256, 777), (2040, 20470, 64),
+         (4096, 5000, 64)]
 
 
 @pytest.mark.parametrize("T,N,K", LARGE)
@@ -179,7 +180,7 @@ def test_gated_large(T, F, K, dtype):
 # so few that their contraction is sliced (over F, or over T).
 GRADIENTS = [(4090, 4088, 33), (6100, 2048, 20), (4090, 2040, 33), (2040, 2040, 17), (40, 4090, 2040),
              (50, 2040, 3050), (33, 2040, 2040), (70, 2040, 1020), (70, 40, 5000), (1, 264, 4100),
-             (5000, 48, 40), (9000, 33, 30), (300, 200, 2111)]
+             (5000, 48, 40), (9000, 33, 30), (300, 200, 2111), (4096, 5000, 33), (2048, 20480, 24)]
 
 
 @pytest.mark.parametrize("T,K,F", GRADIENTS)
