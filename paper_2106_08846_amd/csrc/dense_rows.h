@@ -74,8 +74,9 @@ template <class E, int NT, bool ALIGNED, Out OUT> struct RowsKernel {
 #pragma unroll
             for (int j = 0; j < NW; ++j) sum[j] += part[((v * NW + j) * NT + wave) * 64 + lane];
         const int64_t m = m0 + 16 * wave + fr, n = n0 + 4 * fc;
-        if (m < a.M && n < a.N)
-            finish4<E, OUT>(a, m, n, int(a.N - n < 4 ? a.N - n : 4),
+        const int cnt = a.N - n < 4 ? int(a.N - n) : 4;
+        if (m < a.M && cnt > 0)
+            finish4<E, OUT>(a, ChannelQuad<E, OUT>(a, n, cnt), m, n, cnt,
                             __builtin_bit_cast(i32x4, sum[0]), __builtin_bit_cast(i32x4, sum[1]));
     }
 };

@@ -113,11 +113,27 @@ __device__ __forceinline__ float activate_by(int act, float g) {
     }
 }
 
+// What four channels from n on (`cnt` of which exist) bring to every token's outputs.
+template <class E, Out OUT> struct ChannelQuad {
+    f32x4 s0, s1, b0, b1;
+    __device__ __forceinline__ ChannelQuad(const ProductArgs &a, int64_t n, int cnt) {
+        if constexpr (OUT != Out::kStore) {
+            if constexpr (sizeof(E) == 1) {
+                s0 = load4(a.s0, n, cnt, 0.0f);
+                if constexpr (OUT == Out::kGated) s1 = load4(a.s1, n, cnt, 0.0f);
+            }
+            b0 = b1 = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            if (a.b0) b0 = load4(a.b0, n, cnt, 0.0f);
+            if (OUT == Out::kGated && a.b1) b1 = load4(a.b1, n, cnt, 0.0f);
+        }
+    }
+};
+
 // Four outputs of token m from channel n on (`cnt` of them exist): `p`, and for kGated `q`, hold
 // the products (int8: as integers).
 template <class E, Out OUT>
-__device__ __forceinline__ void finish4(const ProductArgs &a, int64_t m, int64_t n, int cnt,
-                                        i32x4 p, i32x4 q) {
+__device__ __forceinline__ void finish4(const ProductArgs &a, const ChannelQuad<E, OUT> &of, int64_t m,
+                                        int64_t n, int cnt, i32x4 p, i32x4 q) {
     f32x4 x, y;
     if constexpr (sizeof(E) == 1) {
 #pragma unroll
@@ -140,14 +156,14 @@ __device__ __forceinline__ void finish4(const ProductArgs &a, int64_t m, int64_t
     }
     if constexpr (sizeof(E) == 1) {
         const float s = a.sx[m];
-        x = x * s * load4(a.s0, n, cnt, 0.0f);
-        if constexpr (OUT == Out::kGated) y = y * s * load4(a.s1, n, cnt, 0.0f);
+        x = x * s * of.s0;
+        if constexpr (OUT == Out::kGated) y = y * s * of.s1;
     }
-    if (a.b0) x += load4(a.b0, n, cnt, 0.0f);
+    if (a.b0) x += of.b0;
     if constexpr (OUT == Out::kScale) {
         store4(a.out, m * a.ldo + n, a.out_bf16, x, cnt);
     } else {
-        if (a.b1) y += load4(a.b1, n, cnt, 0.0f);
+        if (a.b1) y += of.b1;
         f32x4 h;
 #pragma unroll
         for (int i = 0; i < 4; ++i) h[i] = activate_by(a.act, x[i]) * y[i];
@@ -307,8 +323,15 @@ __device__ __forceinline__ void epilogue(const ProductArgs &a, const Acc (&acc)[
                                          int64_t m0, int64_t n0) {
     constexpr bool kDual = OUT == Out::kGated;
     constexpr int kPitch = NN * kMF + 4;
-    constexpr int kQuads = NN * kMF / (kDual ? 8 : 4);
+    constexpr int kQuads = NN * kMF / (kDual ? 8 : 4);      // of a token; a lane keeps its own
+    static_assert(64 % kQuads == 0, "whole tokens per pass");
     const int lane = threadIdx.x & 63, fr = lane % kMF, fc = lane / kMF;
+    const int quad = lane % kQuads;
+    const int64_t n = n0 + quad * 4;
+    const int cnt = a.N - n < 4 ? int(a.N - n) : 4;
+    const ChannelQuad<E, OUT> of(a, n, cnt);                // nothing where cnt <= 0
+    const int pair = quad / (kMF / 4), r = quad % (kMF / 4) * 4;
+    const int at = kDual ? pair * 2 * kMF + r : quad * 4;
 #pragma unroll
     for (int i = 0; i < NM; ++i) {
 #pragma unroll
@@ -323,20 +346,13 @@ __device__ __forceinline__ void epilogue(const ProductArgs &a, const Acc (&acc)[
         }
         wave_sync();
 #pragma unroll 1
-        for (int e = lane; e < kMF * kQuads; e += 64) {
-            const int t = e / kQuads, quad = e % kQuads;
-            const int64_t m = m0 + i * kMF + t, n = n0 + quad * 4;
-            const float *p = mine + t * kPitch;
-            i32x4 x, y = {0, 0, 0, 0};
-            if constexpr (kDual) {
-                const int pair = quad / (kMF / 4), r = quad % (kMF / 4) * 4;
-                x = *reinterpret_cast<const i32x4 *>(p + pair * 2 * kMF + r);
-                y = *reinterpret_cast<const i32x4 *>(p + pair * 2 * kMF + kMF + r);
-            } else {
-                x = *reinterpret_cast<const i32x4 *>(p + quad * 4);
-            }
-            if (m < a.M && n < a.N)
-                finish4<E, OUT>(a, m, n, int(a.N - n < 4 ? a.N - n : 4), x, y);
+        for (int t = lane / kQuads; t < kMF; t += 64 / kQuads) {
+            const int64_t m = m0 + i * kMF + t;
+            const float *p = mine + t * kPitch + at;
+            const i32x4 x = *reinterpret_cast<const i32x4 *>(p);
+            i32x4 y = {0, 0, 0, 0};
+            if constexpr (kDual) y = *reinterpret_cast<const i32x4 *>(p + kMF);
+            if (m < a.M && cnt > 0) finish4<E, OUT>(a, of, m, n, cnt, x, y);
         }
         wave_sync();
     }
