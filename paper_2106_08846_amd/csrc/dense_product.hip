@@ -431,7 +431,7 @@ __global__ __launch_bounds__(kThreads) void join_slices_kernel(ProductArgs a,
         for (int z = 1; z < slices; ++z) v += load4(sums, (z * a.M + m) * a.N + c, cnt, 0.0f);
         const int64_t row = m < a.split ? m : m - a.split;
         if (row < a.limit)
-            store4(m < a.split ? a.out : a.out2, row * a.ldo + c, sizeof(TG) == 2, v, cnt);
+            store4<false>(m < a.split ? a.out : a.out2, row * a.ldo + c, sizeof(TG) == 2, v, cnt);
     }
 }
 

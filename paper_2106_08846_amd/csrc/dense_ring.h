@@ -251,8 +251,14 @@ struct RingKernel {
         if (s < steps) step(s, fb[0], fb[1]);
         wait_loads<0>();               // what was loaded past the end, before LDS is used again
         __syncthreads();
-        epilogue<E, OUT, NN, NM>(a, acc, reinterpret_cast<float *>(lds + wave * epilogue_bytes(NN)),
-                                 rows.m0 + wm * TM, rows.n0 + wn * (kDual ? TN / 2 : TN));
+        // The tiles that large products take write more than the L2s hold, and store past them: a gated
+        // int8 block of 2048 tokens, 4096 to 10240 features, takes 178 us with plain stores and 165 so,
+        // an int8 product of 8192^3 460 and 453.  The smaller tiles' outputs stay for the kernel that
+        // reads them next (the fp32 gradients of 1000 tokens, 768 features and 1531 hidden units: 150
+        // us past the caches, 146 through them).
+        constexpr bool kPast = BM * BN >= 192 * 256;
+        epilogue<E, OUT, NN, NM, kPast>(a, acc, reinterpret_cast<float *>(lds + wave * epilogue_bytes(NN)),
+                                        rows.m0 + wm * TM, rows.n0 + wn * (kDual ? TN / 2 : TN));
     }
 };
 

@@ -71,21 +71,31 @@ struct ProductArgs {
     int out_bf16, act;
 };
 
-// 4 consecutive outputs, of which the first `n` exist.
+// 4 consecutive outputs, of which the first `n` exist.  PAST: stored past the caches, so that the
+// operands which other workgroups still read keep their place.
+template <bool PAST>
 __device__ __forceinline__ void store4(void *base, int64_t at, bool as_bf16, f32x4 v, int n) {
     if (as_bf16) {
         bf16x4 h;
 #pragma unroll
         for (int i = 0; i < 4; ++i) h[i] = static_cast<__bf16>(v[i]);
         __bf16 *p = static_cast<__bf16 *>(base) + at;
-        if (n >= 4) {
+        if (PAST && n >= 4) {
+            typedef unsigned Words __attribute__((ext_vector_type(2), aligned(2)));
+            Words w;
+            __builtin_memcpy(&w, &h, 8);
+            __builtin_nontemporal_store(w, reinterpret_cast<Words *>(p));
+        } else if (n >= 4) {
             __builtin_memcpy(p, &h, 8);
         } else {
             for (int i = 0; i < n; ++i) p[i] = h[i];
         }
     } else {
         float *p = static_cast<float *>(base) + at;
-        if (n >= 4) {
+        if (PAST && n >= 4) {
+            typedef float Floats __attribute__((ext_vector_type(4), aligned(4)));
+            __builtin_nontemporal_store(Floats(v), reinterpret_cast<Floats *>(p));
+        } else if (n >= 4) {
             __builtin_memcpy(p, &v, 16);
         } else {
             for (int i = 0; i < n; ++i) p[i] = v[i];
@@ -131,7 +141,7 @@ template <class E, Out OUT> struct ChannelQuad {
 
 // Four outputs of token m from channel n on (`cnt` of them exist): `p`, and for kGated `q`, hold
 // the products (int8: as integers).
-template <class E, Out OUT>
+template <class E, Out OUT, bool PAST>
 __device__ __forceinline__ void finish4(const ProductArgs &a, const ChannelQuad<E, OUT> &of, int64_t m,
                                         int64_t n, int cnt, i32x4 p, i32x4 q) {
     f32x4 x, y;
@@ -147,11 +157,12 @@ __device__ __forceinline__ void finish4(const ProductArgs &a, const ChannelQuad<
     }
     if constexpr (OUT == Out::kStore) {
         if (a.slice > 0) {
-            store4(a.out, (blockIdx.y * a.M + m) * a.N + n, false, x, cnt);
+            store4<false>(a.out, (blockIdx.y * a.M + m) * a.N + n, false, x, cnt);
             return;
         }
         const int64_t row = m < a.split ? m : m - a.split;
-        if (row < a.limit) store4(m < a.split ? a.out : a.out2, row * a.ldo + n, a.out_bf16, x, cnt);
+        if (row < a.limit)
+            store4<PAST>(m < a.split ? a.out : a.out2, row * a.ldo + n, a.out_bf16, x, cnt);
         return;
     }
     if constexpr (sizeof(E) == 1) {
@@ -161,16 +172,16 @@ __device__ __forceinline__ void finish4(const ProductArgs &a, const ChannelQuad<
     }
     if (a.b0) x += of.b0;
     if constexpr (OUT == Out::kScale) {
-        store4(a.out, m * a.ldo + n, a.out_bf16, x, cnt);
+        store4<PAST>(a.out, m * a.ldo + n, a.out_bf16, x, cnt);
     } else {
         if (a.b1) y += of.b1;
         f32x4 h;
 #pragma unroll
         for (int i = 0; i < 4; ++i) h[i] = activate_by(a.act, x[i]) * y[i];
-        store4(a.out, m * a.ldo + n, a.out_bf16, h, cnt);
+        store4<PAST>(a.out, m * a.ldo + n, a.out_bf16, h, cnt);
         if (a.G) {
-            store4(a.G, m * a.ldp + n, false, x, cnt);
-            store4(a.U, m * a.ldp + n, false, y, cnt);
+            store4<PAST>(a.G, m * a.ldp + n, false, x, cnt);
+            store4<PAST>(a.U, m * a.ldp + n, false, y, cnt);
         }
     }
 }
@@ -318,7 +329,7 @@ __device__ __forceinline__ void wave_sync() {
 // through the wave's own LDS, so that consecutive lanes finish consecutive channels of a token.
 // m0, n0: the wave's first token and channel.
 constexpr int epilogue_bytes(int NN) { return kMF * (NN * kMF + 4) * 4; }
-template <class E, Out OUT, int NN, int NM, class Acc>
+template <class E, Out OUT, int NN, int NM, bool PAST = false, class Acc>
 __device__ __forceinline__ void epilogue(const ProductArgs &a, const Acc (&acc)[NN][NM], float *mine,
                                          int64_t m0, int64_t n0) {
     constexpr bool kDual = OUT == Out::kGated;
@@ -352,7 +363,7 @@ __device__ __forceinline__ void epilogue(const ProductArgs &a, const Acc (&acc)[
             const i32x4 x = *reinterpret_cast<const i32x4 *>(p);
             i32x4 y = {0, 0, 0, 0};
             if constexpr (kDual) y = *reinterpret_cast<const i32x4 *>(p + kMF);
-            if (m < a.M && cnt > 0) finish4<E, OUT>(a, of, m, n, cnt, x, y);
+            if (m < a.M && cnt > 0) finish4<E, OUT, PAST>(a, of, m, n, cnt, x, y);
         }
         wave_sync();
     }
