@@ -256,30 +256,49 @@ template <class T> __device__ __forceinline__ void load_some(const T *p, int64_t
     }
 }
 
-// out[c][r] = in[r][c] for r < R, c < C; out's rows are padded with zeros to `pad` columns.
-// blockIdx.z counts the matrices.
-template <class T> struct Transposes {
-    const T *in[2];
-    int64_t ldi[2];
-    T *out[2];
+// out[c][r] = in[r][c] for r < R, c < C; out's rows are padded with zeros to `pad` columns.  The
+// gradients' three matrices (both weights and the tokens) go in one launch: tiles from first[i] on
+// are matrix i's.
+struct Transposes {
+    const float *in[3];
+    float *out[3];
+    int64_t ldi[3], R[3], C[3], ldo[3], pad[3];
+    unsigned first[3];
+    int matrices;
+    unsigned tiles;
+    void add(const void *from, int64_t ldi_, int64_t R_, int64_t C_, float *to, int64_t ldo_, int64_t pad_) {
+        const int i = matrices++;
+        in[i] = static_cast<const float *>(from);
+        out[i] = to;
+        ldi[i] = ldi_;
+        R[i] = R_;
+        C[i] = C_;
+        ldo[i] = ldo_;
+        pad[i] = pad_;
+        first[i] = tiles;
+        tiles += unsigned((pad_ + kT - 1) / kT * ((C_ + kT - 1) / kT));
+    }
 };
-template <class T>
-__global__ __launch_bounds__(kThreads) void transpose_kernel(Transposes<T> of, int64_t R, int64_t C,
-                                                             int64_t ldo, int64_t pad) {
-    __shared__ TransposeTile<T> tile;
-    const T *in = blockIdx.z == 0 ? of.in[0] : of.in[1];
-    const int64_t ldi = blockIdx.z == 0 ? of.ldi[0] : of.ldi[1];
-    const int64_t r0 = int64_t(blockIdx.x) * kT, c0 = int64_t(blockIdx.y) * kT;
-    constexpr int per = kT / kV<T>;
+__global__ __launch_bounds__(kThreads) void transpose_kernel(Transposes of) {
+    __shared__ TransposeTile<float> tile;
+    int i = 0;
+#pragma unroll
+    for (int j = 1; j < 3; ++j)
+        if (j < of.matrices && blockIdx.x >= of.first[j]) i = j;
+    const float *in = of.in[i];
+    const int64_t ldi = of.ldi[i], R = of.R[i], C = of.C[i], pad = of.pad[i];
+    const unsigned id = blockIdx.x - of.first[i], across = unsigned((pad + kT - 1) / kT);
+    const int64_t r0 = int64_t(id % across) * kT, c0 = int64_t(id / across) * kT;
+    constexpr int V = kV<float>, per = kT / V;
 #pragma unroll
     for (int e = threadIdx.x; e < kT * per; e += kThreads) {
-        const int r = e / per, c = e % per * kV<T>;
-        T v[kV<T>];
+        const int r = e / per, c = e % per * V;
+        float v[V];
         load_some(in + (r0 + r) * ldi + c0 + c, r0 + r < R ? C - c0 - c : 0, v);
         tile.put(r, c, v);
     }
     __syncthreads();
-    tile.store(blockIdx.z == 0 ? of.out[0] : of.out[1], ldo, r0, c0, C, pad);
+    tile.store(of.out[i], of.ldo[i], r0, c0, C, pad);
 }
 
 // out[r][c] = in[r][c] for c < C, rows of `pad` elements (a multiple of 16 bytes) padded with zeros.
@@ -367,15 +386,28 @@ __global__ __launch_bounds__(kThreads) void gated_slope_kernel(
     }
 }
 
+// The sums of `blocks` rows of partial sums, 2 F each: kBiasCols columns to a workgroup, whose groups
+// of threads take every kBiasRows-th row and are added, in order, through LDS (a thread that walks all
+// rows of its column waits for memory at each: 16384 of them at the most tokens).
+constexpr int kBiasCols = 16, kBiasRows = kThreads / kBiasCols;
 template <class T>
 __global__ __launch_bounds__(kThreads) void bias_grad_kernel(const float *__restrict__ partial,
                                                              int64_t blocks, int64_t F,
                                                              T *__restrict__ dbg,
                                                              T *__restrict__ dbu) {
-    const int64_t f = int64_t(blockIdx.x) * kThreads + threadIdx.x;
-    if (f >= 2 * F) return;
+    __shared__ float sums[kBiasRows][kBiasCols + 1];
+    const int c = threadIdx.x % kBiasCols, y = threadIdx.x / kBiasCols;
+    const int64_t f = int64_t(blockIdx.x) * kBiasCols + c;
     float s = 0.0f;
-    for (int64_t b = 0; b < blocks; ++b) s += partial[b * 2 * F + f];
+    if (f < 2 * F) {
+#pragma unroll 8
+        for (int64_t b = y; b < blocks; b += kBiasRows) s += partial[b * 2 * F + f];
+    }
+    sums[y][c] = s;
+    __syncthreads();
+    if (y > 0 || f >= 2 * F) return;
+#pragma unroll
+    for (int r = 1; r < kBiasRows; ++r) s += sums[r][c];
     if (f < F) {
         if (dbg) dbg[f] = from_float<T>(s);
     } else if (dbu) {
@@ -394,13 +426,6 @@ __global__ __launch_bounds__(kThreads) void zero_rows_kernel(T *__restrict__ p, 
 }
 
 unsigned cover(int64_t n, int64_t tile) { return unsigned((n + tile - 1) / tile); }
-
-template <class T>
-void transpose(const Transposes<T> &of, unsigned matrices, int64_t R, int64_t C, int64_t ldo,
-               int64_t pad, void *stream) {
-    hipLaunchKernelGGL(transpose_kernel<T>, dim3(cover(pad, kT), cover(C, kT), matrices),
-                       dim3(kThreads), 0, as_stream(stream), of, R, C, ldo, pad);
-}
 
 // A matrix as a column operand: itself where its rows are whole 16-byte chunks on 16-byte boundaries,
 // else copied to `space` with rows of Kp elements.
@@ -487,9 +512,20 @@ void backward(const void *dH, int64_t lddh, const void *X, int64_t T_, int64_t l
                                F, D, l.Fp, Dt, l.Tp, partial);
         });
     if (dbg || dbu)
-        hipLaunchKernelGGL(bias_grad_kernel<TG>, dim3(cover(2 * F, kThreads)), dim3(kThreads), 0,
+        hipLaunchKernelGGL(bias_grad_kernel<TG>, dim3(cover(2 * F, kBiasCols)), dim3(kThreads), 0,
                            as_stream(stream), partial, int64_t(cover(T_, kT)), F,
                            static_cast<TG *>(dbg), static_cast<TG *>(dbu));
+    if constexpr (!columns) {
+        Transposes of{};
+        float *Wt = reinterpret_cast<float *>(w_space);
+        if (dX) {
+            of.add(W.Wg, W.ldg, F, K, Wt, 2 * l.Fp, l.Fp);
+            of.add(W.Wu, W.ldu, F, K, Wt + l.Fp, 2 * l.Fp, l.Fp);
+        }
+        if (dWg) of.add(X, ldx, T_, K, reinterpret_cast<float *>(x_space), l.Tp, l.Tp);
+        if (of.matrices && T_ > 0)
+            hipLaunchKernelGGL(transpose_kernel, dim3(of.tiles), dim3(kThreads), 0, as_stream(stream), of);
+    }
     ProductArgs a{};
     a.A = reinterpret_cast<const char *>(D);
     a.lda = 2 * l.Fp * kSize<T>;
@@ -510,11 +546,6 @@ void backward(const void *dH, int64_t lddh, const void *X, int64_t T_, int64_t l
             a.rows_k = int(F);
             a.half = int(l.Fp / 32);
         } else {
-            T *Wt = reinterpret_cast<T *>(w_space);
-            transpose<T>({{static_cast<const T *>(W.Wg), static_cast<const T *>(W.Wu)},
-                          {W.ldg, W.ldu},
-                          {Wt, Wt + l.Fp}},
-                         2, F, K, 2 * l.Fp, l.Fp, stream);
             a.B0 = w_space;
             a.ldb0 = a.lda;
         }
@@ -537,8 +568,6 @@ void backward(const void *dH, int64_t lddh, const void *X, int64_t T_, int64_t l
             a.M = 2 * l.Fp;
             a.split = l.Fp;
         } else {
-            transpose<T>({{static_cast<const T *>(X)}, {ldx}, {reinterpret_cast<T *>(x_space)}}, 1, T_, K,
-                         l.Tp, l.Tp, stream);
             a.A = reinterpret_cast<const char *>(Dt);
             a.B0 = x_space;
             a.lda = a.ldb0 = l.Tp * kSize<T>;

@@ -317,6 +317,22 @@ def test_gated_backward(T, K, F, dtype, grad, pad, shift):
     assert torch.equal(only[3], got[3]) and torch.equal(only[4], got[4]) and only[0] is None
 
 
+@pytest.mark.parametrize("T", [1, 63, 1024, 1025, 5000])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("F", [1, 37])
+def test_bias_gradients_of_many_tokens_are_exact(T, F, dtype):
+    """Whole numbers of at most 4 and relu: every partial sum is a whole number below 2^24."""
+    rng = np.random.default_rng(T + F)
+    x, wg, wu, dh, g, u = (torch.from_numpy(rng.integers(-2, 3, s).astype(np.float32)) for s in
+                           ((T, 3), (F, 3), (F, 3), (T, F), (T, F), (T, F)))
+    b = lambda t: t.to(TORCH[dtype]).to(DEV)  # noqa: E731
+    out = B.bsr_gated_backward(b(dh), b(x), b(wg), b(wu), g.to(DEV), u.to(DEV), act="relu", bias=True,
+                               need=(), grad_dtype=torch.float32)
+    dH, G, U = (t.double().numpy() for t in (dh, g, u))
+    assert np.array_equal(f64(out[3]), (dH * U * (G > 0)).sum(0))
+    assert np.array_equal(f64(out[4]), (dH * np.maximum(G, 0)).sum(0))
+
+
 @pytest.mark.parametrize("T,K,F", [(5, 7, 9), (64, 64, 64), (100, 130, 70), (260, 200, 300)])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_gated_integers_are_exact(T, K, F, dtype):
