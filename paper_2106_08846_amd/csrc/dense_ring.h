@@ -10,9 +10,9 @@
 // more and shorter ones for the small tiles.
 //
 // One workgroup of 256 x 256 outputs fills a CU: 8 waves of 128 x 64, 128 KB of LDS.  At 8192^3
-// (MI355X) it runs at 1.23-1.27 Pflop/s in bf16 and 2.3 Pop/s in int8, within 6% of the library
-// products on the same card; the matrix units are busy 68% of the cycles, at the 1.6 GHz that the
-// card's power leaves them.
+// (MI355X) it runs at 1.23-1.27 Pflop/s in bf16 and 2.4 Pop/s in int8, within 6% of the library
+// products on the same card; the matrix units are busy 60-68% of the cycles, at the 1.6-1.8 GHz that
+// the card's power leaves them.
 // COLS_A, COLS_B (bf16): the operand's rows lie along the outputs instead, k after k: an operand of a
 // gradient, as it is in memory.  A step is then 32 of its rows, cut to the tile's columns, and the
 // fragments are read from LDS with the transposing read (ds_read_b64_tr_b16), which gives a lane four
