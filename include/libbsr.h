@@ -537,7 +537,8 @@ typedef struct {
  *   a quarter of fp32's rounding, for operands of 2^-100 or more), otherwise by fp32 instructions: an
  *   infinite operand, or one from 2^128 (1 - 2^-9) on, may give NaN where fp32 arithmetic gives an
  *   infinity; it reaches the outputs of its token, or of its channel, only.
- * T = 0 is a no-op.  H, G and U must not overlap an input or each other.
+ * T = 0 is a no-op.  H, G and U must not overlap an input or each other; columns of one buffer, at the
+ * same pitch in bytes, do not (G and U side by side with ldp >= 2 F).
  * Errors: BSR_ERR_NULL (also: one of G and U without the other), BSR_ERR_SHAPE, BSR_ERR_ARG (unknown
  *   dtype or activation, overlap), BSR_ERR_DTYPE (BSR_I8), BSR_ERR_UNSUPPORTED (K, F or a pitch
  *   above 2^20, T above 2^24, T * F above 2^35), BSR_ERR_ARCH, BSR_ERR_HIP.

@@ -273,16 +273,30 @@ bsr_status check_attention(const float *Q, int64_t ldq, const float *K, int64_t 
 
 namespace {
 
-// A byte range that a call reads or writes.
+// Rows that a call reads or writes: the bytes from the first to the end of the last, the pitch and
+// the width of a row (an array without rows: its whole width).
 struct Span {
     const void *p;
-    int64_t bytes;
+    int64_t bytes, pitch, width;
 };
 
 // `rows` rows of `width` elements of `size` bytes at pitch ld: sizes that are checked before, except
 // the pitch of an array that is not given.
 Span span(const void *p, int64_t rows, int64_t ld, int64_t width, int64_t size) {
-    return Span{p, p && rows > 0 ? ((rows - 1) * ld + width) * size : 0};
+    if (!p || rows <= 0) return Span{p, 0, 0, 0};
+    return Span{p, ((rows - 1) * ld + width) * size, ld * size, width * size};
+}
+
+// Whether two arrays share bytes.  Columns of one buffer (the same pitch, such as G and U side by side)
+// lie within each other's range without sharing any: their rows stay apart where the distance of
+// their starts, modulo the pitch, leaves room for both.
+bool overlaps(const Span &a, const Span &b) {
+    if (!overlaps(a.p, a.bytes, b.p, b.bytes)) return false;
+    if (a.pitch != b.pitch) return true;
+    const uintptr_t pa = reinterpret_cast<uintptr_t>(a.p), pb = reinterpret_cast<uintptr_t>(b.p);
+    const int64_t apart = int64_t(pb > pa ? pb - pa : pa - pb) % a.pitch;
+    const int64_t first = pb > pa ? a.width : b.width, second = pb > pa ? b.width : a.width;
+    return apart < first || apart + second > a.pitch;
 }
 
 // No output overlaps an input or another output.
@@ -290,9 +304,9 @@ template <size_t I, size_t O>
 bool disjoint(const Span (&in)[I], const Span (&out)[O]) {
     for (size_t i = 0; i < O; ++i) {
         for (size_t j = 0; j < I; ++j)
-            if (overlaps(out[i].p, out[i].bytes, in[j].p, in[j].bytes)) return false;
+            if (overlaps(out[i], in[j])) return false;
         for (size_t j = i + 1; j < O; ++j)
-            if (overlaps(out[i].p, out[i].bytes, out[j].p, out[j].bytes)) return false;
+            if (overlaps(out[i], out[j])) return false;
     }
     return true;
 }
@@ -438,7 +452,7 @@ bsr_status check_gated_backward(const void *dH, int64_t lddh, const void *X, int
                        span(G, T, ldp, F, 4), span(U, T, ldp, F, 4)};
     const Span out[] = {span(dX, T, lddx, K, e), span(dWg, F, lddw, K, g),
                         span(dWu, F, lddw, K, g), span(dbg, 1, F, F, g), span(dbu, 1, F, F, g),
-                        Span{workspace, int64_t(need)}};
+                        span(workspace, 1, int64_t(need), int64_t(need), 1)};
     return disjoint(in, out) ? BSR_OK : BSR_ERR_ARG;
 }
 

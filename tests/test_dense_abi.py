@@ -18,11 +18,14 @@ def L():
     return bsr
 
 
-def check(status, expected):
+def check(call, args, expected):
+    """expected None: a call that passes the checks, which never reaches a GPU with these pointers."""
     if expected is None:
-        assert status in PAST_CHECKS
+        if torch.cuda.is_available():
+            pytest.skip("a GPU is there, and the pointers are not memory")
+        assert call(*args) in PAST_CHECKS
     else:
-        assert status == expected
+        assert call(*args) == expected
 
 
 @pytest.mark.parametrize("kw,status", [
@@ -37,7 +40,7 @@ def check(status, expected):
 def test_quantize_rows(L, kw, status):
     a = dict(X=X, dt=0, T=8, K=64, ldx=64, Q=WG, ldq=64, s=SX)
     a.update(kw)
-    check(L.library().bsr_quantize_rows(*a.values(), None), status)
+    check(L.library().bsr_quantize_rows, (*a.values(), None), status)
 
 
 @pytest.mark.parametrize("kw,status", [
@@ -57,7 +60,7 @@ def test_quantize_rows(L, kw, status):
 def test_matmul_i8(L, kw, status):
     a = dict(X=X, T=8, K=64, ldx=64, sx=SX, W=WG, N=32, ldw=64, sw=SG, b=BG, Y=H, dt=0, ldy=32)
     a.update(kw)
-    check(L.library().bsr_matmul_i8(*a.values(), None), status)
+    check(L.library().bsr_matmul_i8, (*a.values(), None), status)
 
 
 def block(L, kw, i8=False):
@@ -85,13 +88,18 @@ BLOCK_REFUSALS = [
     ({"H": X + 64}, ARG), ({"H": WG + 64}, ARG), ({"H": WU}, ARG), ({"H": BG}, ARG),
     ({"H": BU + 100}, ARG), ({"G": G, "U": G + 500}, ARG), ({"G": H + 256, "U": U}, ARG),
     ({"G": G, "U": X}, ARG),
+    # columns of one buffer: apart, one byte too near, wrapping into the next row, other pitches
+    ({"G": G, "U": G + 32 * 4, "ldp": 64}, None), ({"U": G, "G": G + 32 * 4, "ldp": 64}, None),
+    ({"G": G, "U": G + 32 * 4 - 1, "ldp": 64}, ARG), ({"G": G, "U": G + 32 * 4, "ldp": 63}, ARG),
+    ({"G": G, "U": G + 32 * 4 + 64 * 4, "ldp": 64}, None), ({"G": G, "U": G + 64 * 4, "ldp": 64}, ARG),
+    ({"G": G, "U": G + 33 * 4, "ldp": 64}, ARG), ({"H": X + 64 * 2, "ldx": 96, "ldh": 95}, ARG),
 ])
 def test_gated(L, kw, status):
     kw = dict(kw)
     m = block(L, kw)
     a = dict(X=X, T=8, ldx=64, m=ctypes.byref(m), H=H, ldh=32, G=None, U=None, ldp=32)
     a.update(kw)
-    check(L.library().bsr_gated(*a.values(), None), status)
+    check(L.library().bsr_gated, (*a.values(), None), status)
 
 
 def test_gated_without_a_block(L):
@@ -116,7 +124,7 @@ def test_gated_i8(L, kw, status):
     m = block(L, kw, i8=True)
     a = dict(X=X, T=8, ldx=64, sx=SX, m=ctypes.byref(m), H=H, hd=1, ldh=32)
     a.update(kw)
-    check(L.library().bsr_gated_i8(*a.values(), None), status)
+    check(L.library().bsr_gated_i8, (*a.values(), None), status)
 
 
 @pytest.mark.parametrize("kw,status", BLOCK_REFUSALS + [
@@ -133,6 +141,7 @@ def test_gated_i8(L, kw, status):
     ({"dX": X}, ARG), ({"dWg": WG}, ARG), ({"dWg": DWU + 100}, ARG), ({"dbg": DBU}, ARG),
     ({"dX": DH + 2}, ARG), ({"dWu": G}, ARG), ({"ws": DX}, ARG), ({"ws": U}, ARG),
     ({"dbu": DX + 10}, ARG),
+    ({"dWu": DWG + 64 * 2, "lddw": 128}, None), ({"dWu": DWG + 63 * 2, "lddw": 128}, ARG),
 ])
 def test_gated_backward(L, kw, status):
     kw = dict(kw)
@@ -140,7 +149,7 @@ def test_gated_backward(L, kw, status):
     a = dict(dH=DH, lddh=32, X=X, T=8, ldx=64, m=ctypes.byref(m), G=G, U=U, ldp=32, dX=DX, lddx=64,
              dWg=DWG, dWu=DWU, lddw=64, dbg=DBG, dbu=DBU, gd=1, ws=WS, wsb=MB)
     a.update(kw)
-    check(L.library().bsr_gated_backward(*a.values(), None), status)
+    check(L.library().bsr_gated_backward, (*a.values(), None), status)
 
 
 def test_workspace_bytes(L):

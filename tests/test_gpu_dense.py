@@ -479,6 +479,27 @@ def _step(x, wg, wu, dh, ws):
     return [H, *grads, h8, y8]
 
 
+@pytest.mark.parametrize("T,K,F", [(3, 40, 24), (70, 33, 65), (150, 64, 128)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_arrays_side_by_side_in_one_buffer(T, K, F, dtype):
+    """X beside H, G beside U, dWg beside dWu and dH beside dX, as columns of one buffer each, give what
+    arrays of their own give."""
+    rng, x, wg, wu, _, _ = block_inputs(T, K, F, dtype, False)
+    dt = TORCH[dtype]
+    x, wg, wu, dh = (t.to(dt).to(DEV) for t in (x, wg, wu, rand(rng, T, F, dtype=dtype)))
+    want = B.bsr_gated(x, wg, wu, save=True)
+    want += B.bsr_gated_backward(dh, x, wg, wu, want[1], want[2])[:3]
+    xh, gu = torch.zeros(T, K + F, dtype=dt, device=DEV), torch.zeros(T, 2 * F, device=DEV)
+    dw, dd = torch.zeros(F, 2 * K, dtype=dt, device=DEV), torch.zeros(T, F + K, dtype=dt, device=DEV)
+    xh[:, :K] = x
+    dd[:, :F] = dh
+    got = B.bsr_gated(xh[:, :K], wg, wu, H=xh[:, K:], G=gu[:, :F], U=gu[:, F:])
+    got += B.bsr_gated_backward(dd[:, :F], xh[:, :K], wg, wu, gu[:, :F], gu[:, F:], dX=dd[:, F:],
+                                dWg=dw[:, :K], dWu=dw[:, K:])[:3]
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    assert torch.equal(xh[:, :K], x) and torch.equal(dd[:, :F], dh)
+
+
 @pytest.mark.parametrize("T", [3, 150])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_captured_and_replayed(T, dtype):
