@@ -81,7 +81,7 @@ template <class E, int NT, bool ALIGNED, Out OUT> struct RowsKernel {
         const int cnt = a.N - n < 4 ? int(a.N - n) : 4;
         if (m < a.M && cnt > 0)
             finish4<E, OUT, false>(a, ChannelQuad<E, OUT>(a, n, cnt), m, n, cnt,
-                            __builtin_bit_cast(i32x4, sum[0]), __builtin_bit_cast(i32x4, sum[1]));
+                                   __builtin_bit_cast(i32x4, sum[0]), __builtin_bit_cast(i32x4, sum[1]));
     }
 };
 
