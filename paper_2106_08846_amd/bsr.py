@@ -993,7 +993,8 @@ def bsr_gated_backward(dH: torch.Tensor, X: torch.Tensor, Wg: torch.Tensor, Wu: 
 
     `need` names what is wanted of "X" (dX) and "W" (dWg and dWu), `bias` whether the bias gradients
     are; what is not wanted is None.  Weight and bias gradients are of grad_dtype (default: X's type;
-    float32 suits bsr_iht_update and fp32 master weights), allocated here unless given.  `workspace`
+    float32 suits bsr_iht_update and fp32 master weights, and keeps 16 bits of a bf16 block's dG and dU
+    where bfloat16 keeps 8, at twice the weight gradients' time), allocated here unless given.  `workspace`
     is a uint8 device tensor of bsr_gated_workspace_bytes, allocated here when None; calls that may
     overlap in time need one each."""
     ldx, block = _gated_block(X, Wg, Wu, None, None, None, None, act, _DATA_DTYPES)

@@ -101,7 +101,7 @@ struct GatedWorkspace {
     int64_t Kp;              // bf16: K rounded up to whole 16-byte chunks
     int64_t Tp;              // fp32: T rounded up to whole 16-byte chunks
     size_t grad_offset;      // [T][2 Fp]: dG | dU, of the block's dtype
-    size_t gradt_offset;     // fp32: [2 F][Tp], its transpose
+    size_t gradt_offset;     // fp32: [2 F][Tp], its transpose; bf16: [T][2 Fp], what its rounding dropped
     size_t x_offset;         // bf16: [T][Kp], a copy of an unaligned X; fp32: [K][Tp], X's transpose
     size_t w_offset;         // bf16: [2][F][Kp], copies; fp32: [K][2 Fp], the weights' transposes
     size_t partial_offset;   // fp32 [row blocks][2 F]: partial bias gradients

@@ -318,17 +318,33 @@ __global__ __launch_bounds__(kThreads) void copy_rows_kernel(const T *__restrict
 }
 
 // D[t][f] = dH U act'(G), D[t][Fp + f] = dH act(G), zeros up to Fp, and the sums of their columns over
-// the tile's tokens; BOTH: also the transpose Dt[f][t], Dt[F + f][t].  Memory bound: 16 bytes of D (4
-// or 8 hidden units of a token) per thread and pass.  6144 tokens of 8192 hidden units in bf16 (700
-// MB) take 160 us on MI355X, 4.4 TB/s; reading G and U past the caches made no difference, and tiles of 256
-// hidden units gained 6 us there and cost 8 on a step of 100 tokens (53 us).
-template <class T, int ACT, bool BOTH>
+// the tile's tokens.  Into Dt goes, as ALSO says, the transpose Dt[f][t], Dt[F + f][t], or, in D's layout,
+// what the rounding of D to bf16 dropped, itself rounded to bf16 (at most 2^-16 of a value is left out
+// then; a value that rounds to infinity drops nothing).
+//
+// bf16: D is rounded because it is an operand of the bf16 instructions, an error of at most 2^-8 a term,
+// of the size of a bf16 gradient's own rounding (6144 x 2048 x 8192: gradients 0.235% off, 0.166% with
+// D in fp32).  fp32 gradients have no such rounding, so they take the dropped part too: the weights'
+// product takes 700 us instead of 343 there, the slopes 180 instead of 160, the whole step 1.28-1.30
+// times as long.
+//
+// Memory bound: 16 bytes of D (4 or 8 hidden units of a token) per thread and pass.  6144 tokens of 8192
+// hidden units in bf16 (700 MB) take 160 us on MI355X, 4.4 TB/s; reading G and U past the caches made
+// no difference, and tiles of 256 hidden units gained 6 us there and cost 8 on a step of 100 tokens (53
+// us).
+enum class Also { kNothing, kTransposed, kDropped };
+__device__ __forceinline__ bf16 dropped(float v, bf16 kept) {
+    const float k = to_float(kept);
+    return to_bf16(fabsf(k) < INFINITY ? v - k : 0.0f);
+}
+template <class T, int ACT, Also ALSO>
 __global__ __launch_bounds__(kThreads) void gated_slope_kernel(
     const T *__restrict__ dH, int64_t lddh, const float *__restrict__ G,
     const float *__restrict__ U, int64_t ldp, int64_t T_, int64_t F, T *__restrict__ D, int64_t Fp,
     T *__restrict__ Dt, int64_t Tp, float *__restrict__ partial) {
     constexpr int V = kV<T>, per = kT / V, kRows = kThreads / per;
-    __shared__ typename std::conditional<BOTH, TransposeTile<T>, char>::type tg, tu;
+    constexpr bool kBoth = ALSO == Also::kTransposed;
+    __shared__ typename std::conditional<kBoth, TransposeTile<T>, char>::type tg, tu;
     __shared__ float sums[2][kRows][kT + 1];
     const int64_t t0 = int64_t(blockIdx.x) * kT, f0 = int64_t(blockIdx.y) * kT;
     const int y = threadIdx.x / per, x = threadIdx.x % per * V;
@@ -337,7 +353,7 @@ __global__ __launch_bounds__(kThreads) void gated_slope_kernel(
 #pragma unroll
     for (int i = y; i < kT; i += kRows) {
         const int64_t t = t0 + i, n = t < T_ ? F - f : 0;
-        T dh[V], dg[V], du[V];
+        T dh[V], dg[V], du[V], lg[V], lu[V];
         float g[V], u[V];
         load_some(dH + t * lddh + f, n, dh);
         if (n >= V) {
@@ -360,14 +376,22 @@ __global__ __launch_bounds__(kThreads) void gated_slope_kernel(
             pu[j] += vu;
             dg[j] = from_float<T>(vg);
             du[j] = from_float<T>(vu);
+            if constexpr (ALSO == Also::kDropped) {
+                lg[j] = dropped(vg, dg[j]);
+                lu[j] = dropped(vu, du[j]);
+            }
         }
-        if constexpr (BOTH) {
+        if constexpr (kBoth) {
             tg.put(i, x, dg);
             tu.put(i, x, du);
         }
         if (t < T_ && f < Fp) {
             __builtin_memcpy(D + t * 2 * Fp + f, dg, 16);
             __builtin_memcpy(D + t * 2 * Fp + Fp + f, du, 16);
+            if constexpr (ALSO == Also::kDropped) {
+                __builtin_memcpy(Dt + t * 2 * Fp + f, lg, 16);
+                __builtin_memcpy(Dt + t * 2 * Fp + Fp + f, lu, 16);
+            }
         }
     }
 #pragma unroll
@@ -376,7 +400,7 @@ __global__ __launch_bounds__(kThreads) void gated_slope_kernel(
         sums[1][y][x + j] = pu[j];
     }
     __syncthreads();
-    if constexpr (BOTH) {
+    if constexpr (kBoth) {
         tg.store(Dt, Tp, t0, f0, F, Tp);
         tu.store(Dt + F * Tp, Tp, t0, f0, F, Tp);
     }
@@ -507,12 +531,16 @@ void backward(const void *dH, int64_t lddh, const void *X, int64_t T_, int64_t l
     char *x_space = base + l.x_offset, *w_space = base + l.w_offset;
     float *partial = reinterpret_cast<float *>(base + l.partial_offset);
     float *sums = reinterpret_cast<float *>(base + l.slice_offset);
+    constexpr bool dropped = columns && std::is_same<TG, float>::value;     // of the weights' product
     if (T_ > 0)
         with_act(W.act, [&](auto act) {
-            hipLaunchKernelGGL((gated_slope_kernel<T, decltype(act)::value, !columns>),
-                               dim3(cover(columns ? T_ : l.Tp, kT), cover(l.Fp, kT)), dim3(kThreads),
-                               0, as_stream(stream), static_cast<const T *>(dH), lddh, G, U, ldp, T_,
-                               F, D, l.Fp, Dt, l.Tp, partial);
+            constexpr Also plain = columns ? Also::kNothing : Also::kTransposed;
+            auto kernel = gated_slope_kernel<T, decltype(act)::value, plain>;
+            if constexpr (dropped)
+                if (dWg) kernel = gated_slope_kernel<T, decltype(act)::value, Also::kDropped>;
+            hipLaunchKernelGGL(kernel, dim3(cover(columns ? T_ : l.Tp, kT), cover(l.Fp, kT)),
+                               dim3(kThreads), 0, as_stream(stream), static_cast<const T *>(dH), lddh,
+                               G, U, ldp, T_, F, D, l.Fp, Dt, l.Tp, partial);
         });
     if (dbg || dbu)
         hipLaunchKernelGGL(bias_grad_kernel<TG>, dim3(cover(2 * F, kBiasCols)), dim3(kThreads), 0,
@@ -554,7 +582,7 @@ void backward(const void *dH, int64_t lddh, const void *X, int64_t T_, int64_t l
         }
         gradient_product<T, T, false>(a, l.x_slices, sums, stream);
     }
-    if (dWg && T_ > 0) {          // D^T (2 F x T) times X
+    if (dWg && T_ > 0) {          // D^T (2 F x T) times X; with what D's rounding dropped, twice the terms
         a.N = K;
         a.out = dWg;
         a.out2 = dWu;
@@ -567,7 +595,8 @@ void backward(const void *dH, int64_t lddh, const void *X, int64_t T_, int64_t l
             a.ldb0 = a.ldb1 = x.ld;
             a.rows_k = int(T_);
             a.half = cover(T_, 32);
-            a.Kb = a.half * 64;
+            a.Kb = (dropped ? 2 : 1) * a.half * 64;
+            a.A1 = dropped ? reinterpret_cast<const char *>(Dt) : a.A;
             a.M = 2 * l.Fp;
             a.split = l.Fp;
         } else {

@@ -154,7 +154,7 @@ struct RingKernel {
             ob[i] = r < sb.rows ? unsigned(r) * unsigned(sb.pitch) + c * kChunk : kOut;
         }
         // Columns: the operand's matrices from the tile's first column on.
-        const ColumnSource ca{{a.A + rows.m0 * 2, a.A + rows.m0 * 2}, {a.lda, a.lda}, a.rows_k, a.half,
+        const ColumnSource ca{{a.A + rows.m0 * 2, a.A1 + rows.m0 * 2}, {a.lda, a.lda}, a.rows_k, a.half,
                               unsigned((a.M - rows.m0 + 7) / 8) * kChunk};
         const ColumnSource cb{{a.B0 + rows.n0 * 2, a.B1 + rows.n0 * 2}, {a.ldb0, a.ldb1}, a.rows_k,
                               a.half, unsigned((a.N - rows.n0 + 7) / 8) * kChunk};

@@ -410,7 +410,7 @@ GatedWorkspace gated_workspace_layout(int64_t T, int64_t K, int64_t F, int32_t d
     w.Tp = up(T, per);
     w.grad_offset = 0;
     w.gradt_offset = align256(size_t(T * 2 * w.Fp * e));
-    w.x_offset = align256(w.gradt_offset + (bf16 ? 0 : size_t(2 * F * w.Tp * e)));
+    w.x_offset = align256(w.gradt_offset + size_t((bf16 ? T * 2 * w.Fp : 2 * F * w.Tp) * e));
     w.w_offset = align256(w.x_offset + size_t(bf16 ? T * w.Kp * e : K * w.Tp * e));
     w.partial_offset = align256(w.w_offset + size_t(bf16 ? 2 * F * w.Kp * e : K * 2 * w.Fp * e));
     w.slice_offset = align256(w.partial_offset + size_t(blocks * 2 * F * 4));
