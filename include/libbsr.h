@@ -534,9 +534,10 @@ typedef struct {
  *   pre-activations).
  * bf16 products are exact in fp32.  fp32 products of more than a few tokens are formed from three bf16
  *   pieces of each operand (six exact cross terms; what is left out is below 2^-25.9 of the product,
- *   a quarter of fp32's rounding, for operands of 2^-100 or more), otherwise by fp32 instructions: an
- *   infinite operand, or one from 2^128 (1 - 2^-9) on, may give NaN where fp32 arithmetic gives an
- *   infinity; it reaches the outputs of its token, or of its channel, only.
+ *   a quarter of fp32's rounding), otherwise by fp32 instructions.  The pieces hold every finite operand;
+ *   of one below 2^-100, up to 2^-125 may be lost.  Where the pieces differ from fp32 arithmetic: an
+ *   infinite operand may give NaN instead of an infinity (in the outputs of its token, or of its channel,
+ *   only), and a sum with a term within 2^-8 of the largest finite value may overflow.
  * T = 0 is a no-op.  H, G and U must not overlap an input or each other; columns of one buffer, at the
  * same pitch in bytes, do not (G and U side by side with ldp >= 2 F).
  * Errors: BSR_ERR_NULL (also: one of G and U without the other), BSR_ERR_SHAPE, BSR_ERR_ARG (unknown

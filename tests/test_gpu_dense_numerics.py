@@ -52,3 +52,89 @@ def test_fp32_weight_gradients_of_a_bf16_block(T, K, F, act):
     for t, name, d in ((got[1], "dWg", f64(dh) * f64(u) * da), (got[2], "dWu", f64(dh) * a)):
         v, e = want[name]                   # counts 6.1 roundings a token, and of dG in fp32
         within(t, v, e + 1.01 * 2.0 ** -16 * np.abs(d).T @ np.abs(f64(x)), name)
+
+
+# --- fp32 operands at the ends of the range ---------------------------------------------------------
+
+FLT_MAX = 3.4028234663852886e38
+# Token counts and widths on both sides of the few-token kernel's rule, in both tile sizes.
+ENDS = [(1, 90), (32, 2000), (96, 2000), (200, 2000), (777, 2048)]
+
+
+@pytest.mark.parametrize("T,F", ENDS)
+@pytest.mark.parametrize("K", [100, 101])
+def test_fp32_operands_near_the_largest_finite_one(T, F, K):
+    """Values from 2^128 (1 - 2^-9) on, which one bf16 piece cannot hold, times small ones."""
+    rng = np.random.default_rng(T + F + K)
+    x, wg, wu = rand(rng, T, K), rand(rng, F, K), rand(rng, F, K)
+    x[:, 3] *= 1e-10                        # times 3.4e38
+    wg[5, 3], wu[F - 1, 3], wg[7, 3] = 3.4e38, -FLT_MAX, 2.0 ** 127 * (2 - 2.0 ** -7)
+    x[:, 20] = 0.0
+    wg[8, 20], wu[9, 20] = FLT_MAX, -3.4e38
+    x[T // 2, 90], x[T - 1, K - 1] = -3.4e38, FLT_MAX
+    wg[:, 90] *= 1e-12
+    wu[:, 90] *= 1e-30
+    wg[:, K - 1] *= 1e-25
+    wu[:, K - 1] = 0.0
+    H, G, U = B.bsr_gated(x.to(DEV), wg.to(DEV), wu.to(DEV), act="relu", save=True)
+    with np.errstate(all="ignore"):
+        wh, g, u, eh, eg, eu = D.gated(f64(x), f64(wg), f64(wu), name="relu")
+    within(G, g, eg, "G")
+    within(U, u, eu, "U")
+    fits = np.abs(wh) + eh < 1e38
+    assert fits.mean() > 0.9
+    got = f64(H)
+    assert np.all(np.abs(got - wh)[fits] <= eh[fits])
+    # the outputs without such an operand are those of a call without any
+    for w, channels in ((wg, (5, 7, 8)), (wu, (9, F - 1))):
+        w[list(channels)] = 0.0
+    x[T // 2] = x[T - 1] = 0.0
+    H0, G0, U0 = B.bsr_gated(x.to(DEV), wg.to(DEV), wu.to(DEV), act="relu", save=True)
+    t = torch.ones(T, dtype=torch.bool, device=DEV)
+    t[[T // 2, T - 1]] = False
+    f = torch.ones(F, dtype=torch.bool, device=DEV)
+    f[[5, 7, 8, 9, F - 1]] = False
+    for a, b in ((H, H0), (G, G0), (U, U0)):
+        assert torch.equal(a[t][:, f], b[t][:, f])
+
+
+@pytest.mark.parametrize("T,K,F", [(1, 90, 40), (70, 100, 900), (70, 2040, 1020), (600, 800, 700)])
+def test_fp32_gradients_of_operands_near_the_largest_finite_one(T, K, F):
+    rng = np.random.default_rng(T + F + K)
+    x, wg, wu, dh = rand(rng, T, K), rand(rng, F, K), rand(rng, F, K), rand(rng, T, F, sigma=1e-3)
+    g, u = rand(rng, T, F), rand(rng, T, F)
+    dh[:, 7] *= 1e-15                       # times the weights of channel 7, in dX
+    wg[7, 11], wu[7, 12] = 3.4e38, -FLT_MAX
+    x[T // 2, 30] = -FLT_MAX                # times dG and dU of one token, in dWg and dWu
+    dh[T // 2] *= 1e-20
+    got = B.bsr_gated_backward(*(t.to(DEV) for t in (dh, x, wg, wu, g, u)), act="gelu")
+    want = D.gated_backward(*(f64(t) for t in (dh, x, wg, wu, g, u)), "gelu")
+    # dG and dU of the small token and channel 7 are near 1e-38.  An operand below 2^-100 may lose 2^-125
+    # (dG and dU are themselves rounded to 2^-150 there), which the other operand multiplies.
+    a, da = D.act("gelu", f64(g))
+    dg, du, X, Wg, Wu = f64(dh) * f64(u) * da, f64(dh) * a, f64(x), f64(wg), f64(wu)
+
+    def lost(p, q):
+        return 2.0 ** -125 * ((np.abs(p) < 2.0 ** -100) @ np.abs(q))
+
+    more = {"dX": lost(dg, Wg) + lost(du, Wu), "dWg": lost(dg.T, X), "dWu": lost(du.T, X)}
+    for name, t in zip(("dX", "dWg", "dWu"), got):
+        v, e = want[name]
+        within(t, v, e + more[name], name)
+
+
+@pytest.mark.parametrize("T,F", ENDS)
+@pytest.mark.parametrize("small", [2.0 ** -98, 2.0 ** -104, 2.0 ** -112, 2.0 ** -124])
+def test_fp32_operands_near_the_smallest_ones(T, F, small):
+    """Pieces below 2^-126 may be lost, at most 2^-125 of an operand in all: small tokens times large
+    weights, and the other way round."""
+    K = 96
+    rng = np.random.default_rng(T + F)
+    for sx, sw in ((small, 2.0 ** 50), (2.0 ** 50, small)):
+        x, wg, wu = rand(rng, T, K, sigma=sx), rand(rng, F, K, sigma=sw), rand(rng, F, K, sigma=sw)
+        _, G, U = B.bsr_gated(x.to(DEV), wg.to(DEV), wu.to(DEV), act="relu", save=True)
+        _, g, u, _, eg, eu = D.gated(f64(x), f64(wg), f64(wu), name="relu")
+        for got, want, e, w in ((G, g, eg, wg), (U, u, eu, wu)):
+            operand = w if sx == small else x
+            size = np.abs(f64(operand)).sum(1)
+            within(got, want, e + 2.0 ** -125 * (size[None, :] if sx == small else size[:, None]), "small")
