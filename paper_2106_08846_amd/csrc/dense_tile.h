@@ -142,10 +142,12 @@ template <class E, Out OUT> struct ChannelQuad {
 };
 
 // Four outputs of token m from channel n on (`cnt` of them exist): `p`, and for kGated `q`, hold
-// the products (int8: as integers).
+// the products (int8: as integers).  Every operation rounds, as the 8-bit product is defined: nothing is
+// fused, so that the results do not depend on the kernel.
 template <class E, Out OUT, bool PAST>
 __device__ __forceinline__ void finish4(const ProductArgs &a, const ChannelQuad<E, OUT> &of, int64_t m,
                                         int64_t n, int cnt, i32x4 p, i32x4 q) {
+#pragma clang fp contract(off)
     f32x4 x, y;
     if constexpr (sizeof(E) == 1) {
 #pragma unroll

@@ -6,6 +6,7 @@ import torch
 
 from oracle import dense_oracle as D
 from paper_2106_08846_amd import bsr as B
+from tests.gpu_common import host
 from tests.test_gpu_dense import DEV, TORCH, f64, frame, held, rand, within
 
 pytestmark = pytest.mark.gpu
@@ -138,3 +139,44 @@ def test_fp32_operands_near_the_smallest_ones(T, F, small):
             operand = w if sx == small else x
             size = np.abs(f64(operand)).sum(1)
             within(got, want, e + 2.0 ** -125 * (size[None, :] if sx == small else size[:, None]), "small")
+
+
+# --- defined roundings ---------------------------------------------------------------------------
+
+# Few-token kernel (one token, one round), ring tiles and tiles of unaligned rows.
+I8_SIZES = [(1, 100, 1000), (1, 100, 1001), (16, 257, 256), (30, 257, 255), (33, 6000, 64), (33, 6000, 65),
+            (300, 513, 96), (300, 513, 97), (1100, 1300, 192), (1100, 1300, 191), (4000, 2900, 64),
+            (4000, 2900, 66)]
+
+
+def scaled(xq, sx, wq, sw, bias):
+    """The definition in fp32, one operation after the other."""
+    y = (xq.astype(np.int64) @ wq.astype(np.int64).T).astype(np.float32)
+    return ((y * sx[:, None]) * sw[None, :]) + bias[None, :]
+
+
+@pytest.mark.parametrize("T,N,K", I8_SIZES)
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_matmul_i8_rounds_as_defined(T, N, K, out):
+    rng = np.random.default_rng(T + N + K)
+    xq, wq = (rng.integers(-128, 128, s).astype(np.int8) for s in ((T, K), (N, K)))
+    sx, sw = (rng.uniform(0.001, 0.1, n).astype(np.float32) for n in (T, N))
+    bias = rng.standard_normal(N).astype(np.float32)
+    y = B.bsr_matmul_i8(*(torch.from_numpy(a).to(DEV) for a in (xq, sx, wq, sw, bias)),
+                        out_dtype=TORCH[out])
+    want = torch.from_numpy(scaled(xq, sx, wq, sw, bias)).to(TORCH[out])
+    assert torch.equal(y.cpu(), want)
+
+
+@pytest.mark.parametrize("T,F,K", [(t, n // 2, k) for t, n, k in I8_SIZES])
+def test_gated_i8_rounds_as_defined(T, F, K):
+    """With relu everything after the integer sums is a defined fp32 operation."""
+    rng = np.random.default_rng(T + F + K)
+    xq, gq, uq = (rng.integers(-127, 128, s).astype(np.int8) for s in ((T, K), (F, K), (F, K)))
+    sx, sg, su = (rng.uniform(0.001, 0.1, n).astype(np.float32) for n in (T, F, F))
+    bg, bu = (rng.standard_normal(F).astype(np.float32) for _ in range(2))
+    t = lambda a: torch.from_numpy(a).to(DEV)  # noqa: E731
+    h = B.bsr_gated_i8(t(xq), t(sx), t(gq), t(sg), t(uq), t(su), t(bg), t(bu), act="relu",
+                       out_dtype=torch.float32)
+    want = np.maximum(scaled(xq, sx, gq, sg, bg), np.float32(0)) * scaled(xq, sx, uq, su, bu)
+    assert np.array_equal(host(h), want)
