@@ -35,8 +35,9 @@ __device__ __forceinline__ float fast_exp(float x) {
     return fmaf(e, r * 0.693147182464599609375f, e);
 }
 
-// 1 / (1 + exp(-z)), to about 4 ulp for z > -87, below 2^-126 from there on.  The hardware's exponential and reciprocal (1 ulp
-// each): with expf and a division the epilogue of a 256 x 256 tile took a tenth of the tile's time.
+// 1 / (1 + exp(-z)), to about 4 ulp for z > -87.3, where it is 2^-126, and 0 below: the reciprocal gives
+// nothing smaller, so that the largest -g times it is 0 too.  The hardware's exponential and reciprocal (1
+// ulp each): with expf and a division the epilogue of a 256 x 256 tile took a tenth of the tile's time.
 __device__ __forceinline__ float sigmoid(float z) {
     return __builtin_amdgcn_rcpf(1.0f + fast_exp(__builtin_amdgcn_fmed3f(-z, -88.0f, 88.0f)));
 }
@@ -70,7 +71,9 @@ template <int ACT> __device__ __forceinline__ void activate_slope(float g, float
     } else if constexpr (ACT == BSR_ACT_GELU_TANH) {
         const float p = sigmoid(kTwoSqrt2OverPi * g * (1.0f + kGeluCubic * g * g));
         a = g * p;
-        da = p + g * p * (1.0f - p) * kTwoSqrt2OverPi * (1.0f + 3.0f * kGeluCubic * g * g);
+        // g^2 held below 10^4, where p (1 - p) is 0 from |g| = 11 on: 0 times an infinite square is NaN
+        const float gg = fminf(g * g, 1e4f);
+        da = p + g * p * (1.0f - p) * kTwoSqrt2OverPi * (1.0f + 3.0f * kGeluCubic * gg);
     } else {
         a = g <= 0.0f ? 0.0f : g;
         da = g > 0.0f ? 1.0f : (g <= 0.0f ? 0.0f : g);

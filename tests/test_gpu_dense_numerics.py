@@ -3,6 +3,7 @@ saturated activations, gradients kept in fp32, and results whose every rounding 
 import numpy as np
 import pytest
 import torch
+from scipy.special import erfc, expit
 
 from oracle import dense_oracle as D
 from paper_2106_08846_amd import bsr as B
@@ -139,6 +140,77 @@ def test_fp32_operands_near_the_smallest_ones(T, F, small):
             operand = w if sx == small else x
             size = np.abs(f64(operand)).sum(1)
             within(got, want, e + 2.0 ** -125 * (size[None, :] if sx == small else size[:, None]), "small")
+
+
+# --- saturated activations -------------------------------------------------------------------------
+
+def wide_range():
+    big = [16.7, 17.5, 30.0, 60.0, 86.5, 87.0, 87.25, 87.5, 88.0, 88.5, 89.0, 104.0, 1e3, 1e4, 1e10, 1e19,
+           1.9e19, 1e20, 1e30, 3e38]
+    small = [1e-38, 1e-30, 1e-10, 1e-3, 0.1, 1.0, 3.0, 5.5, 9.0, 10.5, 12.0, 13.5, 14.5]
+    return torch.tensor([s * v for v in big + small for s in (1.0, -1.0)] + [0.0], dtype=torch.float32)
+
+
+def act64(name, g):
+    """act(g), its slope and the exponent of its negative tail, in forms that do not cancel."""
+    with np.errstate(all="ignore"):
+        if name == "silu":
+            p = expit(g)
+            return g * p, p * (1 + g * expit(-g)), np.zeros_like(g)
+        if name == "gelu":
+            p = 0.5 * erfc(-g / np.sqrt(2.0))
+            return g * p, p + g * np.exp(-0.5 * g * g) / np.sqrt(2 * np.pi), g * g
+        if name == "gelu_tanh":
+            c = np.sqrt(2.0 / np.pi)
+            z = c * g * (1 + 0.044715 * g * g)
+            p, q = expit(2 * z), expit(-2 * z)
+            slope = np.where(p * q == 0, p, p + g * p * q * 2 * c * (1 + 3 * 0.044715 * g * g))
+            return g * p, slope, 2 * np.abs(z)
+        return np.maximum(g, 0), np.where(g > 0, 1.0, 0.0), np.zeros_like(g)
+
+
+# What an activation may be off by where its probability lies below 2^-126, for |g| < 2^8; farther out the
+# exact value is below 2^-200.
+TAIL = 2.0 ** -118
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh", "relu"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_activations_far_out(act, dtype):
+    """A relative error of 16 roundings and of the rounded argument of the tail's exponential (4 roundings
+    of up to 200, beyond which the tail is below 2^-126)."""
+    g = wide_range().to(TORCH[dtype])
+    n = len(g)
+    x = torch.zeros(n, 128, dtype=TORCH[dtype])
+    x[:, :n] = torch.eye(n)
+    wg = torch.zeros(24, 128, dtype=TORCH[dtype])
+    wg[:, :n] = g
+    wu = torch.full((24, 128), 0.75, dtype=TORCH[dtype])
+    H, G, U = B.bsr_gated(x.to(DEV), wg.to(DEV), wu.to(DEV), act=act, save=True)
+    v = f64(g)[:, None] * np.ones((1, 24))
+    assert np.array_equal(f64(G), v) and torch.all(U == 0.75)
+    a, _, zeta = act64(act, v)
+    want = 0.75 * a
+    e = D.U32 * np.abs(want) * (20 + 4 * np.minimum(zeta, 200.0)) + TAIL
+    within(H, want, e + D.U_OUT[dtype] * (np.abs(want) + e) * 1.0001, act)
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh", "relu"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_slopes_far_out(act, dtype):
+    """One token with dH = U = 1: the bias gradients are the slopes and the activations.  A slope's
+    summands, of at most 1 + |g| while it is neither 0 nor 1 (|g| < 20), are off by 32 roundings."""
+    g = wide_range()
+    F = len(g)
+    one = torch.ones(1, F, device=DEV)
+    dt = TORCH[dtype]
+    zero = torch.zeros(F, 8, dtype=dt, device=DEV)
+    out = B.bsr_gated_backward(one.to(dt), torch.ones(1, 8, dtype=dt, device=DEV), zero, zero,
+                               g[None].to(DEV), one, act=act, bias=True, grad_dtype=torch.float32)
+    a, da, zeta = act64(act, f64(g))
+    within(out[3], da, 32 * D.U32 * (1 + np.minimum(np.abs(f64(g)), 20.0)), "slope")
+    within(out[4], a, D.U32 * np.abs(a) * (20 + 4 * np.minimum(zeta, 200.0)) + TAIL, "activation")
+    assert all(torch.isfinite(t).all() for t in out)
 
 
 # --- defined roundings ---------------------------------------------------------------------------
