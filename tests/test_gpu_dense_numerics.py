@@ -252,3 +252,53 @@ def test_gated_i8_rounds_as_defined(T, F, K):
                        out_dtype=torch.float32)
     want = np.maximum(scaled(xq, sx, gq, sg, bg), np.float32(0)) * scaled(xq, sx, uq, su, bu)
     assert np.array_equal(host(h), want)
+
+
+# --- offsets past 32 bits --------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gradients_past_32_bits_of_offset(dtype):
+    """Every matrix of a backward call that has a pitch, in turn, with rows that start more than 2^32
+    bytes into it; all rows differ, so that one read or written 2^31 or 2^32 bytes off shows."""
+    if torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("needs 60 GB")
+    pitch, T, K = 1 << 20, 2200, 40
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(3)
+    dt = TORCH[dtype]
+
+    def ints(n, *shape):
+        return torch.randint(-n, n + 1, shape, device=DEV, generator=gen).double()
+
+    def far(t, dtype):
+        view = torch.empty(t.shape[0], pitch, dtype=dtype, device=DEV)[:, :t.shape[1]]
+        view.copy_(t)
+        return view
+
+    # tokens far apart: X, dH, dX (bf16 2 MiB a row, fp32 4), then G and U (4 MiB)
+    F = 48
+    x, wg, wu, dh, g, u = (ints(2, T, K), ints(2, F, K), ints(2, F, K), ints(1, T, F), ints(3, T, F),
+                           ints(3, T, F))
+    dg, du = dh * u * (g > 0), dh * torch.clamp(g, min=0)
+    want = [dg @ wg + du @ wu, dg.t() @ x, du.t() @ x, dg.sum(0), du.sum(0)]
+
+    def call(X, Wg, Wu, dH, G, U, **outs):
+        got = B.bsr_gated_backward(dH, X, Wg, Wu, G, U, act="relu", bias=True,
+                                   grad_dtype=torch.float32, **outs)
+        for t, w, name in zip(got, want, ("dX", "dWg", "dWu", "dbg", "dbu")):
+            assert torch.equal(t, w.float().to(t.dtype)), name
+
+    near = [t.to(dt) for t in (wg, wu)]
+    dX = torch.empty(T, pitch, dtype=dt, device=DEV)[:, :K]
+    assert dX.stride(0) == pitch
+    call(far(x, dt), *near, far(dh, dt), g.float(), u.float(), dX=dX)
+    del dX
+    call(x.to(dt), *near, dh.to(dt), far(g, torch.float32), far(u, torch.float32))
+    # channels far apart: the weights and their gradients
+    T, F = 96, 2200
+    x, wg, wu, dh, g, u = (ints(2, T, K), ints(2, F, K), ints(2, F, K), ints(1, T, F), ints(3, T, F),
+                           ints(3, T, F))
+    dg, du = dh * u * (g > 0), dh * torch.clamp(g, min=0)
+    want = [dg @ wg + du @ wu, dg.t() @ x, du.t() @ x, dg.sum(0), du.sum(0)]
+    dW = [torch.empty(F, pitch, device=DEV)[:, :K] for _ in range(2)]
+    call(x.to(dt), far(wg, dt), far(wu, dt), dh.to(dt), g.float(), u.float(), dWg=dW[0], dWu=dW[1])
