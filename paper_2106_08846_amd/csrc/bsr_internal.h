@@ -74,7 +74,8 @@ bsr_status check_attention(const float *Q, int64_t ldq, const float *K, int64_t 
                            float scale);
 
 // The dense products (8-bit and gated): limits that keep every tile's byte offsets in 32 bits (a
-// tile spans at most 256 rows of at most 4 MiB) and every grid below 2^22 workgroups.
+// tile spans at most 256 rows of at most 4 MiB) and every grid below 2^32 threads in x and 2^16
+// workgroups in y (dense_plan.h, tests/host/dense_grids.cpp).
 constexpr int64_t kDenseMaxWidth = int64_t(1) << 20;    // columns and pitches, elements
 constexpr int64_t kDenseMaxTokens = int64_t(1) << 24;
 constexpr int64_t kDenseMaxOut = int64_t(1) << 36;      // elements of all outputs of one tile grid

@@ -2,6 +2,7 @@
 // gradients, on the tiled matrix-core kernel (dense_tile.h).
 #include <type_traits>
 
+#include "dense_plan.h"
 #include "dense_ring.h"
 #include "dense_rows.h"
 #include "dense_split.h"
@@ -55,30 +56,6 @@ bool rows_aligned(const void *p, int64_t ld) {
     return ((reinterpret_cast<uintptr_t>(p) | uintptr_t(ld)) & 15) == 0;
 }
 
-// Rounds of workgroups that tiles of bm x bn take on the chip's CUs, times the cost of a round.
-int64_t rounds(const ProductArgs &a, bool dual, int bm, int bn, int cost) {
-    const int64_t rows = dual ? 2 * a.N : a.N;
-    const int64_t tiles = ((a.M + bm - 1) / bm) * ((rows + bn - 1) / bn), cus = device_cu_count();
-    return (tiles + cus - 1) / cus * cost;
-}
-
-// The tile by the rounds it takes.  The costs are those of a round of each tile, measured (MI355X) in
-// bf16 and int8 over grids of 1 to 32 rounds, in hundredths of a round of 256 x 256, which takes 110 us
-// at K = 4096 in bf16 and 61 in int8.  So bf16 4096 x 4096 x 4096 takes 110 us in 256 x 256 tiles, 160
-// in 128 x 128 and 259 in 64 x 64; 2048^3 51, 24 and 33; 128 x 8192 x 4096 84, 35 and 20; and
-// 6144 x 2048 x 16384, whose 192 tiles of 256 x 256 leave a quarter of the CUs idle, 438 against 368
-// in 192 x 256; int8 2048 x 20480 x 4096 184 in 256 x 256 (2.5 rounds) and 196 in 192 x 256 (3.4).
-constexpr int kRingTiles = 5;
-int64_t ring_cost(const ProductArgs &a, bool dual, int &best) {
-    const int64_t cost[kRingTiles] = {rounds(a, dual, 256, 256, 100), rounds(a, dual, 192, 256, 78),
-                                      rounds(a, dual, 128, 256, 62), rounds(a, dual, 128, 128, 38),
-                                      rounds(a, dual, 64, 64, 16)};
-    best = 0;
-    for (int i = 1; i < kRingTiles; ++i)
-        if (cost[i] < cost[best]) best = i;
-    return cost[best];
-}
-
 template <class E, Out OUT, bool COLS_A, bool COLS_B>
 void launch_ring_tile(const ProductArgs &a, int tile, void *stream) {
     switch (tile) {
@@ -110,29 +87,22 @@ ProductArgs channels_from(ProductArgs a, int64_t n, bool cols_b) {
     return a;
 }
 
-// A product whose last round of 256 x 256 tiles is not full goes in two launches where that saves a
-// twentieth: as many channels as fill whole rounds, then the rest in the tile that suits it
-// (int8 2048 tokens through 2 x 10240 x 4096: 640 tiles in 2.5 rounds).
+// Rows of the weights that a product's channels take in its tiles.
+int64_t weight_rows(const ProductArgs &a, bool dual) { return dual ? 2 * a.N : a.N; }
+
 template <class E, Out OUT, bool COLS_A = false, bool COLS_B = false>
 void launch_ring_product(const ProductArgs &a, void *stream) {
     constexpr bool dual = OUT == Out::kGated;
-    constexpr int64_t kChannels = dual ? 128 : 256;
-    int tile, rest_tile;
-    const int64_t whole = ring_cost(a, dual, tile);
-    const int64_t cus = device_cu_count(), tiles_m = (a.M + 255) / 256;
-    const int64_t tiles_n = (a.N + kChannels - 1) / kChannels;
-    const int64_t columns = tiles_m * tiles_n / cus * cus / tiles_m;    // of tiles, in full rounds
-    if (columns > 0 && columns < tiles_n) {
+    const int64_t cus = device_cu_count(), rows = weight_rows(a, dual);
+    if (const int64_t whole = rows_in_whole_rounds(a.M, rows, cus)) {
         ProductArgs first = a;
-        first.N = columns * kChannels;
+        first.N = dual ? whole / 2 : whole;
         const ProductArgs rest = channels_from(a, first.N, COLS_B);
-        const int64_t parts = rounds(first, dual, 256, 256, 100) + ring_cost(rest, dual, rest_tile);
-        if (parts * 20 <= whole * 19) {
-            launch_ring_tile<E, OUT, COLS_A, COLS_B>(first, 0, stream);
-            return launch_ring_tile<E, OUT, COLS_A, COLS_B>(rest, rest_tile, stream);
-        }
+        launch_ring_tile<E, OUT, COLS_A, COLS_B>(first, 0, stream);
+        const int tile = cheapest_tile(kRingTiles, a.M, weight_rows(rest, dual), cus);
+        return launch_ring_tile<E, OUT, COLS_A, COLS_B>(rest, tile, stream);
     }
-    launch_ring_tile<E, OUT, COLS_A, COLS_B>(a, tile, stream);
+    launch_ring_tile<E, OUT, COLS_A, COLS_B>(a, cheapest_tile(kRingTiles, a.M, rows, cus), stream);
 }
 
 template <class E, Out OUT> void launch_product(const ProductArgs &a, void *stream) {
@@ -147,25 +117,16 @@ template <class E, Out OUT> void launch_product(const ProductArgs &a, void *stre
         if (a.M <= 32 || ((a.M + 31) / 32) * ((a.N + 15) / 16) <= device_cu_count())
             return launch_rows<E, 2, OUT>(a, aligned, stream);
     }
+    const int64_t cus = device_cu_count(), rows = weight_rows(a, dual);
     if constexpr (sizeof(E) == 4) {
-        // Costs of a round at K = 4096, as above: 1000 x 768 x 3064 takes 102 us in 128 x 128 tiles and
-        // 49 in 64 x 64, 896 x 4096 x 768 36 and 45.
-        if (rounds(a, dual, 128, 128, 168) <= rounds(a, dual, 64, 64, 55))
+        if (cheapest_tile(kSplitTiles, a.M, rows, cus) == 0)
             launch_split<128, 128, 4, 2, OUT>(a, aligned, stream);
         else
             launch_split<64, 64, 4, 2, OUT>(a, aligned, stream);
     } else if (aligned) {
         launch_ring_product<E, OUT>(a, stream);
     } else {
-        // As launch_ring_product: bf16 4096 x 4096 x 4095 takes 146 us in 256 x 256 tiles, 183 in
-        // 128 x 256, 194 in 128 x 128 and 368 in 64 x 64; 2048 x 2048 x 4095 136, 89, 68 and 100;
-        // int8 333 x 2304 x 770 28, 18, 12 and 9.
-        const int64_t cost[4] = {rounds(a, dual, 256, 256, 100), rounds(a, dual, 128, 256, 63),
-                                 rounds(a, dual, 128, 128, 38), rounds(a, dual, 64, 64, 17)};
-        int best = 0;
-        for (int i = 1; i < 4; ++i)
-            if (cost[i] < cost[best]) best = i;
-        switch (best) {
+        switch (cheapest_tile(kRegisterTiles, a.M, rows, cus)) {
             case 0: return launch_tile<E, 256, 256, 2, 4, 1, OUT>(a, stream);
             case 1: return launch_tile<E, 128, 256, 2, 4, 1, OUT>(a, stream);
             case 2: return launch_tile<E, 128, 128, 2, 4, 2, OUT>(a, stream);
@@ -258,7 +219,9 @@ template <class T> __device__ __forceinline__ void load_some(const T *p, int64_t
 
 // out[c][r] = in[r][c] for r < R, c < C; out's rows are padded with zeros to `pad` columns.  The
 // gradients' three matrices (both weights and the tokens) go in one launch (6 us for 1000 tokens, 768
-// features and 1531 hidden units; 11 in two): tiles from first[i] on are matrix i's.
+// features and 1531 hidden units; 11 in two): tiles from first[i] on are matrix i's.  Beyond 2^16
+// tiles a workgroup takes several: 2^24 of them, which the sizes allow, would be more threads than a
+// launch can have.
 struct Transposes {
     const float *in[3];
     float *out[3];
@@ -282,24 +245,27 @@ struct Transposes {
 };
 __global__ __launch_bounds__(kThreads) void transpose_kernel(Transposes of) {
     __shared__ TransposeTile<float> tile;
-    int i = 0;
+    for (unsigned at = blockIdx.x; at < of.tiles; at += gridDim.x) {
+        int i = 0;
 #pragma unroll
-    for (int j = 1; j < 3; ++j)
-        if (j < of.matrices && blockIdx.x >= of.first[j]) i = j;
-    const float *in = of.in[i];
-    const int64_t ldi = of.ldi[i], R = of.R[i], C = of.C[i], pad = of.pad[i];
-    const unsigned id = blockIdx.x - of.first[i], across = unsigned((pad + kT - 1) / kT);
-    const int64_t r0 = int64_t(id % across) * kT, c0 = int64_t(id / across) * kT;
-    constexpr int V = kV<float>, per = kT / V;
+        for (int j = 1; j < 3; ++j)
+            if (j < of.matrices && at >= of.first[j]) i = j;
+        const float *in = of.in[i];
+        const int64_t ldi = of.ldi[i], R = of.R[i], C = of.C[i], pad = of.pad[i];
+        const unsigned id = at - of.first[i], across = unsigned((pad + kT - 1) / kT);
+        const int64_t r0 = int64_t(id % across) * kT, c0 = int64_t(id / across) * kT;
+        constexpr int V = kV<float>, per = kT / V;
 #pragma unroll
-    for (int e = threadIdx.x; e < kT * per; e += kThreads) {
-        const int r = e / per, c = e % per * V;
-        float v[V];
-        load_some(in + (r0 + r) * ldi + c0 + c, r0 + r < R ? C - c0 - c : 0, v);
-        tile.put(r, c, v);
+        for (int e = threadIdx.x; e < kT * per; e += kThreads) {
+            const int r = e / per, c = e % per * V;
+            float v[V];
+            load_some(in + (r0 + r) * ldi + c0 + c, r0 + r < R ? C - c0 - c : 0, v);
+            tile.put(r, c, v);
+        }
+        __syncthreads();
+        tile.store(of.out[i], of.ldo[i], r0, c0, C, pad);
+        __syncthreads();
     }
-    __syncthreads();
-    tile.store(of.out[i], of.ldo[i], r0, c0, C, pad);
 }
 
 // out[r][c] = in[r][c] for c < C, rows of `pad` elements (a multiple of 16 bytes) padded with zeros.
@@ -555,7 +521,8 @@ void backward(const void *dH, int64_t lddh, const void *X, int64_t T_, int64_t l
         }
         if (dWg) of.add(X, ldx, T_, K, reinterpret_cast<float *>(x_space), l.Tp, l.Tp);
         if (of.matrices && T_ > 0)
-            hipLaunchKernelGGL(transpose_kernel, dim3(of.tiles), dim3(kThreads), 0, as_stream(stream), of);
+            hipLaunchKernelGGL(transpose_kernel, dim3(grid_for(of.tiles, 1, kTransposeGroups)),
+                               dim3(kThreads), 0, as_stream(stream), of);
     }
     ProductArgs a{};
     a.A = reinterpret_cast<const char *>(D);

@@ -302,3 +302,16 @@ def test_gradients_past_32_bits_of_offset(dtype):
     want = [dg @ wg + du @ wu, dg.t() @ x, du.t() @ x, dg.sum(0), du.sum(0)]
     dW = [torch.empty(F, pitch, device=DEV)[:, :K] for _ in range(2)]
     call(x.to(dt), far(wg, dt), far(wu, dt), dh.to(dt), g.float(), u.float(), dWg=dW[0], dWu=dW[1])
+
+
+def test_transposes_of_more_tiles_than_workgroups():
+    """fp32 weights of 2 x 192 x 192 tiles of 64 x 64, more than the 2^16 workgroups that transpose."""
+    T, K, F = 5, 12270, 12250
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(9)
+    x, wg, wu, dh, g, u = (torch.randint(-n, n + 1, s, device=DEV, generator=gen).float() for n, s in
+                           ((2, (T, K)), (2, (F, K)), (2, (F, K)), (1, (T, F)), (3, (T, F)), (3, (T, F))))
+    got = B.bsr_gated_backward(dh, x, wg, wu, g, u, act="relu")
+    dg, du = (dh * u * (g > 0)).double(), (dh * torch.clamp(g, min=0)).double()
+    for t, want in zip(got, (dg @ wg.double() + du @ wu.double(), dg.t() @ x.double(), du.t() @ x.double())):
+        assert torch.equal(t.double(), want)          # below 2^24: exact
