@@ -491,8 +491,9 @@ LIBBSR_API bsr_status bsr_quantize_rows(const void *X, bsr_dtype x_dtype, int64_
  * bias added in fp32; bf16 output is rounded once from that (nearest, ties to even).  The result
  * does not depend on how the work is split.
  * Xq: device int8, T x K, row pitch ldx >= K.  Wq: device int8, N x K, row pitch ldw >= K (any
- *   pitch and base; 16-byte aligned rows load faster).  sx: device fp32[T], sw: fp32[N], bias:
- *   fp32[N] or NULL.  Y: device, T x N of y_dtype (BSR_F32 or BSR_BF16), row pitch ldy >= N.
+ *   pitch and base; rows that start on 16-byte boundaries and whose K is a multiple of 16 load faster).
+ *   sx: device fp32[T], sw: fp32[N], bias: fp32[N] or NULL.  Y: device, T x N of y_dtype (BSR_F32 or
+ *   BSR_BF16), row pitch ldy >= N.
  * T = 0 is a no-op; N, K >= 1.  Y must not overlap an input.
  * Errors: BSR_ERR_NULL, BSR_ERR_SHAPE, BSR_ERR_ARG (unknown dtype, overlap), BSR_ERR_DTYPE (y_dtype
  *   BSR_I8), BSR_ERR_UNSUPPORTED (K above 131071, where the 32-bit sum could overflow; N or a pitch

@@ -950,7 +950,10 @@ def bsr_gated(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor,
     """The gated feed-forward block H = act(X Wg^T + bg) * (X Wu^T + bu) in one kernel (bsr_gated):
     X [T, K], Wg and Wu [F, K], all float32 or all bfloat16, biases fp32; H [T, F] of X's type.
     act: "silu", "gelu", "gelu_tanh" or "relu".  With save (or G and U given) returns (H, G, U), G and
-    U the fp32 pre-activations that bsr_gated_backward reads; otherwise H."""
+    U the fp32 pre-activations that bsr_gated_backward reads; otherwise H.
+
+    As everywhere in this binding, autograd does not see the call: what it returns requires no gradient,
+    also from operands that do.  The gradients come from bsr_gated_backward."""
     ldx, block = _gated_block(X, Wg, Wu, None, None, bg, bu, act, _DATA_DTYPES)
     T, F = X.shape[0], block.F
     if (G is None) != (U is None):

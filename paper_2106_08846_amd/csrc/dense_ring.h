@@ -252,8 +252,8 @@ struct RingKernel {
         wait_loads<0>();               // what was loaded past the end, before LDS is used again
         __syncthreads();
         // The tiles that large products take write more than the L2s hold, and store past them: a gated
-        // int8 block of 2048 tokens, 4096 to 10240 features, takes 178 us with plain stores and 165 so,
-        // an int8 product of 8192^3 460 and 453.  The smaller tiles' outputs stay for the kernel that
+        // int8 block of 2048 tokens, 4096 to 10240 features, takes 175 us with plain stores and 168 so,
+        // an int8 product of 8192^3 466 and 457.  The smaller tiles' outputs stay for the kernel that
         // reads them next (the fp32 gradients of 1000 tokens, 768 features and 1531 hidden units: 150
         // us past the caches, 146 through them).
         constexpr bool kPast = BM * BN >= 192 * 256;

@@ -1,16 +1,20 @@
-// The dense products of few tokens (at most 32): the weights are read once, straight into the
-// operand registers of the matrix instructions, and that read is the whole cost.
+// The dense products of few tokens (up to 32, or as many as one round of the chip takes): the weights go
+// straight into the operand registers of the matrix instructions, and that read is the whole cost.
 //
-// A workgroup makes 16 channels (gated: of each matrix) for 16 NT tokens (blockIdx.y counts groups of
-// them).  Its eight waves split the contraction: wave w takes every eighth block of kBlock bytes of
-// the rows, loads a block's chunks all at once, and keeps its own sums; they are added over the
-// waves, in order, through LDS.  What bounds a single token is latency: 16 rows of 4096 bytes are one
-// block per wave, so that everything a workgroup needs is in flight together.  The tokens come from
-// the L2 (every workgroup reads all of them), which is why the tile kernels take over beyond 32.
+// A workgroup makes 16 channels (gated: of each matrix) for 16 NT tokens, at most 32 (blockIdx.y counts
+// groups of them, each of which reads the weights).  Its eight waves split the contraction: wave w takes
+// every eighth block of kBlock bytes of the rows, loads a block's chunks all at once, and keeps its own
+// sums; they are added over the waves, in order, through LDS.  What bounds a single token is latency: 16
+// rows of 4096 bytes are one block per wave, so that everything a workgroup needs is in flight together.
+// The tokens come from the L2 (every workgroup reads all of its group), which is why the tile kernels
+// take over beyond that.
 //
 // On MI355X an int8 token through 4096 x 4096 takes 5.2 us (its 16.8 MB would take 3.5 at a large
 // copy's rate), a bf16 gated block of 4 tokens, 1024 to 4096 features, 6.3 us, and an int8 one of 16
-// tokens, 4096 to 10240 features, 21 us: 84 MB at 4.0 TB/s, where a large copy moves 4.9.
+// tokens, 4096 to 10240 features, 21 us: 84 MB at 4.0 TB/s, where a large copy moves 4.9.  One token of
+// that block takes 35 us in bf16 and 65 in fp32 (5 TB/s).  Rows that are not aligned cost more: each
+// chunk takes two loads and the shifts that put it together, and the choice between whole and partial
+// chunks takes more scalar registers than there are (int8, 4 tokens of 4095 to 10240 features 46 us).
 #pragma once
 
 #include "dense_tile.h"
