@@ -557,7 +557,7 @@ LIBBSR_API size_t bsr_gated_workspace_bytes(int64_t T, int64_t K, int64_t F, bsr
  * The gradients of bsr_gated from dH, the gradient of H, and the pre-activations it kept:
  *   dG = dH * U * act'(G),  dU = dH * act(G)  (fp32; in a bf16 block rounded to bf16 as operands of the
  *   products below, but for fp32 dWg and dWu, which take the rounded values and what their rounding
- *   dropped, to 2^-16),
+ *   dropped, to 2^-16; an infinite X may then give NaN instead of an infinity),
  *   dX = dG Wg + dU Wu,  dWg = dG^T X,  dWu = dU^T X,
  *   dbg[f] = sum over t of dG[t][f],  dbu[f] = sum over t of dU[t][f]  (of the unrounded values).
  * Sums are fp32 in an order fixed by the sizes, products as in bsr_gated: repeated calls are bitwise
