@@ -142,6 +142,30 @@ def test_fp32_operands_near_the_smallest_ones(T, F, small):
             within(got, want, e + 2.0 ** -125 * (size[None, :] if sx == small else size[:, None]), "small")
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,F,K", [(96, 2000, 104), (300, 2000, 101), (777, 2048, 96), (2050, 2300, 72),
+                                   (2050, 2300, 75)])
+def test_non_finite_operands_in_tiles(dtype, T, F, K):
+    """Sizes beyond the few-token kernel's: an infinity or a NaN reaches its token's or channel's outputs
+    and leaves the other ones of its tile as they are."""
+    rng = np.random.default_rng(T + F + K)
+    x, wg, wu = (rand(rng, n, K, dtype=dtype).to(DEV) for n in (T, F, F))
+    clean = B.bsr_gated(x, wg, wu, save=True)
+    x[0, 17], x[T - 2, K - 1] = float("nan"), float("-inf")
+    wg[7, 3], wu[50, K - 1], wg[F - 1, 0] = float("inf"), float("nan"), float("-inf")
+    H, G, U = B.bsr_gated(x, wg, wu, save=True)
+    t = torch.ones(T, dtype=torch.bool, device=DEV)
+    t[[0, T - 2]] = False
+    assert torch.isnan(G[0]).all() and torch.isnan(U[0]).all() and torch.isnan(H[0]).all()
+    assert not torch.isfinite(G[T - 2]).any() and not torch.isfinite(U[T - 2]).any()
+    f = torch.ones(F, dtype=torch.bool, device=DEV)
+    f[[7, 50, F - 1]] = False
+    for a, b in zip((H, G, U), clean):
+        assert torch.equal(a[t][:, f], b[t][:, f])
+    assert not torch.isfinite(G[:, [7, F - 1]]).any() and torch.isnan(U[:, 50]).all()
+    assert torch.equal(G[t][:, 50], clean[1][t][:, 50]) and torch.equal(U[t][:, 7], clean[2][t][:, 7])
+
+
 # --- saturated activations -------------------------------------------------------------------------
 
 def wide_range():
