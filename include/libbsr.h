@@ -595,6 +595,115 @@ LIBBSR_API bsr_status bsr_gated_i8(const int8_t *Xq, int64_t T, int64_t ldx, con
                                    const bsr_gated_t *W, void *H, bsr_dtype h_dtype, int64_t ldh,
                                    void *stream);
 
+/*
+ * The norm between the products of a layer, with the residual sum before it:
+ *   S = X + R  (formed in fp32, rounded to the type; S = X where R is NULL),
+ *   mean[t] = sum over k of S[t][k] / K,  rstd[t] = 1 / sqrt(sum over k of (S[t][k] - mean[t])^2 / K + eps),
+ *   Y[t][k] = (S[t][k] - mean[t]) * rstd[t] * gamma[k] + beta[k],
+ * in fp32 throughout, Y rounded once to the type.  The mean is formed before the deviations, so a row far
+ * from zero keeps its variance.  The statistics are fp32: of a row whose squared deviations sum to 2^128 or
+ * more rstd is 0, and so is (S - mean) * rstd.  A NaN or an infinity in a row reaches that row only.
+ * X, R, Y, S: device, T x K of `dtype` (BSR_F32 or BSR_BF16), row pitches >= K.  R may be NULL; S (written
+ *   with R only) may be NULL.  gamma, beta: device fp32[K], each may be NULL (ones, zeros).  mean, rstd:
+ *   device fp32[T], kept for bsr_layer_norm_backward, or both NULL.
+ * T = 0 is a no-op; K >= 1; eps >= 0 and finite (with 0, a row of equal values gives NaN).  Outputs must
+ * not overlap an input or each other (columns of one buffer at the same pitch in bytes do not).
+ * Errors: BSR_ERR_NULL (also: one of mean and rstd without the other), BSR_ERR_SHAPE, BSR_ERR_ARG (unknown
+ *   dtype, eps, S without R, overlap), BSR_ERR_DTYPE (BSR_I8), BSR_ERR_UNSUPPORTED (K or a pitch above
+ *   2^20, T above 2^24), BSR_ERR_ARCH, BSR_ERR_HIP.
+ */
+LIBBSR_API bsr_status bsr_layer_norm(const void *X, int64_t ldx, const void *R, int64_t ldr, int64_t T,
+                                     int64_t K, bsr_dtype dtype, const float *gamma, const float *beta,
+                                     float eps, void *Y, int64_t ldy, void *S, int64_t lds, float *mean,
+                                     float *rstd, void *stream);
+
+/* Device workspace bytes of bsr_layer_norm_backward (0 if the sizes are invalid).  Host only. */
+LIBBSR_API size_t bsr_layer_norm_workspace_bytes(int64_t T, int64_t K);
+
+/*
+ * The gradients of bsr_layer_norm from dY, the gradient of Y, and the sum and statistics it kept.  With
+ * h = (S - mean) * rstd and g = dY * gamma, row by row:
+ *   dX = rstd * (g - sum over k of g / K - h * sum over k of (g * h) / K)  +  dS,
+ *   dgamma[k] = sum over t of dY[t][k] h[t][k],   dbeta[k] = sum over t of dY[t][k].
+ * dX is the gradient of X and of R alike.  All of it is fp32; dX is rounded once to the type, dgamma and
+ * dbeta once to grad_dtype.  Sums are formed in an order fixed by the sizes: repeated calls are bitwise
+ * reproducible.
+ * dY, S: device, T x K of `dtype`, row pitches >= K; S is bsr_layer_norm's (without a residual its X).
+ * gamma: device fp32[K] or NULL (ones).  mean, rstd: device fp32[T].
+ * dS: device, T x K of `dtype`: the gradient that reaches S by another path (the residual stream), or NULL.
+ * dX: device, T x K of `dtype`, or NULL (not wanted).  dgamma, dbeta: device, K elements of grad_dtype
+ *   (BSR_F32 or BSR_BF16); each may be NULL.
+ * workspace: device memory of at least bsr_layer_norm_workspace_bytes(T, K) bytes, 16-byte aligned; not
+ *   needed (may be NULL) where neither dgamma nor dbeta is wanted.  Its contents on entry do not matter.
+ *   It is in use until the enqueued work completes: calls that may overlap in time need one each.
+ * T = 0 sets dgamma and dbeta to zero.  Outputs and workspace must not overlap an input or each other.
+ * Errors: those of bsr_layer_norm, BSR_ERR_WORKSPACE (missing, too small or misaligned).
+ */
+LIBBSR_API bsr_status bsr_layer_norm_backward(const void *dY, int64_t lddy, const void *S, int64_t lds,
+                                              int64_t T, int64_t K, bsr_dtype dtype, const float *gamma,
+                                              const float *mean, const float *rstd, const void *dS,
+                                              int64_t ldds, void *dX, int64_t lddx, void *dgamma,
+                                              void *dbeta, bsr_dtype grad_dtype, void *workspace,
+                                              size_t ws_bytes, void *stream);
+
+/* 8-bit floating point, one byte an element: sign, exponent, fraction.  E4M3: largest value 448, least
+ * positive 2^-9, no infinities.  E5M2: largest 57344, least 2^-16. */
+typedef enum { BSR_E4M3 = 0, BSR_E5M2 = 1 } bsr_f8_format;
+
+/*
+ * A matrix in 8-bit floating point with an fp32 scale for each block: block_rows (1 or 128) rows of 128
+ * columns, shorter at the ends.  With a = max |x| over the block and m the format's largest value:
+ *   s = a / m;  r = m / a;  q = x r, rounded to the nearest value of the format, ties to even;
+ * every operation is rounded to fp32, so codes and scales are defined to the bit; x ~ s q.  A block with
+ * a < 2^-64 is multiplied by 2^64 first (exact), for r and q only.  A block of zeros has q = 0 and s = 0.
+ * One that holds an infinity has s = infinity and q = 0, one that holds a NaN s = NaN and q = 0: every
+ * output of a product with it is NaN.
+ * block_rows = 1 is the form of activations and gradients, 128 that of a weight.
+ * X: device, T x K of x_dtype (BSR_F32 or BSR_BF16), row pitch ldx >= K.
+ * Q: device, T x K codes, row pitch ldq >= K; scale: device fp32, ceil(K / 128) x ceil(T / block_rows):
+ *   row b holds the scales of columns 128 b .. of all rows side by side; pitch ldscale.  Both NULL: not
+ *   wanted.
+ * QT, scale_t: the same of X's transpose, whose blocks are block_rows columns of X by 128 of its rows: K x
+ *   T codes with pitch ldqt >= T, and ceil(T / 128) x ceil(K / block_rows) scales with pitch ldscale_t;
+ *   both NULL: not wanted.  Nothing beyond the rows' widths is written.
+ * T = 0 is a no-op; K >= 1.  Outputs must not overlap X or each other.
+ * Errors: BSR_ERR_NULL (also: codes without scales, or nothing wanted), BSR_ERR_SHAPE, BSR_ERR_ARG
+ *   (unknown dtype or format, block_rows, overlap), BSR_ERR_DTYPE (BSR_I8), BSR_ERR_UNSUPPORTED (K, ldx,
+ *   ldq or ldqt above 2^20, T or a scale pitch above 2^24), BSR_ERR_ARCH, BSR_ERR_HIP.
+ */
+LIBBSR_API bsr_status bsr_quantize_f8(const void *X, bsr_dtype x_dtype, int64_t T, int64_t K, int64_t ldx,
+                                      int32_t block_rows, bsr_f8_format format, void *Q, int64_t ldq,
+                                      float *scale, int64_t ldscale, void *QT, int64_t ldqt,
+                                      float *scale_t, int64_t ldscale_t, void *stream);
+
+/*
+ * The product of two matrices in 8-bit floating point with scales for blocks of 128:
+ *   Y[t][n] = sum over blocks b of  sx[b][t] sw[b][n'] * (sum over k in b of Xq[t][k] Wq[n][k])  +  bias[n],
+ * b = k / 128 and n' = n / w_block_rows.  Products and sums are fp32, in an order fixed by the sizes
+ * (repeated calls are bitwise reproducible); sx * sw is formed first, so where it lies below 2^-126 its
+ * bits are lost.  bf16 output is rounded once, from the sum with the bias, and may come from the 8-bit
+ * matrix instructions: of every eight consecutive products they drop what lies below 2^-13 of the largest
+ * one's power of two (of a sum of normally distributed products about 1.5e-5, where bf16 rounds by 4e-3).
+ * fp32 output keeps every product.
+ * With the codes and scales of bsr_quantize_f8 it is a layer's forward product (X by rows, W in blocks of
+ * 128 rows), its way back to the inputs (dY by rows, W's transpose), and the gradient of W (dY's and X's
+ * transposes with a scale for each row: w_block_rows = 1).
+ * Xq: device, T x K codes of x_format, row pitch ldx >= K; sx: device fp32, ceil(K / 128) x T, pitch ldsx.
+ * Wq: device, N x K codes of BSR_E4M3, row pitch ldw >= K; sw: device fp32, ceil(K / 128) x
+ *   ceil(N / w_block_rows), pitch ldsw; w_block_rows 1 or 128.  bias: device fp32[N] or NULL.
+ *   Rows that start on 16-byte boundaries load faster.
+ * Y: device, T x N of y_dtype (BSR_F32 or BSR_BF16), row pitch ldy >= N; must not overlap an input.
+ * T = 0 is a no-op; N, K >= 1.
+ * Errors: BSR_ERR_NULL, BSR_ERR_SHAPE, BSR_ERR_ARG (unknown dtype or format, w_block_rows, overlap),
+ *   BSR_ERR_DTYPE (y_dtype BSR_I8), BSR_ERR_UNSUPPORTED (K, N or a pitch of codes or Y above 2^20, T or a
+ *   scale pitch above 2^24, T * N above 2^36), BSR_ERR_ARCH, BSR_ERR_HIP.
+ */
+LIBBSR_API bsr_status bsr_matmul_f8(const void *Xq, bsr_f8_format x_format, int64_t T, int64_t K,
+                                    int64_t ldx, const float *sx, int64_t ldsx, const void *Wq, int64_t N,
+                                    int64_t ldw, const float *sw, int64_t ldsw, int32_t w_block_rows,
+                                    const float *bias, void *Y, bsr_dtype y_dtype, int64_t ldy,
+                                    void *stream);
+
 /* Static, human-readable name of a status code. */
 LIBBSR_API const char *bsr_status_str(bsr_status s);
 

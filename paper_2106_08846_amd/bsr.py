@@ -32,6 +32,8 @@ EXPORTS = ["bsr_prune_count", "bsr_prune_count_ex", "bsr_prune_workspace_bytes",
            "bsr_cast_f32_bf16", "bsr_iht_update",
            "bsr_quantize_rows", "bsr_matmul_i8", "bsr_gated", "bsr_gated_workspace_bytes",
            "bsr_gated_backward", "bsr_gated_i8",
+           "bsr_layer_norm", "bsr_layer_norm_workspace_bytes", "bsr_layer_norm_backward",
+           "bsr_quantize_f8", "bsr_matmul_f8",
            "bsr_status_str", "bsr_last_hip_error"]
 NORM_L2, NORM_L1 = 0, 1
 SELECT_GLOBAL, SELECT_PER_ROW = 0, 1
@@ -171,6 +173,21 @@ def _lib() -> ctypes.CDLL:
         lib.bsr_gated_backward.restype = st
         lib.bsr_gated_i8.argtypes = [p, i64, i64, p, block, p, st, i64, p]
         lib.bsr_gated_i8.restype = st
+        f32 = ctypes.c_float
+        lib.bsr_layer_norm.argtypes = [p, i64, p, i64, i64, i64, st, p, p, f32, p, i64, p, i64, p,
+                                       p, p]
+        lib.bsr_layer_norm.restype = st
+        lib.bsr_layer_norm_workspace_bytes.argtypes = [i64, i64]
+        lib.bsr_layer_norm_workspace_bytes.restype = sz
+        lib.bsr_layer_norm_backward.argtypes = [p, i64, p, i64, i64, i64, st, p, p, p, p, i64, p,
+                                                i64, p, p, st, p, sz, p]
+        lib.bsr_layer_norm_backward.restype = st
+        lib.bsr_quantize_f8.argtypes = [p, st, i64, i64, i64, i32, st, p, i64, p, i64, p, i64, p,
+                                        i64, p]
+        lib.bsr_quantize_f8.restype = st
+        lib.bsr_matmul_f8.argtypes = [p, st, i64, i64, i64, p, i64, p, i64, i64, p, i64, i32, p, p,
+                                      st, i64, p]
+        lib.bsr_matmul_f8.restype = st
         lib.bsr_status_str.argtypes = [ctypes.c_int]
         lib.bsr_status_str.restype = ctypes.c_char_p
         lib.bsr_last_hip_error.argtypes = []
@@ -1078,3 +1095,226 @@ def bsr_gated_i8(Xq: torch.Tensor, sx: torch.Tensor, Wgq: torch.Tensor, sg: torc
                                _ptr(H), _DTYPE_CODE[H.dtype], ldh, _on_stream(stream, made)),
            "bsr_gated_i8")
     return H
+
+
+def bsr_layer_norm(X: torch.Tensor, gamma: torch.Tensor | None = None,
+                   beta: torch.Tensor | None = None, R: torch.Tensor | None = None,
+                   eps: float = 1e-5, save: bool = False, keep_sum: bool = False,
+                   Y: torch.Tensor | None = None, S: torch.Tensor | None = None,
+                   mean: torch.Tensor | None = None, rstd: torch.Tensor | None = None, stream=None):
+    """Layer norm over the columns of S = X + R (bsr_layer_norm): X, R [T, K] float32 or bfloat16, gamma
+    and beta fp32 [K] (None: ones, zeros); R None: S is X.  Returns Y of X's type; with keep_sum (or S
+    given) (Y, S); with save (or mean and rstd given) (Y, S, mean, rstd), what
+    bsr_layer_norm_backward reads."""
+    ldx = _matrix_arg(X, "X", None, None, _DATA_DTYPES)
+    T, K = X.shape
+    kind = (X.dtype,)
+    ldr = 0 if R is None else _matrix_arg(R, "R", T, K, kind)
+    if gamma is not None:
+        _vector_arg(gamma, "gamma", K)
+    if beta is not None:
+        _vector_arg(beta, "beta", K)
+    if (mean is None) != (rstd is None):
+        raise ValueError("give both mean and rstd, or neither")
+    if S is not None and R is None:
+        raise ValueError("S is X itself without a residual R")
+    made = []
+    save = save or mean is not None
+    keep_sum = keep_sum or save or S is not None
+    if Y is None:
+        Y = torch.empty(T, K, dtype=X.dtype, device=X.device)
+        made.append(Y)
+        ldy = K
+    else:
+        ldy = _matrix_arg(Y, "Y", T, K, kind)
+    lds = 0
+    if R is not None and keep_sum:
+        if S is None:
+            S = torch.empty(T, K, dtype=X.dtype, device=X.device)
+            made.append(S)
+            lds = K
+        else:
+            lds = _matrix_arg(S, "S", T, K, kind)
+    if save:
+        if mean is None:
+            mean = torch.empty(T, dtype=_F32, device=X.device)
+            rstd = torch.empty(T, dtype=_F32, device=X.device)
+            made += [mean, rstd]
+        else:
+            _vector_arg(mean, "mean", T)
+            _vector_arg(rstd, "rstd", T)
+    _one_device(X, R, gamma, beta, Y, S, mean, rstd)
+    _check(_lib().bsr_layer_norm(_ptr(X), ldx, _ptr(R), ldr, T, K, _DTYPE_CODE[X.dtype], _ptr(gamma),
+                                 _ptr(beta), eps, _ptr(Y), ldy, _ptr(S), lds, _ptr(mean), _ptr(rstd),
+                                 _on_stream(stream, *made)), "bsr_layer_norm")
+    if R is None:
+        S = X
+    return (Y, S, mean, rstd) if save else (Y, S) if keep_sum else Y
+
+
+def bsr_layer_norm_workspace_bytes(T: int, K: int) -> int:
+    """Device bytes of bsr_layer_norm_backward's workspace."""
+    return int(_lib().bsr_layer_norm_workspace_bytes(T, K))
+
+
+def bsr_layer_norm_backward(dY: torch.Tensor, S: torch.Tensor, mean: torch.Tensor,
+                            rstd: torch.Tensor, gamma: torch.Tensor | None = None,
+                            dS: torch.Tensor | None = None, affine: bool = True,
+                            dX: torch.Tensor | None = None, dgamma: torch.Tensor | None = None,
+                            dbeta: torch.Tensor | None = None,
+                            grad_dtype: torch.dtype | None = None, need_dX: bool = True,
+                            workspace: torch.Tensor | None = None, stream=None):
+    """The gradients of bsr_layer_norm (bsr_layer_norm_backward) from dY, the gradient of Y, and the S,
+    mean and rstd that the forward call returned: returns (dX, dgamma, dbeta).  dX is the gradient of X
+    and of R; dS, when given, is the gradient that reaches S by another path and is added to it.
+
+    `affine` says whether dgamma and dbeta are wanted, `need_dX` whether dX is; what is not wanted is
+    None.  dgamma and dbeta are of grad_dtype (default: S's type), allocated here unless given.
+    `workspace` is a uint8 device tensor of bsr_layer_norm_workspace_bytes, allocated here when None; calls
+    that may overlap in time need one each."""
+    lds = _matrix_arg(S, "S", None, None, _DATA_DTYPES)
+    T, K = S.shape
+    kind = (S.dtype,)
+    lddy = _matrix_arg(dY, "dY", T, K, kind)
+    ldds = 0 if dS is None else _matrix_arg(dS, "dS", T, K, kind)
+    if mean is None or rstd is None:
+        raise ValueError("give mean and rstd, as the forward call with save returned them")
+    _vector_arg(mean, "mean", T)
+    _vector_arg(rstd, "rstd", T)
+    if gamma is not None:
+        _vector_arg(gamma, "gamma", K)
+    given = dgamma if dgamma is not None else dbeta
+    if grad_dtype is None:
+        grad_dtype = S.dtype if given is None else given.dtype
+    if grad_dtype not in _DATA_DTYPES:
+        raise TypeError("grad_dtype must be float32 or bfloat16")
+    made = []
+
+    def make(*shape, dtype):
+        made.append(torch.empty(*shape, dtype=dtype, device=S.device))
+        return made[-1]
+
+    if need_dX and dX is None:
+        dX = make(T, K, dtype=S.dtype)
+    lddx = 0 if dX is None else _matrix_arg(dX, "dX", T, K, kind)
+    if affine and dgamma is None:
+        dgamma = make(K, dtype=grad_dtype)
+    if affine and dbeta is None:
+        dbeta = make(K, dtype=grad_dtype)
+    for t, name in ((dgamma, "dgamma"), (dbeta, "dbeta")):
+        if t is not None:
+            _vector_arg(t, name, K, grad_dtype)
+    if workspace is None:
+        if dgamma is not None or dbeta is not None:
+            workspace = make(max(bsr_layer_norm_workspace_bytes(T, K), 1), dtype=torch.uint8)
+    elif (not isinstance(workspace, torch.Tensor) or workspace.dtype != torch.uint8
+            or workspace.dim() != 1 or not workspace.is_contiguous()):
+        raise ValueError("workspace must be a contiguous uint8 tensor")
+    _one_device(dY, S, mean, rstd, gamma, dS, dX, dgamma, dbeta, workspace)
+    _check(_lib().bsr_layer_norm_backward(
+        _ptr(dY), lddy, _ptr(S), lds, T, K, _DTYPE_CODE[S.dtype], _ptr(gamma), _ptr(mean), _ptr(rstd),
+        _ptr(dS), ldds, _ptr(dX), lddx, _ptr(dgamma), _ptr(dbeta), _DTYPE_CODE[grad_dtype],
+        _ptr(workspace), 0 if workspace is None else workspace.numel(), _on_stream(stream, *made)),
+        "bsr_layer_norm_backward")
+    return dX, dgamma, dbeta
+
+
+_F8_CODE = {torch.float8_e4m3fn: 0, torch.float8_e5m2: 1}
+_F8_DTYPES = tuple(_F8_CODE)
+_F8_BLOCK = 128
+
+
+def _f8_blocks(n: int, rows: int = _F8_BLOCK) -> int:
+    return (n + rows - 1) // rows
+
+
+def bsr_quantize_f8(X: torch.Tensor, block_rows: int = 1, q_dtype: torch.dtype = torch.float8_e4m3fn,
+                    form: str = "rows", Q: torch.Tensor | None = None,
+                    scale: torch.Tensor | None = None, QT: torch.Tensor | None = None,
+                    scale_t: torch.Tensor | None = None, stream=None):
+    """X in 8-bit floating point with an fp32 scale for each block of block_rows (1: activations and
+    gradients, 128: weights) x 128 (bsr_quantize_f8).  X [T, K] float32 or bfloat16; q_dtype
+    float8_e4m3fn or float8_e5m2.
+
+    form "rows" returns (Q [T, K], scale [ceil(K / 128), ceil(T / block_rows)]); "columns" the same of X's
+    transpose, (QT [K, T], scale_t [ceil(T / 128), ceil(K / block_rows)]); "both" all four.  Codes that
+    are allocated here have rows on 16-byte boundaries, which bsr_matmul_f8 loads faster."""
+    if form not in ("rows", "columns", "both"):
+        raise ValueError('form must be "rows", "columns" or "both"')
+    if block_rows not in (1, _F8_BLOCK):
+        raise ValueError("block_rows must be 1 or 128")
+    if q_dtype not in _F8_CODE:
+        raise TypeError("q_dtype must be float8_e4m3fn or float8_e5m2")
+    ldx = _matrix_arg(X, "X", None, None, _DATA_DTYPES)
+    T, K = X.shape
+    made = []
+
+    def codes(t, name, rows, cols):
+        if t is None:
+            pitch = (cols + 15) // 16 * 16
+            t = torch.empty(rows, pitch, dtype=q_dtype, device=X.device)
+            made.append(t)
+            return (t if pitch == cols else t[:, :cols]), max(pitch, 1)
+        return t, _matrix_arg(t, name, rows, cols, (q_dtype,))
+
+    def scales(t, name, rows, cols):
+        if t is None:
+            t = torch.empty(rows, cols, dtype=_F32, device=X.device)
+            made.append(t)
+            return t, max(cols, 1)
+        return t, _matrix_arg(t, name, rows, cols, _F32_DTYPES)
+
+    if (form == "columns" and (Q is not None or scale is not None)) or (
+            form == "rows" and (QT is not None or scale_t is not None)):
+        raise ValueError(f'an output is given that form "{form}" does not make')
+    ldq = ldscale = ldqt = ldscale_t = 0
+    if form != "columns":
+        Q, ldq = codes(Q, "Q", T, K)
+        scale, ldscale = scales(scale, "scale", _f8_blocks(K), _f8_blocks(T, block_rows))
+    if form != "rows":
+        QT, ldqt = codes(QT, "QT", K, T)
+        scale_t, ldscale_t = scales(scale_t, "scale_t", _f8_blocks(T), _f8_blocks(K, block_rows))
+    _one_device(X, Q, scale, QT, scale_t)
+    _check(_lib().bsr_quantize_f8(_ptr(X), _DTYPE_CODE[X.dtype], T, K, ldx, block_rows, _F8_CODE[q_dtype],
+                                  _ptr(Q), ldq, _ptr(scale), ldscale, _ptr(QT), ldqt, _ptr(scale_t),
+                                  ldscale_t, _on_stream(stream, *made)), "bsr_quantize_f8")
+    if form == "rows":
+        return Q, scale
+    return (QT, scale_t) if form == "columns" else (Q, scale, QT, scale_t)
+
+
+def bsr_matmul_f8(Xq: torch.Tensor, sx: torch.Tensor, Wq: torch.Tensor, sw: torch.Tensor,
+                  bias: torch.Tensor | None = None, Y: torch.Tensor | None = None,
+                  out_dtype: torch.dtype = torch.float32, stream=None) -> torch.Tensor:
+    """Y = X W^T + bias from 8-bit floating point in blocks of 128 (bsr_matmul_f8): Xq [T, K]
+    float8_e4m3fn or float8_e5m2 with sx fp32 [ceil(K / 128), T]; Wq [N, K] float8_e4m3fn with sw fp32
+    [ceil(K / 128), ceil(N / 128)] (a weight) or [ceil(K / 128), N] (a scale for each row); bias fp32 [N]; Y
+    [T, N] float32 or bfloat16 (out_dtype, when Y is None)."""
+    ldx = _matrix_arg(Xq, "Xq", None, None, _F8_DTYPES)
+    T, K = Xq.shape
+    ldw = _matrix_arg(Wq, "Wq", None, K, _F8_DTYPES[:1])
+    N = Wq.shape[0]
+    blocks = _f8_blocks(K)
+    ldsx = _matrix_arg(sx, "sx", blocks, T, _F32_DTYPES)
+    ldsw = _matrix_arg(sw, "sw", blocks, None, _F32_DTYPES)
+    if sw.shape[1] == N:
+        block_rows = 1
+    elif sw.shape[1] == _f8_blocks(N):
+        block_rows = _F8_BLOCK
+    else:
+        raise ValueError(f"sw must be [{blocks}, {N}] or [{blocks}, {_f8_blocks(N)}]")
+    if bias is not None:
+        _vector_arg(bias, "bias", N)
+    made = None
+    if Y is None:
+        if out_dtype not in _DATA_DTYPES:
+            raise TypeError("out_dtype must be float32 or bfloat16")
+        Y = made = torch.empty(T, N, dtype=out_dtype, device=Xq.device)
+        ldy = N
+    else:
+        ldy = _matrix_arg(Y, "Y", T, N, _DATA_DTYPES)
+    _one_device(Xq, sx, Wq, sw, bias, Y)
+    _check(_lib().bsr_matmul_f8(_ptr(Xq), _F8_CODE[Xq.dtype], T, K, ldx, _ptr(sx), ldsx, _ptr(Wq), N,
+                                ldw, _ptr(sw), ldsw, block_rows, _ptr(bias), _ptr(Y),
+                                _DTYPE_CODE[Y.dtype], ldy, _on_stream(stream, made)), "bsr_matmul_f8")
+    return Y

@@ -552,4 +552,60 @@ bsr_status bsr_gated_i8(const int8_t *Xq, int64_t T, int64_t ldx, const float *s
     return bsr::launch_gated_i8(Xq, T, ldx, sx, *W, H, dt, ldh, stream);
 }
 
+bsr_status bsr_layer_norm(const void *X, int64_t ldx, const void *R, int64_t ldr, int64_t T, int64_t K,
+                          bsr_dtype dtype, const float *gamma, const float *beta, float eps, void *Y,
+                          int64_t ldy, void *S, int64_t lds, float *mean, float *rstd, void *stream) {
+    const int32_t dt = bsr::raw_enum(dtype);
+    bsr_status s =
+        bsr::check_layer_norm(X, ldx, R, ldr, T, K, dt, gamma, beta, eps, Y, ldy, S, lds, mean, rstd);
+    if (s != BSR_OK) return s;
+    if (T == 0) return BSR_OK;
+    if ((s = bsr::ensure_device()) != BSR_OK) return s;
+    return bsr::launch_layer_norm(X, ldx, R, ldr, T, K, dt, gamma, beta, eps, Y, ldy, S, lds, mean, rstd,
+                                  stream);
+}
+
+bsr_status bsr_layer_norm_backward(const void *dY, int64_t lddy, const void *S, int64_t lds, int64_t T,
+                                   int64_t K, bsr_dtype dtype, const float *gamma, const float *mean,
+                                   const float *rstd, const void *dS, int64_t ldds, void *dX,
+                                   int64_t lddx, void *dgamma, void *dbeta, bsr_dtype grad_dtype,
+                                   void *workspace, size_t ws_bytes, void *stream) {
+    const int32_t dt = bsr::raw_enum(dtype), gt = bsr::raw_enum(grad_dtype);
+    bsr_status s = bsr::check_layer_norm_backward(dY, lddy, S, lds, T, K, dt, gamma, mean, rstd, dS, ldds,
+                                                  dX, lddx, dgamma, dbeta, gt, workspace, ws_bytes);
+    if (s != BSR_OK) return s;
+    if (!dgamma && !dbeta && (!dX || T == 0)) return BSR_OK;
+    if ((s = bsr::ensure_device()) != BSR_OK) return s;
+    return bsr::launch_layer_norm_backward(dY, lddy, S, lds, T, K, dt, gamma, mean, rstd, dS, ldds, dX,
+                                           lddx, dgamma, dbeta, gt, workspace, stream);
+}
+
+bsr_status bsr_quantize_f8(const void *X, bsr_dtype x_dtype, int64_t T, int64_t K, int64_t ldx,
+                           int32_t block_rows, bsr_f8_format format, void *Q, int64_t ldq, float *scale,
+                           int64_t ldscale, void *QT, int64_t ldqt, float *scale_t, int64_t ldscale_t,
+                           void *stream) {
+    const int32_t dt = bsr::raw_enum(x_dtype), f = bsr::raw_enum(format);
+    bsr_status s = bsr::check_quantize_f8(X, dt, T, K, ldx, block_rows, f, Q, ldq, scale, ldscale, QT,
+                                          ldqt, scale_t, ldscale_t);
+    if (s != BSR_OK) return s;
+    if (T == 0) return BSR_OK;
+    if ((s = bsr::ensure_device()) != BSR_OK) return s;
+    return bsr::launch_quantize_f8(X, dt, T, K, ldx, block_rows, f, Q, ldq, scale, ldscale, QT, ldqt,
+                                   scale_t, ldscale_t, stream);
+}
+
+bsr_status bsr_matmul_f8(const void *Xq, bsr_f8_format x_format, int64_t T, int64_t K, int64_t ldx,
+                         const float *sx, int64_t ldsx, const void *Wq, int64_t N, int64_t ldw,
+                         const float *sw, int64_t ldsw, int32_t w_block_rows, const float *bias, void *Y,
+                         bsr_dtype y_dtype, int64_t ldy, void *stream) {
+    const int32_t f = bsr::raw_enum(x_format), dt = bsr::raw_enum(y_dtype);
+    bsr_status s = bsr::check_matmul_f8(Xq, f, T, K, ldx, sx, ldsx, Wq, N, ldw, sw, ldsw, w_block_rows,
+                                        bias, Y, dt, ldy);
+    if (s != BSR_OK) return s;
+    if (T == 0) return BSR_OK;
+    if ((s = bsr::ensure_device()) != BSR_OK) return s;
+    return bsr::launch_matmul_f8(Xq, f, T, K, ldx, sx, ldsx, Wq, N, ldw, sw, ldsw, w_block_rows, bias, Y,
+                                 dt, ldy, stream);
+}
+
 }  // extern "C"

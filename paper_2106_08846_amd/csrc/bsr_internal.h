@@ -124,6 +124,43 @@ inline int gated_slices(int64_t M, int64_t N, int64_t steps, bool bf16) {
 constexpr int kGatedRowsPerPartial = 64;
 GatedWorkspace gated_workspace_layout(int64_t T, int64_t K, int64_t F, int32_t dtype);
 
+// Norms and 8-bit floating point: the limits of the dense products.
+constexpr int kF8Block = 128;                           // columns that share a scale
+// Row groups of the norm's backward pass, each of which sums dgamma and dbeta over its rows.  Up to
+// kNormFusedWidth columns a workgroup holds a row of both operands in registers and makes dX with them:
+// one wave to 1024 columns, four rows to a workgroup; four waves to 4096, sixteen beyond.  512 workgroups
+// of four waves are two to a CU.
+constexpr int64_t kNormFusedWidth = 16384;
+constexpr int norm_row_waves(int64_t K) { return K <= 1024 ? 1 : K <= 4096 ? 4 : 16; }
+struct NormWorkspace {
+    int groups;      // fp32 [groups][2][K]: the groups' sums
+    size_t bytes;
+};
+inline NormWorkspace layer_norm_workspace(int64_t T, int64_t K) {
+    const int64_t rows = K <= 1024 ? 4 : K <= kNormFusedWidth ? 1 : 64;
+    const int64_t most = K <= 4096 ? 512 : K <= kNormFusedWidth ? 256 : 64;
+    const int64_t groups = (T + rows - 1) / rows;
+    const int64_t n = groups < most ? groups : most;
+    return NormWorkspace{int(n), size_t(n > 0 ? n : 1) * 2 * size_t(K) * 4};
+}
+bsr_status check_layer_norm(const void *X, int64_t ldx, const void *R, int64_t ldr, int64_t T, int64_t K,
+                            int32_t dtype, const float *gamma, const float *beta, float eps,
+                            const void *Y, int64_t ldy, const void *S, int64_t lds, const float *mean,
+                            const float *rstd);
+bsr_status check_layer_norm_backward(const void *dY, int64_t lddy, const void *S, int64_t lds, int64_t T,
+                                     int64_t K, int32_t dtype, const float *gamma, const float *mean,
+                                     const float *rstd, const void *dS, int64_t ldds, const void *dX,
+                                     int64_t lddx, const void *dgamma, const void *dbeta,
+                                     int32_t grad_dtype, const void *workspace, size_t ws_bytes);
+bsr_status check_quantize_f8(const void *X, int32_t x_dtype, int64_t T, int64_t K, int64_t ldx,
+                             int32_t block_rows, int32_t format, const void *Q, int64_t ldq,
+                             const float *scale, int64_t ldscale, const void *QT, int64_t ldqt,
+                             const float *scale_t, int64_t ldscale_t);
+bsr_status check_matmul_f8(const void *Xq, int32_t x_format, int64_t T, int64_t K, int64_t ldx,
+                           const float *sx, int64_t ldsx, const void *Wq, int64_t N, int64_t ldw,
+                           const float *sw, int64_t ldsw, int32_t w_block_rows, const float *bias,
+                           const void *Y, int32_t y_dtype, int64_t ldy);
+
 // Device-side entry points (implemented in the .hip files).  Arguments are already validated.
 bsr_status ensure_device();  // current device is gfx950; caches its properties
 int device_cu_count();
@@ -168,6 +205,23 @@ bsr_status launch_gated_backward(const void *dH, int64_t lddh, const void *X, in
                                  const float *U, int64_t ldp, void *dX, int64_t lddx, void *dWg,
                                  void *dWu, int64_t lddw, void *dbg, void *dbu, int grad_dtype,
                                  void *workspace, void *stream);
+
+bsr_status launch_layer_norm(const void *X, int64_t ldx, const void *R, int64_t ldr, int64_t T, int64_t K,
+                             int dtype, const float *gamma, const float *beta, float eps, void *Y,
+                             int64_t ldy, void *S, int64_t lds, float *mean, float *rstd, void *stream);
+bsr_status launch_layer_norm_backward(const void *dY, int64_t lddy, const void *S, int64_t lds, int64_t T,
+                                      int64_t K, int dtype, const float *gamma, const float *mean,
+                                      const float *rstd, const void *dS, int64_t ldds, void *dX,
+                                      int64_t lddx, void *dgamma, void *dbeta, int grad_dtype,
+                                      void *workspace, void *stream);
+bsr_status launch_quantize_f8(const void *X, int x_dtype, int64_t T, int64_t K, int64_t ldx,
+                              int block_rows, int format, void *Q, int64_t ldq, float *scale,
+                              int64_t ldscale, void *QT, int64_t ldqt, float *scale_t,
+                              int64_t ldscale_t, void *stream);
+bsr_status launch_matmul_f8(const void *Xq, int x_format, int64_t T, int64_t K, int64_t ldx,
+                            const float *sx, int64_t ldsx, const void *Wq, int64_t N, int64_t ldw,
+                            const float *sw, int64_t ldsw, int w_block_rows, const float *bias, void *Y,
+                            int y_dtype, int64_t ldy, void *stream);
 
 void set_last_hip_error(const char *msg);
 

@@ -1,0 +1,412 @@
+// Layer norm with the residual sum before it, and its gradients.
+//
+// Memory bound: the forward pass reads X (and R) and writes Y (and S), the backward pass reads dY and S
+// (and dS) and writes dX, each once; a row stays in registers between its sums and its outputs.
+#include "row_vec.h"
+
+namespace bsr {
+
+namespace {
+
+struct NormArgs {
+    const void *X, *R;
+    const float *gamma, *beta;
+    void *Y, *S;
+    float *mean, *rstd;
+    int64_t T, ldx, ldr, ldy, lds;
+    int K;
+    float eps;
+};
+
+// kVec values of a vector that may be missing.
+template <bool WHOLE>
+__device__ __forceinline__ void load_or(const float *p, int k, int K, float other, float (&v)[kVec]) {
+    if (p) {
+        load_vec<float, WHOLE>(p, k, K, v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) v[i] = other;
+    }
+}
+
+// The sum of v over a row's waves, in every lane; `at` is the row's own LDS, used once.
+template <int WAVES> __device__ __forceinline__ float row_sum(float v, float *at) {
+    v = wave_sum(v);
+    if constexpr (WAVES > 1) {
+        if ((threadIdx.x & 63) == 0) at[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) v += at[w];
+    }
+    return v;
+}
+
+constexpr int kHeld = 8;       // load steps of a row that the forward pass holds in registers
+
+// WAVES waves per row, ROWS rows per workgroup.  WHOLE: K is a multiple of a load step's elements.  Rows
+// longer than the registers hold are read again for the deviations and for the outputs.
+template <class T, int WAVES, int ROWS, bool WHOLE>
+__global__ __launch_bounds__(64 * WAVES * ROWS) void norm_kernel(NormArgs a) {
+    static_assert(WAVES == 1 || ROWS == 1, "one row per barrier");
+    constexpr int kSpan = 64 * WAVES * kVec;
+    __shared__ float red[2][WAVES];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, K = a.K;
+    const int64_t row = int64_t(blockIdx.x) * ROWS + wave / WAVES;
+    if (row >= a.T) return;                    // whole waves, and no barrier where ROWS > 1
+    const T *x = static_cast<const T *>(a.X) + row * a.ldx;
+    const T *r = a.R ? static_cast<const T *>(a.R) + row * a.ldr : nullptr;
+    T *y = static_cast<T *>(a.Y) + row * a.ldy;
+    T *sum_out = a.S ? static_cast<T *>(a.S) + row * a.lds : nullptr;
+    const int k0 = (wave % WAVES * 64 + lane) * kVec;
+    // S[k ..], rounded to the type.
+    const auto load = [&](int k, float (&v)[kVec]) {
+        load_vec<T, WHOLE>(x, k, K, v);
+        if (r) {
+            float w[kVec];
+            load_vec<T, WHOLE>(r, k, K, w);
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) v[i] = to_float(from_float<T>(v[i] + w[i]));
+        }
+    };
+    const auto squares = [&](int k, const float (&v)[kVec], float mean) {
+        float q = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+            const float d = WHOLE || k + i < K ? v[i] - mean : 0.0f;
+            q = fmaf(d, d, q);
+        }
+        return q;
+    };
+    float v[kHeld][kVec];
+#pragma unroll
+    for (int s = 0; s < kHeld; ++s) {
+        if (s * kSpan >= K) break;
+        load(k0 + s * kSpan, v[s]);
+    }
+    float sum = 0.0f;
+#pragma unroll
+    for (int s = 0; s < kHeld; ++s) {
+        if (s * kSpan >= K) break;
+        if (sum_out) write_vec<T, WHOLE>(sum_out, k0 + s * kSpan, K, v[s]);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) sum += v[s][i];
+    }
+    for (int k = k0 + kHeld * kSpan; k < K; k += kSpan) {
+        float w[kVec];
+        load(k, w);
+        if (sum_out) write_vec<T, WHOLE>(sum_out, k, K, w);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) sum += w[i];
+    }
+    const float mean = row_sum<WAVES>(sum, red[0]) / float(K);
+    float square = 0.0f;
+#pragma unroll
+    for (int s = 0; s < kHeld; ++s) {
+        if (s * kSpan >= K) break;
+        square += squares(k0 + s * kSpan, v[s], mean);
+    }
+    for (int k = k0 + kHeld * kSpan; k < K; k += kSpan) {
+        float w[kVec];
+        load(k, w);
+        square += squares(k, w, mean);
+    }
+    const float rstd = 1.0f / sqrtf(row_sum<WAVES>(square, red[1]) / float(K) + a.eps);
+    if (lane == 0 && wave % WAVES == 0 && a.mean) {
+        a.mean[row] = mean;
+        a.rstd[row] = rstd;
+    }
+    const auto store = [&](int k, const float (&v)[kVec]) {
+        float g[kVec], b[kVec], out[kVec];
+        load_or<WHOLE>(a.gamma, k, K, 1.0f, g);
+        load_or<WHOLE>(a.beta, k, K, 0.0f, b);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) out[i] = fmaf((v[i] - mean) * rstd, g[i], b[i]);
+        write_vec<T, WHOLE>(y, k, K, out);
+    };
+#pragma unroll
+    for (int s = 0; s < kHeld; ++s) {
+        if (s * kSpan >= K) break;
+        store(k0 + s * kSpan, v[s]);
+    }
+    for (int k = k0 + kHeld * kSpan; k < K; k += kSpan) {
+        float w[kVec];
+        load(k, w);
+        store(k, w);
+    }
+}
+
+constexpr int64_t kRowsPerLaunch = int64_t(1) << 21;     // a grid has under 2^32 threads
+
+template <class T, int WAVES, int ROWS> void launch_norm(const NormArgs &args, void *stream) {
+    const auto kernel = args.K % (64 * WAVES * kVec) == 0 ? norm_kernel<T, WAVES, ROWS, true>
+                                                          : norm_kernel<T, WAVES, ROWS, false>;
+    for (int64_t t = 0; t < args.T; t += kRowsPerLaunch) {
+        NormArgs a = args;
+        a.T = args.T - t < kRowsPerLaunch ? args.T - t : kRowsPerLaunch;
+        a.X = static_cast<const T *>(a.X) + t * a.ldx;
+        if (a.R) a.R = static_cast<const T *>(a.R) + t * a.ldr;
+        a.Y = static_cast<T *>(a.Y) + t * a.ldy;
+        if (a.S) a.S = static_cast<T *>(a.S) + t * a.lds;
+        if (a.mean) a.mean += t, a.rstd += t;
+        hipLaunchKernelGGL(kernel, dim3(unsigned((a.T + ROWS - 1) / ROWS)), dim3(64 * WAVES * ROWS), 0,
+                           as_stream(stream), a);
+    }
+}
+
+template <class T> void norm(const NormArgs &a, void *stream) {
+    constexpr int64_t held = 64 * kVec * kHeld;   // elements of a row that a wave holds
+    if (a.K <= held)
+        launch_norm<T, 1, 4>(a, stream);
+    else if (a.K <= 4 * held)
+        launch_norm<T, 4, 1>(a, stream);
+    else
+        launch_norm<T, 16, 1>(a, stream);
+}
+
+// --- gradients ----------------------------------------------------------------------------------
+
+struct NormGradArgs {
+    const void *dY, *S, *dS;
+    const float *gamma, *mean, *rstd;
+    void *dX;
+    float *partial;          // [groups][2][K], or NULL: neither dgamma nor dbeta
+    int64_t T, lddy, lds, ldds, lddx;
+    int K;
+};
+
+// Rows of up to 1024 WAVES columns: a group of WAVES waves takes every row from its first on, one after
+// another, with its columns' gamma, dgamma and dbeta in registers.
+template <class T, int WAVES, int ROWS, bool WHOLE>
+__global__ __launch_bounds__(64 * WAVES * ROWS) void norm_backward_kernel(NormGradArgs a) {
+    static_assert(WAVES == 1 || ROWS == 1, "one row per barrier");
+    constexpr int kSteps = 2, kSpan = 64 * WAVES * kVec, kWidth = kSteps * kSpan;
+    __shared__ float red[2][2][WAVES];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, K = a.K;
+    const int k0 = (wave % WAVES * 64 + lane) * kVec;
+    float gamma[kSteps][kVec], dgamma[kSteps][kVec] = {}, dbeta[kSteps][kVec] = {};
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s)
+        if (s * kSpan < K) load_or<WHOLE>(a.gamma, k0 + s * kSpan, K, 1.0f, gamma[s]);
+    int parity = 0;
+    for (int64_t row = int64_t(blockIdx.x) * ROWS + wave / WAVES; row < a.T;
+         row += int64_t(gridDim.x) * ROWS) {
+        const T *dy = static_cast<const T *>(a.dY) + row * a.lddy;
+        const T *sum = static_cast<const T *>(a.S) + row * a.lds;
+        const float mean = a.mean[row], rstd = a.rstd[row];
+        float d[kSteps][kVec], h[kSteps][kVec];
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            if (s * kSpan >= K) break;
+            load_vec<T, WHOLE>(dy, k0 + s * kSpan, K, d[s]);
+            load_vec<T, WHOLE>(sum, k0 + s * kSpan, K, h[s]);
+        }
+        float c1 = 0.0f, c2 = 0.0f;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            if (s * kSpan >= K) break;
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) {
+                h[s][i] = (h[s][i] - mean) * rstd;
+                dgamma[s][i] = fmaf(d[s][i], h[s][i], dgamma[s][i]);
+                dbeta[s][i] += d[s][i];
+                d[s][i] *= gamma[s][i];
+                c1 += d[s][i];
+                c2 = fmaf(d[s][i], h[s][i], c2);
+            }
+        }
+        if (!a.dX) continue;
+        c1 = wave_sum(c1);
+        c2 = wave_sum(c2);
+        if constexpr (WAVES > 1) {
+            // The other half is written for the next row, and this one again only after its barrier.
+            if (lane == 0) red[parity][0][wave] = c1, red[parity][1][wave] = c2;
+            __syncthreads();
+            c1 = c2 = 0.0f;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) c1 += red[parity][0][w], c2 += red[parity][1][w];
+            parity ^= 1;
+        }
+        c1 /= float(K);
+        c2 /= float(K);
+        T *dx = static_cast<T *>(a.dX) + row * a.lddx;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            if (s * kSpan >= K) break;
+            float out[kVec], more[kVec] = {};
+            if (a.dS)
+                load_vec<T, WHOLE>(static_cast<const T *>(a.dS) + row * a.ldds, k0 + s * kSpan, K, more);
+#pragma unroll
+            for (int i = 0; i < kVec; ++i)
+                out[i] = fmaf(d[s][i] - c1 - h[s][i] * c2, rstd, more[i]);
+            write_vec<T, WHOLE>(dx, k0 + s * kSpan, K, out);
+        }
+    }
+    if (!a.partial) return;
+    float *to = a.partial + int64_t(blockIdx.x) * 2 * K;
+    if constexpr (ROWS > 1) {                  // the workgroup's rows, in order
+        __shared__ float all[ROWS][2][kWidth];
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) {
+                all[wave][0][k0 + s * kSpan + i] = dgamma[s][i];
+                all[wave][1][k0 + s * kSpan + i] = dbeta[s][i];
+            }
+        __syncthreads();
+        for (int at = threadIdx.x; at < 2 * kWidth; at += 64 * ROWS) {
+            const int which = at / kWidth, k = at % kWidth;
+            float sum = 0.0f;
+#pragma unroll
+            for (int w = 0; w < ROWS; ++w) sum += all[w][which][k];
+            if (k < K) to[which * K + k] = sum;
+        }
+    } else {
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            if (s * kSpan >= K) break;
+            write_vec<float, WHOLE>(to, k0 + s * kSpan, K, dgamma[s]);
+            write_vec<float, WHOLE>(to + K, k0 + s * kSpan, K, dbeta[s]);
+        }
+    }
+}
+
+// Longer rows: dX by a workgroup per row, which reads its row twice, and the sums over the rows apart.
+template <class T> __global__ __launch_bounds__(1024) void norm_dx_kernel(NormGradArgs a) {
+    constexpr int kSpan = 1024 * kVec;
+    __shared__ float red[2][2][16];
+    const int K = a.K, k0 = threadIdx.x * kVec;
+    int parity = 0;
+    for (int64_t row = blockIdx.x; row < a.T; row += gridDim.x) {
+        const T *dy = static_cast<const T *>(a.dY) + row * a.lddy;
+        const T *sum = static_cast<const T *>(a.S) + row * a.lds;
+        const float mean = a.mean[row], rstd = a.rstd[row];
+        const auto load = [&](int k, float (&g)[kVec], float (&h)[kVec]) {
+            float w[kVec];
+            load_vec<T, false>(dy, k, K, g);
+            load_vec<T, false>(sum, k, K, h);
+            load_or<false>(a.gamma, k, K, 1.0f, w);
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) {
+                g[i] *= w[i];
+                h[i] = (h[i] - mean) * rstd;
+            }
+        };
+        float c1 = 0.0f, c2 = 0.0f, g[kVec], h[kVec];
+        for (int k = k0; k < K; k += kSpan) {
+            load(k, g, h);
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) c1 += g[i], c2 = fmaf(g[i], h[i], c2);
+        }
+        c1 = row_sum<16>(c1, red[parity][0]) / float(K);
+        c2 = row_sum<16>(c2, red[parity][1]) / float(K);
+        parity ^= 1;
+        T *dx = static_cast<T *>(a.dX) + row * a.lddx;
+        for (int k = k0; k < K; k += kSpan) {
+            float out[kVec], more[kVec] = {};
+            load(k, g, h);
+            if (a.dS) load_vec<T, false>(static_cast<const T *>(a.dS) + row * a.ldds, k, K, more);
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) out[i] = fmaf(g[i] - c1 - h[i] * c2, rstd, more[i]);
+            write_vec<T, false>(dx, k, K, out);
+        }
+    }
+}
+constexpr int kColumnThreads = 256, kColumns = kColumnThreads * kVec;
+template <class T> __global__ __launch_bounds__(kColumnThreads) void norm_columns_kernel(NormGradArgs a) {
+    const int K = a.K, k = int(blockIdx.x) * kColumns + threadIdx.x * kVec;
+    if (k >= K) return;
+    float dgamma[kVec] = {}, dbeta[kVec] = {};
+    for (int64_t row = blockIdx.y; row < a.T; row += gridDim.y) {
+        float d[kVec], h[kVec];
+        load_vec<T, false>(static_cast<const T *>(a.dY) + row * a.lddy, k, K, d);
+        load_vec<T, false>(static_cast<const T *>(a.S) + row * a.lds, k, K, h);
+        const float mean = a.mean[row], rstd = a.rstd[row];
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+            dgamma[i] = fmaf(d[i], (h[i] - mean) * rstd, dgamma[i]);
+            dbeta[i] += d[i];
+        }
+    }
+    float *to = a.partial + int64_t(blockIdx.y) * 2 * K;
+    write_vec<float, false>(to, k, K, dgamma);
+    write_vec<float, false>(to + K, k, K, dbeta);
+}
+
+// The groups' sums joined, in order: 64 columns to a workgroup, whose waves take every 16th group each.
+constexpr int kJoinWaves = 16;
+template <class G>
+__global__ __launch_bounds__(64 * kJoinWaves) void norm_join_kernel(const float *partial, int groups, int K,
+                                                                    G *dgamma, G *dbeta) {
+    __shared__ float part[kJoinWaves][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t at = int64_t(blockIdx.x) * 64 + lane, width = 2 * int64_t(K);
+    float sum = 0.0f;
+    if (at < width)
+        for (int g = wave; g < groups; g += kJoinWaves) sum += partial[g * width + at];
+    part[wave][lane] = sum;
+    __syncthreads();
+    if (wave > 0 || at >= width) return;
+    sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kJoinWaves; ++w) sum += part[w][lane];
+    G *to = at < K ? dgamma : dbeta;
+    if (to) to[at < K ? at : at - K] = from_float<G>(sum);
+}
+
+template <class T, int WAVES, int ROWS> void launch_backward(const NormGradArgs &a, int groups, void *stream) {
+    const auto kernel = a.K % (64 * WAVES * kVec) == 0 ? norm_backward_kernel<T, WAVES, ROWS, true>
+                                                       : norm_backward_kernel<T, WAVES, ROWS, false>;
+    hipLaunchKernelGGL(kernel, dim3(unsigned(groups)), dim3(64 * WAVES * ROWS), 0, as_stream(stream), a);
+}
+
+template <class T> void norm_backward(const NormGradArgs &a, int groups, void *stream) {
+    if (a.K <= kNormFusedWidth) {
+        switch (norm_row_waves(a.K)) {
+            case 1: return launch_backward<T, 1, 4>(a, groups, stream);
+            case 4: return launch_backward<T, 4, 1>(a, groups, stream);
+            default: return launch_backward<T, 16, 1>(a, groups, stream);
+        }
+    }
+    if (a.dX)
+        hipLaunchKernelGGL(norm_dx_kernel<T>, dim3(grid_for(a.T, 1, 1 << 16)), dim3(1024), 0,
+                           as_stream(stream), a);
+    if (a.partial)
+        hipLaunchKernelGGL(norm_columns_kernel<T>,
+                           dim3(unsigned((a.K + kColumns - 1) / kColumns), unsigned(groups)),
+                           dim3(kColumnThreads), 0, as_stream(stream), a);
+}
+
+template <class G>
+void join(const float *partial, int groups, int64_t K, void *dgamma, void *dbeta, void *stream) {
+    hipLaunchKernelGGL(norm_join_kernel<G>, dim3(unsigned((2 * K + 63) / 64)), dim3(64 * kJoinWaves), 0,
+                       as_stream(stream), partial, groups, int(K), static_cast<G *>(dgamma),
+                       static_cast<G *>(dbeta));
+}
+
+}  // namespace
+
+bsr_status launch_layer_norm(const void *X, int64_t ldx, const void *R, int64_t ldr, int64_t T, int64_t K,
+                             int dtype, const float *gamma, const float *beta, float eps, void *Y,
+                             int64_t ldy, void *S, int64_t lds, float *mean, float *rstd, void *stream) {
+    const NormArgs a{X, R, gamma, beta, Y, S, mean, rstd, T, ldx, ldr, ldy, lds, int(K), eps};
+    dtype == BSR_BF16 ? norm<bf16>(a, stream) : norm<float>(a, stream);
+    return launch_status();
+}
+
+bsr_status launch_layer_norm_backward(const void *dY, int64_t lddy, const void *S, int64_t lds, int64_t T,
+                                      int64_t K, int dtype, const float *gamma, const float *mean,
+                                      const float *rstd, const void *dS, int64_t ldds, void *dX,
+                                      int64_t lddx, void *dgamma, void *dbeta, int grad_dtype,
+                                      void *workspace, void *stream) {
+    const bool vectors = dgamma || dbeta;
+    const int groups = layer_norm_workspace(T, K).groups;
+    const NormGradArgs a{dY, S, dS, gamma, mean, rstd, dX, vectors ? static_cast<float *>(workspace) : nullptr,
+                         T, lddy, lds, ldds, lddx, int(K)};
+    if (T > 0) dtype == BSR_BF16 ? norm_backward<bf16>(a, groups, stream) : norm_backward<float>(a, groups, stream);
+    if (vectors)
+        (grad_dtype == BSR_BF16 ? join<bf16> : join<float>)(a.partial, groups, K, dgamma, dbeta, stream);
+    return launch_status();
+}
+
+}  // namespace bsr

@@ -7,30 +7,13 @@
 // above infinity), so a NaN or an infinity anywhere in the row reaches its scale.
 // 8192 rows of 4096 bf16 take 16.5 us (MI355X), 6.1 TB/s over both directions; a single row of 1024
 // takes 1.8 us, a memory latency and the two ends of a kernel.
-#include "dense_math.h"
+#include "row_vec.h"
 
 namespace bsr {
 
 namespace {
 
-constexpr int kVec = 8;        // elements per lane and load step
 constexpr int kHeld = 8;       // load steps held in registers
-
-__device__ __forceinline__ unsigned abs_bits(float x) { return __float_as_uint(x) & 0x7fffffffu; }
-
-// kVec elements from x[k] on, as fp32; those from K on are 0.  WHOLE: there are none from K on.
-template <class T, bool WHOLE>
-__device__ __forceinline__ void load_vec(const T *x, int k, int K, float (&v)[kVec]) {
-    if (WHOLE || k + kVec <= K) {
-        T raw[kVec];
-        __builtin_memcpy(raw, x + k, sizeof raw);
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) v[i] = to_float(raw[i]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) v[i] = k + i < K ? to_float(x[k + i]) : 0.0f;
-    }
-}
 
 template <bool WHOLE>
 __device__ __forceinline__ void store_vec(int8_t *q, int k, int K, const float (&v)[kVec],

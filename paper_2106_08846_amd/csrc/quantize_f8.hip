@@ -1,0 +1,232 @@
+// Matrices in 8-bit floating point: an fp32 scale for each block of 1 x 128 or 128 x 128, by rows, by
+// columns (the transpose) or both.
+//
+// Memory bound: every element is read once and a byte is written for it in each order that is wanted.
+// By rows alone a wave takes rows of 512 elements, four blocks side by side, each held by 16 lanes.
+// Everything else goes by tiles of 128 x 128 that stay in registers between the maxima and the codes; the
+// transpose is made of 8 x 8 pieces in the lanes and put together in LDS.
+#include "row_vec.h"
+
+namespace bsr {
+
+namespace {
+
+constexpr int kThreads = 256;
+
+struct QuantizeArgs {
+    const void *X;
+    int64_t T, ldx;
+    int K;
+    uint8_t *Q, *QT;
+    float *scale, *scale_t;
+    int64_t ldq, ldscale, ldqt, ldscale_t;
+    int64_t t0;              // first row of this launch (a multiple of 128)
+};
+
+// What a block's largest magnitude (its bits) makes of it.
+template <int FMT> struct BlockScale {
+    static constexpr float kLargest = FMT == BSR_E4M3 ? 448.0f : 57344.0f;
+    float scale, lift, r;
+    bool plain;              // else zeros, or with an infinity or a NaN: every code is 0
+    __device__ __forceinline__ explicit BlockScale(unsigned top) {
+        const float a = __uint_as_float(top);
+        plain = top > 0 && top < 0x7f800000u;
+        lift = a < 0x1p-64f ? 0x1p64f : 1.0f;
+        r = plain ? kLargest / (a * lift) : 0.0f;
+        scale = a / kLargest;
+    }
+    __device__ __forceinline__ float of(float x) const { return plain ? (x * lift) * r : 0.0f; }
+};
+
+// Codes of four values, the first in the lowest byte (nearest, ties to even; none is beyond the largest
+// value by more than its rounding).
+template <int FMT> __device__ __forceinline__ unsigned codes4(float a, float b, float c, float d) {
+    int v = 0;
+    if constexpr (FMT == BSR_E4M3) {
+        v = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, v, false);
+        v = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, v, true);
+    } else {
+        v = __builtin_amdgcn_cvt_pk_bf8_f32(a, b, v, false);
+        v = __builtin_amdgcn_cvt_pk_bf8_f32(c, d, v, true);
+    }
+    return unsigned(v);
+}
+template <int FMT> __device__ __forceinline__ uint2 codes8(const BlockScale<FMT> &s, const float (&v)[kVec]) {
+    return uint2{codes4<FMT>(s.of(v[0]), s.of(v[1]), s.of(v[2]), s.of(v[3])),
+                 codes4<FMT>(s.of(v[4]), s.of(v[5]), s.of(v[6]), s.of(v[7]))};
+}
+
+// The first n of N bytes of v at p.
+template <int N, class V> __device__ __forceinline__ void store_bytes(uint8_t *p, int64_t n, const V &v) {
+    static_assert(sizeof(V) == N, "whole values");
+    if (n >= N) {
+        __builtin_memcpy(p, &v, N);
+    } else {
+        uint8_t b[N];
+        __builtin_memcpy(b, &v, N);
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i < n) p[i] = b[i];
+    }
+}
+
+__device__ __forceinline__ unsigned top_of(const float (&v)[kVec]) {
+    unsigned top = 0;
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) top = max(top, abs_bits(v[i]));
+    return top;
+}
+
+// By rows, blocks of 1 x 128: 16 rows of 512 columns to a workgroup, four rows to a wave, all loaded at
+// once.  The scales of one block lie side by side for the rows, so they are stored 16 at a time.
+constexpr int kStripRows = 16, kStripColumns = 64 * kVec;
+template <class T, int FMT> __global__ __launch_bounds__(kThreads) void quantize_strip_kernel(QuantizeArgs a) {
+    constexpr int kRows = 4, kBlocks = kStripColumns / kF8Block;
+    __shared__ float scales[kBlocks][kStripRows];
+    const int strips = (a.K + kStripColumns - 1) / kStripColumns;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, K = a.K;
+    const int64_t t0 = a.t0 + int64_t(blockIdx.x / strips) * kStripRows;
+    const int c0 = int(blockIdx.x % strips) * kStripColumns, k = c0 + lane * kVec;
+    float v[kRows][kVec] = {};
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        const int64_t t = t0 + wave * kRows + i;
+        if (t < a.T) load_vec<T, false>(static_cast<const T *>(a.X) + t * a.ldx, k, K, v[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        const int64_t t = t0 + wave * kRows + i;
+        const BlockScale<FMT> s(row_max(top_of(v[i])));
+        if (lane % 16 == 0) scales[lane / 16][wave * kRows + i] = s.scale;
+        if (t < a.T && k < K) store_bytes<8>(a.Q + t * a.ldq + k, K - k, codes8(s, v[i]));
+    }
+    __syncthreads();
+    const int b = threadIdx.x / kStripRows, i = threadIdx.x % kStripRows;
+    if (b < kBlocks && c0 + b * kF8Block < K && t0 + i < a.T)
+        a.scale[(c0 / kF8Block + b) * a.ldscale + t0 + i] = scales[b][i];
+}
+
+// Tiles of 128 x 128: a thread holds 8 rows of 8 columns.  ROWS: rows of a block by rows (1 or 128),
+// which is the width of one by columns.
+template <class T, int FMT, int ROWS> __global__ __launch_bounds__(kThreads) void quantize_tile_kernel(QuantizeArgs a) {
+    constexpr int kB = kF8Block, kWaves = kThreads / 64;
+    __shared__ unsigned tops[kWaves][kB];
+    __shared__ __align__(16) uint8_t turned[kB * kB];
+    const int tiles = (a.K + kB - 1) / kB;
+    const int64_t t0 = a.t0 + int64_t(blockIdx.x / tiles) * kB;
+    const int k0 = int(blockIdx.x % tiles) * kB, K = a.K;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int c = threadIdx.x % 16, r = threadIdx.x / 16;
+    const int k = k0 + c * kVec;
+    const int64_t t = t0 + r * kVec;
+    float v[kVec][kVec] = {};
+#pragma unroll
+    for (int i = 0; i < kVec; ++i)
+        if (t + i < a.T) load_vec<T, false>(static_cast<const T *>(a.X) + (t + i) * a.ldx, k, K, v[i]);
+
+    unsigned whole = 0;                        // ROWS = 128: the tile's largest
+    if constexpr (ROWS > 1) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) whole = max(whole, top_of(v[i]));
+        whole = row_max(whole);
+        if (lane % 16 == 0) tops[wave][lane / 16] = whole;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) whole = max(whole, tops[w][i]);
+        const BlockScale<FMT> s(whole);
+        if (threadIdx.x == 0) {
+            if (a.Q) a.scale[(k0 / kB) * a.ldscale + t0 / kB] = s.scale;
+            if (a.QT) a.scale_t[(t0 / kB) * a.ldscale_t + k0 / kB] = s.scale;
+        }
+    }
+    if (a.Q) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+            const BlockScale<FMT> s(ROWS > 1 ? whole : row_max(top_of(v[i])));
+            if (t + i >= a.T) continue;
+            if (ROWS == 1 && c == 0) a.scale[(k0 / kB) * a.ldscale + t + i] = s.scale;
+            if (k < K) store_bytes<8>(a.Q + (t + i) * a.ldq + k, K - k, codes8(s, v[i]));
+        }
+    }
+    if (!a.QT) return;
+    if constexpr (ROWS == 1) {                 // the largest of every column
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) {
+            unsigned top = 0;
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) top = max(top, abs_bits(v[i][j]));
+            top = max(top, unsigned(__shfl_xor(int(top), 16)));
+            top = max(top, unsigned(__shfl_xor(int(top), 32)));
+            if (lane < 16) tops[wave][c * kVec + j] = top;
+        }
+        __syncthreads();
+    }
+    // Column f of the tile is row f of `turned`, whose 16-byte chunks are permuted by f / 8.
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) {
+        const int f = c * kVec + j;
+        unsigned top = whole;
+        if constexpr (ROWS == 1) {
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) top = max(top, tops[w][f]);
+        }
+        const BlockScale<FMT> s(top);
+        if (ROWS == 1 && r == 0 && k0 + f < K) a.scale_t[(t0 / kB) * a.ldscale_t + k0 + f] = s.scale;
+        float column[kVec];
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) column[i] = v[i][j];
+        *reinterpret_cast<uint2 *>(turned + f * kB + (((r >> 1) ^ (c & 7)) << 4) + (r & 1) * 8) =
+            codes8(s, column);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < kB * kB / 16 / kThreads; ++e) {
+        const int at = e * kThreads + threadIdx.x, f = at / 8, part = at % 8;
+        const int64_t left = a.T - t0 - part * 16;
+        if (k0 + f < K && left > 0)
+            store_bytes<16>(a.QT + (k0 + f) * a.ldqt + t0 + part * 16, left,
+                            *reinterpret_cast<const uint4 *>(turned + f * kB + ((part ^ ((f >> 3) & 7)) << 4)));
+    }
+}
+
+// Workgroups of a launch: a grid has under 2^32 threads.
+constexpr int64_t kGroupsPerLaunch = int64_t(1) << 23;
+
+void launch(void (*kernel)(QuantizeArgs), QuantizeArgs a, int64_t tile_rows, int64_t tile_columns,
+            void *stream) {
+    const int64_t across = (a.K + tile_columns - 1) / tile_columns;
+    const int64_t down = (a.T + tile_rows - 1) / tile_rows, most = kGroupsPerLaunch / across;
+    for (int64_t first = 0; first < down; first += most) {
+        const int64_t n = down - first < most ? down - first : most;
+        a.t0 = first * tile_rows;
+        hipLaunchKernelGGL(kernel, dim3(unsigned(n * across)), dim3(kThreads), 0, as_stream(stream), a);
+    }
+}
+
+template <class T, int FMT> void quantize(const QuantizeArgs &a, int block_rows, void *stream) {
+    if (block_rows > 1)
+        launch(quantize_tile_kernel<T, FMT, kF8Block>, a, kF8Block, kF8Block, stream);
+    else if (a.QT)
+        launch(quantize_tile_kernel<T, FMT, 1>, a, kF8Block, kF8Block, stream);
+    else
+        launch(quantize_strip_kernel<T, FMT>, a, kStripRows, kStripColumns, stream);
+}
+
+}  // namespace
+
+bsr_status launch_quantize_f8(const void *X, int x_dtype, int64_t T, int64_t K, int64_t ldx,
+                              int block_rows, int format, void *Q, int64_t ldq, float *scale,
+                              int64_t ldscale, void *QT, int64_t ldqt, float *scale_t,
+                              int64_t ldscale_t, void *stream) {
+    const QuantizeArgs a{X, T, ldx, int(K), static_cast<uint8_t *>(Q), static_cast<uint8_t *>(QT),
+                         scale, scale_t, ldq, ldscale, ldqt, ldscale_t, 0};
+    const auto f = x_dtype == BSR_BF16
+                       ? (format == BSR_E4M3 ? quantize<bf16, BSR_E4M3> : quantize<bf16, BSR_E5M2>)
+                       : (format == BSR_E4M3 ? quantize<float, BSR_E4M3> : quantize<float, BSR_E5M2>);
+    f(a, block_rows, stream);
+    return launch_status();
+}
+
+}  // namespace bsr

@@ -456,9 +456,119 @@ bsr_status check_gated_backward(const void *dH, int64_t lddh, const void *X, int
     return disjoint(in, out) ? BSR_OK : BSR_ERR_ARG;
 }
 
+// --- norms and 8-bit floating point -------------------------------------------------------------
+
+bsr_status check_layer_norm(const void *X, int64_t ldx, const void *R, int64_t ldr, int64_t T, int64_t K,
+                            int32_t dtype, const float *gamma, const float *beta, float eps,
+                            const void *Y, int64_t ldy, const void *S, int64_t lds, const float *mean,
+                            const float *rstd) {
+    if (!known_dtype(dtype) || !std::isfinite(eps) || eps < 0.0f || (S && !R)) return BSR_ERR_ARG;
+    if (dtype == BSR_I8) return BSR_ERR_DTYPE;
+    if (T < 0 || K < 1 || ldx < K || ldy < K || (R && ldr < K) || (S && lds < K)) return BSR_ERR_SHAPE;
+    if (T > kDenseMaxTokens || K > kDenseMaxWidth || ldx > kDenseMaxWidth || ldy > kDenseMaxWidth ||
+        (R && ldr > kDenseMaxWidth) || (S && lds > kDenseMaxWidth))
+        return BSR_ERR_UNSUPPORTED;
+    if (!mean != !rstd) return BSR_ERR_NULL;
+    if (T == 0) return BSR_OK;
+    if (!X || !Y) return BSR_ERR_NULL;
+    const int64_t e = dtype_size(dtype);
+    const Span in[] = {span(X, T, ldx, K, e), span(R, T, ldr, K, e), span(gamma, 1, K, K, 4),
+                       span(beta, 1, K, K, 4)};
+    const Span out[] = {span(Y, T, ldy, K, e), span(S, T, lds, K, e), span(mean, 1, T, T, 4),
+                        span(rstd, 1, T, T, 4)};
+    return disjoint(in, out) ? BSR_OK : BSR_ERR_ARG;
+}
+
+bsr_status check_layer_norm_backward(const void *dY, int64_t lddy, const void *S, int64_t lds, int64_t T,
+                                     int64_t K, int32_t dtype, const float *gamma, const float *mean,
+                                     const float *rstd, const void *dS, int64_t ldds, const void *dX,
+                                     int64_t lddx, const void *dgamma, const void *dbeta,
+                                     int32_t grad_dtype, const void *workspace, size_t ws_bytes) {
+    if (!known_dtype(dtype) || !known_dtype(grad_dtype)) return BSR_ERR_ARG;
+    if (dtype == BSR_I8 || grad_dtype == BSR_I8) return BSR_ERR_DTYPE;
+    if (T < 0 || K < 1 || lddy < K || lds < K || (dS && ldds < K) || (dX && lddx < K))
+        return BSR_ERR_SHAPE;
+    if (T > kDenseMaxTokens || K > kDenseMaxWidth || lddy > kDenseMaxWidth || lds > kDenseMaxWidth ||
+        (dS && ldds > kDenseMaxWidth) || (dX && lddx > kDenseMaxWidth))
+        return BSR_ERR_UNSUPPORTED;
+    if (T > 0 && (!dY || !S || !mean || !rstd)) return BSR_ERR_NULL;
+    const bool vectors = dgamma || dbeta;
+    const size_t need = vectors ? layer_norm_workspace(T, K).bytes : 0;
+    if (vectors &&
+        (!workspace || ws_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 15) != 0))
+        return BSR_ERR_WORKSPACE;
+    const int64_t e = dtype_size(dtype), g = dtype_size(grad_dtype);
+    const Span in[] = {span(dY, T, lddy, K, e),   span(S, T, lds, K, e),   span(dS, T, ldds, K, e),
+                       span(gamma, 1, K, K, 4), span(mean, 1, T, T, 4), span(rstd, 1, T, T, 4)};
+    const Span out[] = {span(dX, T, lddx, K, e), span(dgamma, 1, K, K, g), span(dbeta, 1, K, K, g),
+                        span(vectors ? workspace : nullptr, 1, int64_t(need), int64_t(need), 1)};
+    return disjoint(in, out) ? BSR_OK : BSR_ERR_ARG;
+}
+
+namespace {
+
+bool known_f8(int32_t f) { return f == BSR_E4M3 || f == BSR_E5M2; }
+int64_t blocks_of(int64_t n, int64_t rows) { return n / rows + (n % rows != 0); }
+
+}  // namespace
+
+bsr_status check_quantize_f8(const void *X, int32_t x_dtype, int64_t T, int64_t K, int64_t ldx,
+                             int32_t block_rows, int32_t format, const void *Q, int64_t ldq,
+                             const float *scale, int64_t ldscale, const void *QT, int64_t ldqt,
+                             const float *scale_t, int64_t ldscale_t) {
+    if (!known_dtype(x_dtype) || !known_f8(format) || (block_rows != 1 && block_rows != kF8Block))
+        return BSR_ERR_ARG;
+    if (x_dtype == BSR_I8) return BSR_ERR_DTYPE;
+    if (T < 0 || K < 1 || ldx < K) return BSR_ERR_SHAPE;
+    if (T > kDenseMaxTokens || ldx > kDenseMaxWidth) return BSR_ERR_UNSUPPORTED;
+    const bool rows = Q || scale, columns = QT || scale_t;
+    const int64_t kb = blocks_of(K, kF8Block), tb = blocks_of(T, kF8Block);
+    const int64_t row_scales = blocks_of(T, block_rows), column_scales = blocks_of(K, block_rows);
+    if ((rows && (ldq < K || ldscale < row_scales)) ||
+        (columns && (ldqt < T || ldqt < 1 || ldscale_t < column_scales)))
+        return BSR_ERR_SHAPE;
+    if ((rows && (ldq > kDenseMaxWidth || ldscale > kDenseMaxTokens)) ||
+        (columns && (ldqt > kDenseMaxWidth || ldscale_t > kDenseMaxTokens)))
+        return BSR_ERR_UNSUPPORTED;
+    if (T == 0) return BSR_OK;
+    if (!X || !Q != !scale || !QT != !scale_t || (!Q && !QT)) return BSR_ERR_NULL;
+    const Span in[] = {span(X, T, ldx, K, dtype_size(x_dtype))};
+    const Span out[] = {span(Q, T, ldq, K, 1), span(scale, kb, ldscale, row_scales, 4),
+                        span(QT, K, ldqt, T, 1), span(scale_t, tb, ldscale_t, column_scales, 4)};
+    return disjoint(in, out) ? BSR_OK : BSR_ERR_ARG;
+}
+
+bsr_status check_matmul_f8(const void *Xq, int32_t x_format, int64_t T, int64_t K, int64_t ldx,
+                           const float *sx, int64_t ldsx, const void *Wq, int64_t N, int64_t ldw,
+                           const float *sw, int64_t ldsw, int32_t w_block_rows, const float *bias,
+                           const void *Y, int32_t y_dtype, int64_t ldy) {
+    if (!known_dtype(y_dtype) || !known_f8(x_format) || (w_block_rows != 1 && w_block_rows != kF8Block))
+        return BSR_ERR_ARG;
+    if (y_dtype == BSR_I8) return BSR_ERR_DTYPE;
+    if (T < 0 || K < 1 || N < 1 || ldx < K || ldw < K || ldy < N || ldsx < T ||
+        ldsw < blocks_of(N, w_block_rows))
+        return BSR_ERR_SHAPE;
+    if (ldx > kDenseMaxWidth || ldw > kDenseMaxWidth || ldy > kDenseMaxWidth || N > kDenseMaxWidth ||
+        T > kDenseMaxTokens || ldsx > kDenseMaxTokens || ldsw > kDenseMaxTokens ||
+        T * N > kDenseMaxOut)
+        return BSR_ERR_UNSUPPORTED;
+    if (T == 0) return BSR_OK;
+    if (!Xq || !sx || !Wq || !sw || !Y) return BSR_ERR_NULL;
+    const int64_t kb = blocks_of(K, kF8Block), wb = blocks_of(N, w_block_rows);
+    const Span in[] = {span(Xq, T, ldx, K, 1), span(Wq, N, ldw, K, 1), span(sx, kb, ldsx, T, 4),
+                       span(sw, kb, ldsw, wb, 4), span(bias, 1, N, N, 4)};
+    const Span out[] = {span(Y, T, ldy, N, dtype_size(y_dtype))};
+    return disjoint(in, out) ? BSR_OK : BSR_ERR_ARG;
+}
+
 }  // namespace bsr
 
 extern "C" {
+
+size_t bsr_layer_norm_workspace_bytes(int64_t T, int64_t K) {
+    if (T < 0 || K < 1 || T > bsr::kDenseMaxTokens || K > bsr::kDenseMaxWidth) return 0;
+    return bsr::layer_norm_workspace(T, K).bytes;
+}
 
 size_t bsr_gated_workspace_bytes(int64_t T, int64_t K, int64_t F, bsr_dtype dtype) {
     const int32_t dt = bsr::raw_enum(dtype);

@@ -1,0 +1,305 @@
+"""Matrices in 8-bit floating point and their product on the GPU: codes and scales bit for bit as the
+oracle defines them, products within bounds that count the roundings of fp32 (oracle/f8_oracle.py) and bit
+for bit where every operation is exact."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import f8_oracle as F
+from paper_2106_08846_amd import bsr as B
+from tests.gpu_common import host
+from tests.test_gpu_dense import DEV, TORCH, f64, held, rand, within
+
+pytestmark = pytest.mark.gpu
+
+F8 = {"e4m3": torch.float8_e4m3fn, "e5m2": torch.float8_e5m2}
+
+
+def bits(t):
+    return host(t.contiguous().view(torch.uint8))
+
+
+def codes(q, fmt, pad=0, shift=0, gap=0x7F):
+    """Codes (uint8) on the device at pitch width + pad, `shift` bytes into their storage; NaN between."""
+    T, K = q.shape
+    buf = torch.full((T * (K + pad) + shift + 8,), gap, dtype=torch.uint8, device=DEV)
+    view = buf[shift:shift + T * (K + pad)].view(T, K + pad)[:, :K]
+    view.copy_(torch.from_numpy(q))
+    return view.view(F8[fmt])
+
+
+def code_frame(T, K, fmt, pad, shift):
+    buf = torch.full((T * (K + pad) + shift + 64,), 77, dtype=torch.uint8, device=DEV)
+    view = buf[shift:shift + T * (K + pad)].view(T, K + pad)[:, :K]
+
+    def untouched():
+        copy = buf.clone()
+        copy[shift:shift + T * (K + pad)].view(T, K + pad)[:, :K] = 77
+        return bool((copy == 77).all())
+    return view.view(F8[fmt]), untouched
+
+
+def check_codes(x, q, scale, rows, fmt):
+    want, want_s = F.quantize(x, rows, fmt)
+    assert np.array_equal(bits(q), want)
+    got = host(scale)
+    assert got.shape == want_s.shape
+    assert np.array_equal(np.isnan(got), np.isnan(want_s))
+    ok = ~np.isnan(want_s)
+    assert np.array_equal(got[ok].view(np.uint32), want_s[ok].view(np.uint32))
+
+
+@pytest.mark.parametrize("T,K", [(1, 1), (1, 128), (2, 129), (3, 770), (16, 512), (17, 513), (128, 128),
+                                 (129, 127), (300, 1000), (5, 4096), (127, 259), (256, 384)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,fmt", [(1, "e4m3"), (1, "e5m2"), (128, "e4m3"), (128, "e5m2")])
+def test_quantize(T, K, dtype, rows, fmt):
+    rng = np.random.default_rng(T * 100003 + K)
+    x = rand(rng, T, K, dtype=dtype) * torch.from_numpy(
+        np.exp(rng.uniform(-20, 20, (T, 1))).astype(np.float32)).to(TORCH[dtype])
+    xn = x.float().numpy()
+    for pad, shift in ((0, 0), (3, 1)):
+        X = held(x, pad, shift)
+        q, clean = code_frame(T, K, fmt, pad, shift)
+        qt, clean_t = code_frame(K, T, fmt, pad, shift)
+        Q, s, QT, st = B.bsr_quantize_f8(X, rows, F8[fmt], "both", Q=q, QT=qt)
+        check_codes(xn, Q, s, rows, fmt)
+        check_codes(np.ascontiguousarray(xn.T), QT, st, rows, fmt)
+        assert clean() and clean_t()
+        only, only_s = B.bsr_quantize_f8(X, rows, F8[fmt])
+        assert np.array_equal(bits(only), bits(Q)) and torch.equal(only_s, s)
+        only, only_s = B.bsr_quantize_f8(X, rows, F8[fmt], "columns")
+        assert np.array_equal(bits(only), bits(QT)) and torch.equal(only_s, st)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("rows", [1, 128])
+def test_quantize_special_values(dtype, fmt, rows):
+    rng = np.random.default_rng(5)
+    x = rng.standard_normal((9 * rows, 300)).astype(np.float32)
+    at = lambda i: i * rows                           # noqa: E731  the first row of block row i
+    x[at(0):at(1)] = 0.0
+    x[at(1), 299] = np.inf
+    x[at(2), 0] = -np.inf
+    x[at(3), 130] = np.nan
+    x[at(4):at(5)] *= np.float32(2.0 ** -130)         # subnormal blocks
+    x[at(5):at(6)] = np.float32(2.0 ** -133)
+    x[at(6):at(7)] *= np.float32(1e37)
+    x[at(7), 0], x[at(7), 5] = np.inf, np.nan
+    x[at(8):] = -0.0
+    # ties and the largest value exactly: 448 and 57344 are 1.75 times a power of two
+    x[at(6), :128] = np.arange(128, dtype=np.float32) * np.float32(1.75 / 127)
+    t = torch.from_numpy(x).to(TORCH[dtype])
+    Q, s, QT, st = B.bsr_quantize_f8(t.to(DEV), rows, F8[fmt], "both")
+    check_codes(t.float().numpy(), Q, s, rows, fmt)
+    check_codes(np.ascontiguousarray(t.float().numpy().T), QT, st, rows, fmt)
+
+
+def test_quantize_long_offsets():
+    T, K, pitch = 2200, 200, 1 << 20
+    x = rand(np.random.default_rng(9), T, K, dtype="bf16")
+    buf = torch.empty(T * pitch, dtype=torch.bfloat16, device=DEV)
+    X = buf.view(T, pitch)[:, :K]
+    X.copy_(x)
+    out = torch.empty(T * pitch, dtype=torch.uint8, device=DEV).view(T, pitch)[:, :K].view(F8["e4m3"])
+    Q, s, QT, st = B.bsr_quantize_f8(X, form="both", Q=out)
+    check_codes(x.float().numpy(), Q, s, 1, "e4m3")
+    check_codes(np.ascontiguousarray(x.float().numpy().T), QT, st, 1, "e4m3")
+
+
+# --- product ------------------------------------------------------------------------------------
+
+# Token counts around the small-batch and tile sizes; widths around blocks of 128 and chunks of 16.
+SIZES = [(1, 1, 1), (1, 64, 128), (1, 100, 1000), (2, 33, 770), (4, 4096, 64), (7, 16, 4096),
+         (16, 257, 256), (17, 129, 255), (32, 64, 2048), (33, 96, 129), (63, 100, 96), (64, 256, 384),
+         (65, 255, 130), (128, 128, 1024), (130, 640, 48), (257, 130, 514), (300, 513, 1),
+         (512, 1024, 256), (1100, 1300, 192), (3, 5, 20001)]
+
+
+def random_codes(rng, T, K, fmt):
+    """Any finite code."""
+    table = F.values(fmt)
+    fine = np.nonzero(np.isfinite(table))[0].astype(np.uint8)
+    return fine[rng.integers(0, len(fine), (T, K))]
+
+
+def product_case(rng, T, N, K, rows, x_fmt):
+    xq, wq = random_codes(rng, T, K, x_fmt), random_codes(rng, N, K, "e4m3")
+    kb = -(-K // 128)
+    sx = np.exp(rng.uniform(-8, 2, (kb, T))).astype(np.float32)
+    sw = np.exp(rng.uniform(-8, 2, (kb, -(-N // rows)))).astype(np.float32)
+    return xq, sx, wq, sw
+
+
+@pytest.mark.parametrize("T,N,K", SIZES)
+@pytest.mark.parametrize("rows,x_fmt", [(128, "e4m3"), (1, "e4m3"), (128, "e5m2"), (1, "e5m2")])
+@pytest.mark.parametrize("pad,shift", [(0, 0), (1, 3), (16, 16), (-1, 0)])
+def test_matmul(T, N, K, rows, x_fmt, pad, shift):
+    """pad -1: rows on 16-byte boundaries, whatever their width."""
+    rng = np.random.default_rng(T * 7919 + N * 31 + K + rows)
+    xq, sx, wq, sw = product_case(rng, T, N, K, rows, x_fmt)
+    pad = -K % 16 if pad < 0 else pad
+    bias = rand(rng, N) if (T + N) % 2 else None
+    out = ["f32", "bf16"][(T + K) % 2]
+    buf = torch.full((T * (N + 5) + 64,), 77, dtype=TORCH[out], device=DEV)
+    Y = buf[3:3 + T * (N + 5)].view(T, N + 5)[:, :N]
+    y = B.bsr_matmul_f8(codes(xq, x_fmt, pad, shift), held(torch.from_numpy(sx), 2, 1),
+                        codes(wq, "e4m3", pad, shift), held(torch.from_numpy(sw), 1, 3),
+                        None if bias is None else bias.to(DEV), Y=Y)
+    want, bound = F.matmul(xq, sx, wq, sw, rows, None if bias is None else bias.numpy(), x_fmt, out)
+    within(y, want, bound, "Y")
+    copy = buf.clone()
+    copy[3:3 + T * (N + 5)].view(T, N + 5)[:, :N] = 77
+    assert bool((copy == 77).all())
+    again = B.bsr_matmul_f8(codes(xq, x_fmt, pad, shift), torch.from_numpy(sx).to(DEV),
+                            codes(wq, "e4m3", pad, shift), torch.from_numpy(sw).to(DEV),
+                            None if bias is None else bias.to(DEV), out_dtype=TORCH[out])
+    assert torch.equal(again, y)
+
+
+@pytest.mark.parametrize("T,N,K", [(1, 48, 4096), (19, 70, 770), (200, 300, 1000), (600, 700, 512)])
+@pytest.mark.parametrize("rows", [1, 128])
+def test_matmul_exact(T, N, K, rows):
+    """Small integers and scales that are powers of two: every product and sum is exact."""
+    rng = np.random.default_rng(K)
+    x, w = (rng.integers(-4, 5, s).astype(np.float32) for s in ((T, K), (N, K)))
+    kb = -(-K // 128)
+    sx = (2.0 ** rng.integers(-1, 2, (kb, T))).astype(np.float32)
+    sw = (2.0 ** rng.integers(-1, 2, (kb, -(-N // rows)))).astype(np.float32)
+    xq, wq = F.encode(x, "e4m3"), F.encode(w, "e4m3")
+    Y = B.bsr_matmul_f8(codes(xq, "e4m3"), torch.from_numpy(sx).to(DEV), codes(wq, "e4m3"),
+                        torch.from_numpy(sw).to(DEV))
+    want, _ = F.matmul(xq, sx, wq, sw, rows)
+    assert np.array_equal(f64(Y), want)
+
+
+@pytest.mark.parametrize("T,N,K", [(5, 40, 300), (150, 200, 300), (700, 600, 1024)])
+def test_matmul_not_finite(T, N, K):
+    """A NaN or infinite scale, or a NaN code, reaches every output of its token or channel and no other;
+    what lies between the rows reaches none."""
+    rng = np.random.default_rng(3)
+    xq, sx, wq, sw = product_case(rng, T, N, K, 1, "e5m2")
+    clean = F.matmul(xq, sx, wq, sw, 1, x_fmt="e5m2")
+    sx[0, 1], sx[1, 3], sw[2, 7] = np.nan, np.inf, np.nan
+    xq[1], xq[3], xq[4, K - 1], wq[11, 17] = 0, 0, 0x7F, 0x7F
+    Y = f64(B.bsr_matmul_f8(codes(xq, "e5m2", 5), torch.from_numpy(sx).to(DEV), codes(wq, "e4m3", 5),
+                            torch.from_numpy(sw).to(DEV)))
+    bad = np.zeros((T, N), bool)
+    bad[[1, 3, 4]] = True
+    bad[:, [7, 11]] = True
+    assert np.array_equal(np.isnan(Y), bad)
+    assert np.all((np.abs(Y - clean[0]) <= clean[1])[~bad])
+
+
+def test_matmul_of_views():
+    """Tokens, blocks and channels cut out of larger matrices, with the scales' views."""
+    rng = np.random.default_rng(8)
+    xq, sx, wq, sw = product_case(rng, 96, 512, 1024, 128, "e4m3")
+    X, SX = codes(xq, "e4m3"), torch.from_numpy(sx).to(DEV)
+    W, SW = codes(wq, "e4m3"), torch.from_numpy(sw).to(DEV)
+    t, k, n = slice(5, 78), slice(256, 1000), slice(128, 470)
+    Y = B.bsr_matmul_f8(X[t, k], SX[2:8, t], W[n, k], SW[2:8, 1:4])
+    want, bound = F.matmul(xq[t, k], sx[2:8, t], wq[n, k], sw[2:8, 1:4], 128)
+    within(Y, want, bound, "Y")
+    assert B.bsr_matmul_f8(X[:0], SX[:, :0], W, SW).shape == (0, 512)
+
+
+@pytest.mark.parametrize("T,N", [(3, 130), (260, 130)])
+def test_matmul_long_offsets(T, N):
+    """Rows and outputs beyond 2^31 bytes from the first, for the tokens and the channels."""
+    rng = np.random.default_rng(12)
+    K, pitch = 272, 1 << 20
+    rows_x, rows_w = (T, 2600) if T < 100 else (2600, 130)
+    xq, wq = random_codes(rng, rows_x, K, "e4m3"), random_codes(rng, rows_w, K, "e4m3")
+
+    def far(q):
+        buf = torch.full((len(q) * pitch,), 0x7F, dtype=torch.uint8, device=DEV).view(len(q), pitch)[:, :K]
+        buf.copy_(torch.from_numpy(q))
+        return buf.view(F8["e4m3"])
+    sx = np.exp(rng.uniform(-3, 0, (3, rows_x))).astype(np.float32)
+    sw = np.exp(rng.uniform(-3, 0, (3, -(-rows_w // 128)))).astype(np.float32)
+    Y = B.bsr_matmul_f8(far(xq), torch.from_numpy(sx).to(DEV), far(wq), torch.from_numpy(sw).to(DEV))
+    want, bound = F.matmul(xq, sx, wq, sw, 128)
+    within(Y, want, bound, "Y")
+
+
+def test_matmul_many_columns_of_scales():
+    """Scales whose pitch puts a block's beyond 2^31 bytes from the first."""
+    rng = np.random.default_rng(13)
+    T, N, K, pitch = 40, 70, 128 * 40, 1 << 24
+    xq, sx, wq, sw = product_case(rng, T, N, K, 1, "e4m3")
+    buf = torch.empty(40 * pitch, device=DEV).view(40, pitch)
+    S, SW = buf[:, :T], buf[:, 1 << 20:(1 << 20) + N]
+    S.copy_(torch.from_numpy(sx))
+    SW.copy_(torch.from_numpy(sw))
+    want, bound = F.matmul(xq, sx, wq, sw, 1)
+    within(B.bsr_matmul_f8(codes(xq, "e4m3"), S, codes(wq, "e4m3"), SW), want, bound, "Y")
+    T2 = 12                                           # few tokens
+    within(B.bsr_matmul_f8(codes(xq[:T2], "e4m3"), S[:, :T2], codes(wq, "e4m3"), SW), want[:T2],
+           bound[:T2], "Y")
+
+
+def test_streams_and_graphs():
+    rng = np.random.default_rng(14)
+    xs = [rand(rng, 300, 640, dtype="bf16").to(DEV) for _ in range(3)]
+    w = B.bsr_quantize_f8(rand(rng, 256, 640, sigma=0.02).to(DEV), 128)
+    eager = [B.bsr_matmul_f8(*B.bsr_quantize_f8(x), *w) for x in xs]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    other = B.bsr_matmul_f8(*B.bsr_quantize_f8(xs[0], stream=side), *w, stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(other, eager[0])
+    X = xs[0].clone()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        Y = B.bsr_matmul_f8(*B.bsr_quantize_f8(X), *w)
+    for i in (1, 2, 0, 1):
+        X.copy_(xs[i])
+        graph.replay()
+        again = B.bsr_matmul_f8(*B.bsr_quantize_f8(xs[i]), *w)
+        torch.cuda.synchronize()
+        assert torch.equal(Y, eager[i]) and torch.equal(again, eager[i])
+
+
+# --- a layer with its norm, as it is trained -----------------------------------------------------
+
+def test_layer_step():
+    """h = norm(x + r), y = h W^T in 8 bits, and from dy the gradients of W, x, gamma and beta: every stage
+    against its oracle on the stage's own inputs, and the ends against the step without rounding to 8
+    bits, whose codes are off by at most 2^-4 of their value, or 2^-10 of the block's scale below the
+    least exponent."""
+    rng = np.random.default_rng(21)
+    T, K, Nn = 333, 770, 520
+    x, r = rand(rng, T, K).to(DEV), rand(rng, T, K).to(DEV)
+    gamma, beta = (rand(rng, K, sigma=0.1) + 1.0).to(DEV), rand(rng, K, sigma=0.1).to(DEV)
+    W, dy = rand(rng, Nn, K, sigma=0.02).to(DEV), rand(rng, T, Nn, sigma=0.1).to(DEV)
+    h, s, mean, rstd = B.bsr_layer_norm(x, gamma, beta, R=r, save=True)
+    hq, sh, hqt, sht = B.bsr_quantize_f8(h, form="both")
+    wq, sw, wqt, swt = B.bsr_quantize_f8(W, 128, form="both")
+    y = B.bsr_matmul_f8(hq, sh, wq, sw)
+    dq, sd, dqt, sdt = B.bsr_quantize_f8(dy, form="both")
+    dh = B.bsr_matmul_f8(dq, sd, wqt, swt)
+    dW = B.bsr_matmul_f8(dqt, sdt, hqt, sht)
+    dx, dgamma, dbeta = B.bsr_layer_norm_backward(dh, s, mean, rstd, gamma)
+    for got, ops, rows in ((y, (hq, sh, wq, sw), 128), (dh, (dq, sd, wqt, swt), 128),
+                           (dW, (dqt, sdt, hqt, sht), 1)):
+        a = [bits(t) if i % 2 == 0 else host(t) for i, t in enumerate(ops)]
+        within(got, *F.matmul(*a, rows), "product")
+    from oracle import norm_oracle as N
+    want = N.backward(f64(dh), f64(s), f64(mean), f64(rstd), f64(gamma))
+    for name, got in (("dX", dx), ("dgamma", dgamma), ("dbeta", dbeta)):
+        within(got, *want[name], name)
+
+    def off(a, scale, rows):        # how far the codes of a may be from it
+        at, to = np.arange(a.shape[1]) // 128, np.arange(a.shape[0]) // rows
+        return 2.0 ** -4 * np.abs(a) + 2.0 ** -10 * host(scale).astype(np.float64)[at][:, to].T
+
+    for got, (a, sa, ra), (b, sb, rb) in (
+            (y, (f64(h), sh, 1), (f64(W), sw, 128)), (dh, (f64(dy), sd, 1), (f64(W).T, swt, 128)),
+            (dW, (f64(dy).T, sdt, 1), (f64(h).T, sht, 1))):
+        ea, eb = off(a, sa, ra) * 1.001, off(b, sb, rb) * 1.001
+        bound = ea @ np.abs(b).T + np.abs(a) @ eb.T + ea @ eb.T
+        bound += (a.shape[1] + 4) * 2.0 ** -24 * ((np.abs(a) + ea) @ (np.abs(b) + eb).T)
+        within(got, a @ b.T, bound, "step")

@@ -1,0 +1,219 @@
+"""The layer norm and its gradients on the GPU against the fp64 oracle, within bounds that count the
+roundings (oracle/norm_oracle.py).  Sizes straddle what a wave and a workgroup hold, rows start at no
+particular alignment, pitches exceed widths, and the gaps between rows hold NaN on the way in and a
+sentinel on the way out."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import norm_oracle as N
+from paper_2106_08846_amd import bsr as B
+from tests.test_gpu_dense import DEV, TORCH, f64, frame, held, rand
+
+pytestmark = pytest.mark.gpu
+
+SIZES = [(1, 1), (1, 7), (3, 64), (5, 511), (4, 512), (17, 768), (2, 1024), (9, 1025), (33, 4096),
+         (6, 4097), (3, 16384), (2, 16385), (2, 70001), (1000, 96), (2053, 24)]
+
+
+def to_type(dtype):
+    return lambda a: torch.from_numpy(a).to(TORCH[dtype]).float().numpy()
+
+
+def within(got, want, bound, what):
+    err = np.abs(f64(got) - want)
+    assert np.all(np.isfinite(f64(got))), what
+    assert np.all(err <= bound), (what, float(np.max(err / bound)))
+
+
+def operands(rng, T, K, dtype, affine=True):
+    x = rand(rng, T, K, dtype=dtype) + 0.5
+    r = rand(rng, T, K, sigma=2.0, dtype=dtype)
+    gamma = rand(rng, K) + 1.0 if affine else None
+    beta = rand(rng, K) if affine else None
+    return x, r, gamma, beta
+
+
+def dev(t):
+    return None if t is None else t.to(DEV)
+
+
+@pytest.mark.parametrize("T,K", SIZES)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("pad,shift,residual", [(0, 0, True), (3, 1, False), (16, 8, True), (1, 3, True)])
+def test_norm(T, K, dtype, pad, shift, residual):
+    rng = np.random.default_rng(T * 100003 + K)
+    affine = (T + K) % 3 > 0
+    x, r, gamma, beta = operands(rng, T, K, dtype, affine)
+    R = held(r, pad, shift) if residual else None
+    Y, clean = frame(T, K, TORCH[dtype], pad, shift)
+    S, clean_s = frame(T, K, TORCH[dtype], pad + 1, shift) if residual else (None, None)
+    y, s, mean, rstd = B.bsr_layer_norm(held(x, pad, shift), dev(gamma), dev(beta), R=R, eps=1e-5,
+                                        save=True, Y=Y, S=S)
+    want_s = N.residual_sum(x.float().numpy(), r.float().numpy() if residual else None, to_type(dtype))
+    assert np.array_equal(f64(s).astype(np.float32), want_s)
+    want, bound = N.layer_norm(want_s, None if gamma is None else gamma.numpy(),
+                               None if beta is None else beta.numpy(), 1e-5, dtype)
+    within(y, want, bound, "Y")
+    m, rs, _, e_mean, r_rstd = N.statistics(want_s, 1e-5)
+    within(mean, m[:, 0], e_mean[:, 0], "mean")
+    within(rstd, rs[:, 0], (rs * r_rstd)[:, 0], "rstd")
+    assert clean() and (clean_s is None or clean_s())
+    # without the statistics, and with outputs of the binding: the same bits
+    again = B.bsr_layer_norm(held(x, 0, 0), dev(gamma), dev(beta), R=R)
+    assert torch.equal(again, y)
+
+
+@pytest.mark.parametrize("T,K", SIZES)
+@pytest.mark.parametrize("dtype,grad", [("f32", "f32"), ("bf16", "f32"), ("bf16", "bf16")])
+@pytest.mark.parametrize("pad,shift,extra", [(0, 0, True), (3, 1, False), (16, 8, True)])
+def test_backward(T, K, dtype, grad, pad, shift, extra):
+    rng = np.random.default_rng(T * 7919 + K)
+    affine = (T + K) % 3 > 0
+    x, dy, gamma, beta = operands(rng, T, K, dtype, affine)
+    ds = rand(rng, T, K, sigma=0.3, dtype=dtype)
+    X = held(x, pad, shift)
+    _, S, mean, rstd = B.bsr_layer_norm(X, dev(gamma), dev(beta), save=True)
+    assert S is X
+    dX, clean = frame(T, K, TORCH[dtype], pad, shift)
+    got = dict(zip(("dX", "dgamma", "dbeta"), B.bsr_layer_norm_backward(
+        held(dy, pad, shift), S, mean, rstd, dev(gamma), dS=held(ds, pad, shift) if extra else None,
+        dX=dX, grad_dtype=TORCH[grad])))
+    want = N.backward(f64(dy), f64(x), f64(mean), f64(rstd), None if gamma is None else gamma.numpy(),
+                      f64(ds) if extra else None, dtype, grad)
+    for name, (value, bound) in want.items():
+        within(got[name], value, bound, name)
+    assert clean()
+
+
+@pytest.mark.parametrize("T,K", [(37, 768), (9, 2050), (4, 20000)])
+def test_parts_of_the_gradients(T, K):
+    """Each gradient alone has the bits of all of them together; the workspace may be the caller's."""
+    rng = np.random.default_rng(11)
+    x, dy, gamma, _ = operands(rng, T, K, "bf16")
+    X, dY, g = dev(x), dev(dy), dev(gamma)
+    _, S, mean, rstd = B.bsr_layer_norm(X, g, save=True)
+    dX, dg, db = B.bsr_layer_norm_backward(dY, S, mean, rstd, g, grad_dtype=torch.float32)
+    only, none, none2 = B.bsr_layer_norm_backward(dY, S, mean, rstd, g, affine=False)
+    assert none is None and none2 is None and torch.equal(only, dX)
+    ws = torch.full((B.bsr_layer_norm_workspace_bytes(T, K) + 64,), 255, dtype=torch.uint8, device=DEV)
+    none, dg2, db2 = B.bsr_layer_norm_backward(dY, S, mean, rstd, g, grad_dtype=torch.float32,
+                                               need_dX=False, workspace=ws)
+    assert none is None and torch.equal(dg2, dg) and torch.equal(db2, db)
+    assert bool((ws[-64:] == 255).all())
+    db3 = torch.empty(K, device=DEV)
+    _, none, db4 = B.bsr_layer_norm_backward(dY, S, mean, rstd, g, affine=False, dbeta=db3, need_dX=False)
+    assert none is None and db4 is db3 and torch.equal(db3, db)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_no_tokens(dtype):
+    X = torch.empty(0, 96, dtype=TORCH[dtype], device=DEV)
+    Y, S, mean, rstd = B.bsr_layer_norm(X, save=True)
+    assert Y.shape == (0, 96) and mean.shape == (0,)
+    dX, dg, db = B.bsr_layer_norm_backward(X, S, mean, rstd)
+    assert dX.shape == (0, 96) and not bool(dg.any()) and not bool(db.any())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("K", [5, 768, 4500])
+def test_special_rows(dtype, K):
+    x = np.random.default_rng(5).standard_normal((10, K)).astype(np.float32)
+    x[0] = 3.0                                       # no variance: Y is beta
+    x[1] = 0.0
+    x[2, K - 1] = np.inf
+    x[3, 0] = np.nan
+    x[4, 0], x[4, 1] = np.inf, -np.inf
+    x[5] *= np.float32(2.0 ** -70)                   # squares that vanish beside eps
+    x[6] *= np.float32(2.0 ** 90)                    # squares beyond fp32: rstd is 0
+    x[7] += 1000.0                                   # far from zero
+    t = torch.from_numpy(x).to(TORCH[dtype])
+    beta = torch.linspace(-1, 1, K)
+    Y, S, mean, rstd = B.bsr_layer_norm(t.to(DEV), None, beta.to(DEV), save=True)
+    y = f64(Y)
+    want, bound = N.layer_norm(t.double().numpy(), None, beta.numpy(), 1e-5, dtype)
+    for row in (0, 1, 5, 7, 8, 9):
+        assert np.all(np.abs(y[row] - want[row]) <= bound[row]), row
+    assert np.all(np.isnan(y[2:5]).any(1)) and np.all(np.isnan(f64(rstd)[2:5]))
+    assert f64(rstd)[6] == 0.0 and np.array_equal(y[6], f64(beta.to(TORCH[dtype])))
+    dX = B.bsr_layer_norm_backward(torch.ones_like(S), S, mean, rstd)[0]
+    assert np.all(np.isfinite(f64(dX)[[0, 1, 5, 6, 7, 8, 9]]))
+
+
+def test_offset_rows_keep_their_variance():
+    """Rows of 4096 values 1000 from zero with deviations of 2^-6: the mean of the squares alone would
+    lose the variance in fp32."""
+    rng = np.random.default_rng(2)
+    x = (1000.0 + rng.integers(-4, 5, (3, 4096)) * 2.0 ** -8).astype(np.float32)
+    Y = B.bsr_layer_norm(torch.from_numpy(x).to(DEV))
+    want, bound = N.layer_norm(x)
+    # the computed mean is off by up to e_mean of the magnitude 1000; the rest of the bound is small
+    within(Y, want, bound, "Y")
+    assert abs(float(Y.double().std()) - float(want.std())) < 0.01
+
+
+def test_long_offsets():
+    """Rows beyond 2^31 elements from the first."""
+    T, K, pitch = 2200, 72, 1 << 20
+    rng = np.random.default_rng(9)
+    x = rand(rng, T, K, dtype="bf16")
+    buf = torch.empty(T * pitch, dtype=torch.bfloat16, device=DEV)
+    out = torch.empty(T * pitch, dtype=torch.bfloat16, device=DEV)
+    X, Y = buf.view(T, pitch)[:, :K], out.view(T, pitch)[:, :K]
+    X.copy_(x)
+    _, S, mean, rstd = B.bsr_layer_norm(X, Y=Y, save=True)
+    want, bound = N.layer_norm(x.double().numpy(), out="bf16")
+    within(Y, want, bound, "Y")
+    dX, dg, db = B.bsr_layer_norm_backward(Y, S, mean, rstd, dX=Y[:, :K].clone(), grad_dtype=torch.float32)
+    got = N.backward(f64(Y), x.double().numpy(), f64(mean), f64(rstd), out="bf16")
+    within(dX, *got["dX"], "dX")
+    within(dg, *got["dgamma"], "dgamma")
+    within(db, *got["dbeta"], "dbeta")
+
+
+def test_repeated_calls_and_streams():
+    rng = np.random.default_rng(4)
+    x, dy, gamma, beta = operands(rng, 1500, 1030, "bf16")
+    X, dY, g, b = dev(x), dev(dy), dev(gamma), dev(beta)
+    first = B.bsr_layer_norm(X, g, b, R=dY, save=True)
+    grads = B.bsr_layer_norm_backward(dY, *first[1:], g)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for stream in (None, side):
+        again = B.bsr_layer_norm(X, g, b, R=dY, save=True, stream=stream)
+        more = B.bsr_layer_norm_backward(dY, *again[1:], g, stream=stream)
+        torch.cuda.synchronize()
+        for p, q in zip((*first, *grads), (*again, *more)):
+            assert torch.equal(p, q)
+
+
+def test_captured_steps():
+    """Forward and backward in a graph, replayed on other inputs with eager work between, two graphs with a
+    workspace each."""
+    rng = np.random.default_rng(6)
+    T, K = 700, 1536
+    g = dev(rand(rng, K) + 1.0)
+    xs = [dev(rand(rng, T, K, dtype="bf16")) for _ in range(4)]
+    graphs = []
+    for _ in range(2):
+        X, dY = torch.empty_like(xs[0]), torch.empty_like(xs[0])
+        X.copy_(xs[0])
+        dY.copy_(xs[1])
+        ws = torch.empty(B.bsr_layer_norm_workspace_bytes(T, K), dtype=torch.uint8, device=DEV)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = B.bsr_layer_norm(X, g, save=True)
+            grads = B.bsr_layer_norm_backward(dY, *out[1:], g, grad_dtype=torch.float32, workspace=ws)
+        graphs.append((graph, X, dY, out, grads))
+    for i in range(4):
+        for n, (graph, X, dY, out, grads) in enumerate(graphs):
+            x, dy = xs[(i + n) % 4], xs[(i + n + 1) % 4]
+            X.copy_(x)
+            dY.copy_(dy)
+            graph.replay()
+            want = B.bsr_layer_norm(x, g, save=True)
+            more = B.bsr_layer_norm_backward(dy, *want[1:], g, grad_dtype=torch.float32)
+            torch.cuda.synchronize()
+            for p, q in zip((out[0], *out[2:], *grads), (want[0], *want[2:], *more)):
+                assert torch.equal(p, q)
