@@ -70,113 +70,14 @@ __device__ __forceinline__ i32x8 join_chunks(i32x4 lo, i32x4 hi) {
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// BM x BN tile, WM x WN waves: operands go through registers into one of two LDS stages of one block
-// each, together with the scales of its rows.  WROWS: a scale for each row of B, else for 128.
-template <int BM, int BN, int WM, int WN, int XF, bool WROWS, bool WIDE> struct F8TileKernel {
-    static constexpr int kThreads = 64 * WM * WN;
-    static constexpr int TM = BM / WM, TN = BN / WN;
-    static constexpr int NM = TM / kMF, NN = TN / kMF;
-    static constexpr int kRowBytes = kF8Block, kRowChunks = kRowBytes / kChunk;
-    static constexpr int kRowsPerPass = kThreads / kRowChunks;
-    static constexpr int LA = BM / kRowsPerPass, LB = BN / kRowsPerPass;
-    static constexpr int kScales = BM + (WROWS ? BN : 0);
-    static constexpr int kStageBytes = (BM + BN) * kRowBytes + kScales * 4;
-    static constexpr int kEpiBytes = WM * WN * epilogue_bytes(NN);
-    static constexpr int kLds = 2 * kStageBytes > kEpiBytes ? 2 * kStageBytes : kEpiBytes;
-    static constexpr int kTileN = BN;
-    static_assert(BM % kRowsPerPass == 0 && BN % kRowsPerPass == 0 && BM <= kThreads && BN <= kThreads,
-                  "whole passes");
-    static_assert(kF8Block % TN == 0 && kStageBytes % 16 == 0, "one scale of B for a wave's channels");
-
-    static __device__ __forceinline__ int swizzled(int row, int c) { return c ^ ((row >> 1) & 7); }
-
-    static __device__ __forceinline__ void run(const F8Args &args, char *lds) {
-        const ProductArgs &a = args.p;
-        const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
-        const int wm = wave % WM, wn = wave / WM;
-        const TileRows<BM, kTileN, false> rows(a);
-        const int c = tid & (kRowChunks - 1), r0 = tid / kRowChunks;
-        i32x4 ha[LA], hb[LB];
-        float hx = 0.0f, hw = 0.0f;
-        RowChunks<int8_t, Load::kBytes> ca[LA], cb[LB];
+// The first n bytes of v (0 <= n <= 16), the others 0.
+__device__ __forceinline__ i32x4 first_bytes(i32x4 v, int n) {
 #pragma unroll
-        for (int i = 0; i < LA; ++i) ca[i].set(rows.a, i * kRowsPerPass + r0, c * kChunk, a.Kb);
-#pragma unroll
-        for (int i = 0; i < LB; ++i) cb[i].set(rows.b0, i * kRowsPerPass + r0, c * kChunk, a.Kb);
-        const int steps = (a.Kb + kRowBytes - 1) / kRowBytes;
-        const bool has_x = tid < BM && rows.m0 + tid < a.M;
-        const bool has_w = WROWS && tid < BN && rows.n0 + tid < a.N;
-        // The wave's channels share a scale where B has one for 128 rows; beyond the last, any.
-        const int64_t n_wave = rows.n0 + wn * TN;
-        const float *sw = args.sw + (WROWS ? rows.n0 : (n_wave < a.N ? n_wave : a.N - 1) / kF8Block);
-        auto load = [&](int step) {                // zeros from Kb on
-            const int kb = step * kRowBytes, left = a.Kb - c * kChunk - kb;
-#pragma unroll
-            for (int i = 0; i < LA; ++i) ha[i] = ca[i].load(kb, left);
-#pragma unroll
-            for (int i = 0; i < LB; ++i) hb[i] = cb[i].load(kb, left);
-            if (has_x && step < steps) hx = args.sx[step * args.ldsx + rows.m0 + tid];
-            if (has_w && step < steps) hw = sw[step * args.ldsw + tid];
-        };
-        auto put = [&](int buf) {
-            char *p = lds + buf * kStageBytes;
-#pragma unroll
-            for (int i = 0; i < LA + LB; ++i) {
-                const int row = (i < LA ? i : i - LA) * kRowsPerPass + r0;
-                *reinterpret_cast<i32x4 *>(p + (i < LA ? 0 : BM * kRowBytes) + row * kRowBytes +
-                                           swizzled(row, c) * kChunk) = i < LA ? ha[i] : hb[i - LA];
-            }
-            float *s = reinterpret_cast<float *>(p + (BM + BN) * kRowBytes);
-            if (tid < BM) s[tid] = hx;
-            if (WROWS && tid < BN) s[BM + tid] = hw;
-        };
-        f32x4 acc[NN][NM] = {};
-        const int fr = lane % kMF, fc = lane / kMF;
-        load(0);
-        put(0);
-        load(1);
-        for (int s = 0; s < steps; ++s) {
-            const float one = WROWS ? 0.0f : sw[s * args.ldsw];
-            __syncthreads();
-            const char *p = lds + (s & 1) * kStageBytes;
-            const float *scale = reinterpret_cast<const float *>(p + (BM + BN) * kRowBytes);
-            auto fetch = [&](int row) {
-                const char *q = p + row * kRowBytes;
-                return join_chunks(*reinterpret_cast<const i32x4 *>(q + swizzled(fr, fc) * kChunk),
-                                   *reinterpret_cast<const i32x4 *>(q + swizzled(fr, fc + 4) * kChunk));
-            };
-            F8Fragment<BSR_E4M3, WIDE> fb[NN];
-#pragma unroll
-            for (int j = 0; j < NN; ++j) fb[j].set(fetch(BM + wn * TN + j * kMF + fr));
-#pragma unroll
-            for (int i = 0; i < NM; ++i) {
-                F8Fragment<XF, WIDE> fa;
-                fa.set(fetch(wm * TM + i * kMF + fr));
-                const float sx = scale[wm * TM + i * kMF + fr];
-#pragma unroll
-                for (int j = 0; j < NN; ++j) {
-                    f32x4 of = {one, one, one, one};
-                    if constexpr (WROWS)
-                        of = *reinterpret_cast<const f32x4 *>(scale + BM + wn * TN + j * kMF + 4 * fc);
-                    const f32x4 sum = block_sums<XF>(fb[j], fa);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[j][i][e] = fmaf(sum[e], sx * of[e], acc[j][i][e]);
-                }
-            }
-            put((s + 1) & 1);
-            load(s + 2);
-        }
-        __syncthreads();
-        epilogue<bf16, Out::kScale, NN, NM>(a, acc, reinterpret_cast<float *>(lds + wave * epilogue_bytes(NN)),
-                                            rows.m0 + wm * TM, rows.n0 + wn * TN);
+    for (int i = 0; i < 4; ++i) {
+        const int left = n - 4 * i;
+        v[i] = left >= 4 ? v[i] : left <= 0 ? 0 : v[i] & int((1u << (8 * left)) - 1u);
     }
-};
-
-template <int BM, int BN, int WM, int WN, int XF, bool WROWS, bool WIDE>
-__global__ __launch_bounds__(64 * WM * WN) void f8_tile_kernel(F8Args a) {
-    using K = F8TileKernel<BM, BN, WM, WN, XF, WROWS, WIDE>;
-    __shared__ __align__(16) char lds[K::kLds];
-    K::run(a, lds);
+    return v;
 }
 
 }  // namespace bsr

@@ -1,6 +1,7 @@
 // Launches of the 8-bit floating-point product.
-#include "dense_plan.h"
-#include "f8_product.h"
+#include "f8_plan.h"
+#include "f8_ring.h"
+#include "f8_rows.h"
 
 namespace bsr {
 
@@ -13,9 +14,68 @@ template <class K, int BM> void launch_tiles(void (*kernel)(F8Args), F8Args a, v
                        as_stream(stream), a);
 }
 
+template <int BM, int BN, int WM, int WN, int XF, bool WROWS, bool WIDE, bool DIRECT>
+void launch_ring(const F8Args &a, void *stream) {
+    launch_tiles<F8RingKernel<BM, BN, WM, WN, XF, WROWS, WIDE, DIRECT>, BM>(
+        f8_ring_kernel<BM, BN, WM, WN, XF, WROWS, WIDE, DIRECT>, a, stream);
+}
+template <int XF, bool WROWS, bool WIDE, bool DIRECT> void launch_tile(const F8Args &a, int tile, void *stream) {
+    constexpr F8Cost cost = kF8Costs[DIRECT ? 1 : 0][WIDE ? 1 : 0][WROWS ? 1 : 0];
+    switch (tile) {
+        case 0:
+            if constexpr (cost.round[0] > 0)
+                return launch_ring<256, 256, 2, 4, XF, WROWS, WIDE, DIRECT>(a, stream);
+            break;
+        case 1:
+            if constexpr (cost.round[1] > 0)
+                return launch_ring<192, 256, 2, 4, XF, WROWS, WIDE, DIRECT>(a, stream);
+            break;
+        case 2: return launch_ring<128, 256, 2, 4, XF, WROWS, WIDE, DIRECT>(a, stream);
+        case 3: return launch_ring<128, 128, 2, 4, XF, WROWS, WIDE, DIRECT>(a, stream);
+        default: return launch_ring<64, 64, 2, 2, XF, WROWS, WIDE, DIRECT>(a, stream);
+    }
+}
+
+// The product's channels from n on (a multiple of 128), as a product of its own.
+F8Args channels_from(F8Args a, int64_t n, bool w_rows) {
+    a.p.B0 += n * a.p.ldb0;
+    a.p.b0 = a.p.b0 ? a.p.b0 + n : nullptr;
+    a.p.out = static_cast<char *>(a.p.out) + n * (a.p.out_bf16 ? 2 : 4);
+    a.p.N -= n;
+    a.sw += w_rows ? n : n / kF8Block;
+    return a;
+}
+
+bool rows_aligned(const void *p, int64_t ld) {
+    return ((reinterpret_cast<uintptr_t>(p) | uintptr_t(ld)) & 15) == 0;
+}
+
+template <int NT, int XF, bool WROWS> void launch_rows(const F8Args &a, bool aligned, void *stream) {
+    using K = F8RowsKernel<NT, XF, WROWS, true>;
+    const auto kernel = aligned ? f8_rows_kernel<NT, XF, WROWS, true> : f8_rows_kernel<NT, XF, WROWS, false>;
+    const unsigned groups_n = unsigned((a.p.N + K::kChannels - 1) / K::kChannels);
+    const unsigned groups_m = unsigned((a.p.M + 16 * NT - 1) / (16 * NT));
+    hipLaunchKernelGGL(kernel, dim3(groups_n, groups_m), dim3(64 * K::kWaves), 0, as_stream(stream), a);
+}
+
 template <int XF, bool WROWS, bool WIDE> void product(const F8Args &a, void *stream) {
-    launch_tiles<F8TileKernel<64, 64, 2, 2, XF, WROWS, WIDE>, 64>(
-        f8_tile_kernel<64, 64, 2, 2, XF, WROWS, WIDE>, a, stream);
+    const bool aligned = rows_aligned(a.p.A, a.p.lda) && rows_aligned(a.p.B0, a.p.ldb0);
+    const int64_t cus = device_cu_count(), M = a.p.M;
+    // 64 x 1024 x 4096 takes 9 us there and 14 in tiles (fp32 output 21), 128 x 1024 x 8192 14 and 25; two
+    // rounds of it, 32 x 12288 x 4096, 20 and 19 (fp32 22).
+    if (f8_few_tokens(M, a.p.N, cus))
+        return M <= 16 ? launch_rows<1, XF, WROWS>(a, aligned, stream)
+                       : launch_rows<2, XF, WROWS>(a, aligned, stream);
+    const F8Cost &cost = f8_cost(aligned, WIDE, WROWS);
+    const auto launch = aligned ? launch_tile<XF, WROWS, WIDE, true> : launch_tile<XF, WROWS, WIDE, false>;
+    const int large = f8_largest(cost);
+    const int64_t whole = f8_whole_rounds(cost, large, M, a.p.N, cus);
+    if (whole == 0) return launch(a, f8_tile(cost, M, a.p.N, cus), stream);
+    const F8Args rest = channels_from(a, whole, WROWS);
+    F8Args first = a;
+    first.p.N = whole;
+    launch(first, large, stream);
+    launch(rest, f8_tile(cost, M, rest.p.N, cus), stream);
 }
 template <int XF> void product(const F8Args &a, bool w_rows, void *stream) {
     const auto f = w_rows ? (a.p.out_bf16 ? product<XF, true, false> : product<XF, true, true>)

@@ -1,0 +1,261 @@
+// The product of 8-bit floating-point matrices (f8_product.h) in tiles.  LDS holds two stages of one block
+// of 128 columns each, with the block's scales.
+//
+// A wave's order of work in a block: token fragment i meets the channel fragments j in turn.  The sums of
+// (i, j) are added to the outputs while the matrix unit forms those of the next pair.  A token fragment is
+// read from LDS two i before its use, a channel fragment as soon as its last product is issued, so the
+// reads of a block end two i before its products do: there every wave waits for the next block's data
+// and meets the others, and the loads of the block after that go into the stage that is free from then on.
+// They have a whole block's products to arrive.
+//
+// DIRECT (rows on 16-byte boundaries): codes go straight from memory into LDS.  Otherwise they go through
+// registers, loaded at the same point and written shortly before the next meeting.
+#pragma once
+
+#include <type_traits>
+
+#include "f8_product.h"
+
+namespace bsr {
+
+template <int BM, int BN, int WM, int WN, int XF, bool WROWS, bool WIDE, bool DIRECT> struct F8RingKernel {
+    static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves;
+    static constexpr int TM = BM / WM, TN = BN / WN;
+    static constexpr int NM = TM / kMF, NN = TN / kMF;
+    static constexpr int kRowBytes = kF8Block;
+    // A load of a wave is 8 rows of 128 bytes.  Scales: 64 of a load, in as many loads for either operand.
+    static constexpr int PA = BM / 8 / kWaves, PB = BN / 8 / kWaves;
+    static constexpr int kScaleLoadsX = BM / 64, kScaleLoadsW = WROWS ? BN / 64 : 1;
+    static constexpr int kScaleAt = (BM + BN) * kRowBytes, kScaleWAt = kScaleAt + BM * 4;
+    static constexpr int kStageBytes = kScaleWAt + kScaleLoadsW * 256;
+    static constexpr int kEpiBytes = kWaves * epilogue_bytes(NN);
+    static constexpr int kLds = 2 * kStageBytes > kEpiBytes ? 2 * kStageBytes : kEpiBytes;
+    static constexpr int kTileN = BN;
+    static_assert(BM % (8 * kWaves) == 0 && BN % (8 * kWaves) == 0 && BM % 64 == 0, "whole loads");
+    static_assert(kScaleLoadsX + kScaleLoadsW <= 2 * kWaves, "two scale loads of a wave at most");
+    static_assert(kF8Block % TN == 0 && NM >= 2, "one scale of B for a wave's channels");
+    static_assert(kLds <= 160 * 1024, "LDS of a CU");
+
+    typedef __attribute__((address_space(3))) char lds_char;
+    typedef __attribute__((address_space(3))) void lds_void;
+
+    static __device__ __forceinline__ int swizzled(int row, int c) { return c ^ ((row >> 1) & 7); }
+    static __device__ __forceinline__ void pin() { asm volatile("" ::: "memory"); }
+
+    static __device__ __forceinline__ void run(const F8Args &args, char *lds) {
+        const ProductArgs &a = args.p;
+        const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+        const int wm = wave % WM, wn = wave / WM;
+        const TileRows<BM, kTileN, false> rows(a);
+        const Source &sa = rows.a, &sb = rows.b0;
+        constexpr unsigned kOut = 0x80000000u;      // out of every range: loads zeros
+        // The last row's end is rounded up to the dword that holds it, which the range check would drop.
+        const auto end = [&](const Source &s) {
+            return (unsigned((s.rows - 1) * s.pitch) + unsigned(a.Kb) + 3u) & ~3u;
+        };
+        const auto rsa = buffer_rsrc(sa.base, end(sa)), rsb = buffer_rsrc(sb.base, end(sb));
+        // A lane's place in a load's 8 rows, and the chunk of the row that belongs there, the same for all of
+        // its loads (a multiple of 16 rows apart).  Rows that do not exist begin past the range's end.
+        static_assert(kWaves % 2 == 0, "loads of a wave a multiple of 16 rows apart");
+        const int row0 = wave * 8 + (lane >> 3), c0 = swizzled(row0, lane & 7) * kChunk;
+        const unsigned oa = unsigned(row0) * unsigned(sa.pitch) + c0;
+        const unsigned ob = unsigned(row0) * unsigned(sb.pitch) + c0;
+        const int64_t left_m = a.M - rows.m0, left_n = a.N - rows.n0;
+        const int w_first = int(WROWS ? 0 : rows.n0 / kF8Block);
+        const float *sx = args.sx + rows.m0, *sw = args.sw + (WROWS ? rows.n0 : w_first);
+        const unsigned bytes_x = unsigned(left_m < BM ? left_m : BM) * 4;
+        const unsigned bytes_w = WROWS ? unsigned(left_n < BN ? left_n : BN) * 4
+                                       : unsigned((a.N - 1) / kF8Block - w_first + 1 < (BN + 127) / 128
+                                                      ? (a.N - 1) / kF8Block - w_first + 1
+                                                      : (BN + 127) / 128) * 4;
+        const int steps = (a.Kb + kRowBytes - 1) / kRowBytes;
+        // The codes of a step into its stage.
+        auto load = [&](int step) {
+            const int kb = step * kRowBytes;
+            lds_char *stage = (lds_char *)lds + (step & 1) * kStageBytes + wave * 1024;
+            const bool in = kb + c0 < a.Kb;              // chunks past the row's end: zeros
+            const unsigned va = in ? oa : kOut, vb = in ? ob : kOut;
+#pragma unroll
+            for (int i = 0; i < PA; ++i)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsa, (lds_void *)(stage + i * kWaves * 1024), 16, va,
+                                                         kb + i * kWaves * 8 * int(sa.pitch), 0, 0);
+            stage += BM * kRowBytes;
+#pragma unroll
+            for (int i = 0; i < PB; ++i)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsb, (lds_void *)(stage + i * kWaves * 1024), 16, vb,
+                                                         kb + i * kWaves * 8 * int(sb.pitch), 0, 0);
+        };
+        auto load_scales = [&](int step) {
+            lds_char *stage = (lds_char *)lds + (step & 1) * kStageBytes + kScaleAt;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int n = i * kWaves + wave;
+                if (n < kScaleLoadsX)
+                    __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                        buffer_rsrc(sx + step * args.ldsx, bytes_x), (lds_void *)(stage + n * 256), 4,
+                        n * 256 + lane * 4, 0, 0, 0);
+                else if (n < kScaleLoadsX + kScaleLoadsW)
+                    __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                        buffer_rsrc(sw + step * args.ldsw, bytes_w),
+                        (lds_void *)(stage + BM * 4 + (n - kScaleLoadsX) * 256), 4,
+                        (n - kScaleLoadsX) * 256 + lane * 4, 0, 0, 0);
+            }
+        };
+        // !DIRECT: the codes of a step on their way through registers, in the same places.  Rows that do not
+        // exist stand for the last one: they reach only outputs that do not exist.
+        i32x4 held[DIRECT ? 1 : PA + PB];
+        RowChunks<int8_t, Load::kBytes> chunk[DIRECT ? 1 : PA + PB];
+        if constexpr (!DIRECT) {
+#pragma unroll
+            for (int i = 0; i < PA + PB; ++i)
+                chunk[i].set(i < PA ? sa : sb, row0 + (i < PA ? i : i - PA) * kWaves * 8, c0, a.Kb);
+        }
+        auto take = [&](int step) {
+            const int kb = step * kRowBytes;
+            if (kb + kRowBytes <= a.Kb) {
+#pragma unroll
+                for (int i = 0; i < PA + PB; ++i) held[i] = chunk[i].load(kb, kChunk);
+            } else {
+#pragma unroll
+                for (int i = 0; i < PA + PB; ++i) held[i] = chunk[i].load(kb, a.Kb - c0 - kb);
+            }
+        };
+        auto put = [&](int step) {
+            char *p = lds + (step & 1) * kStageBytes + wave * 1024 + lane * kChunk;
+#pragma unroll
+            for (int i = 0; i < PA + PB; ++i)
+                *reinterpret_cast<i32x4 *>(p + (i < PA ? i : i - PA) * kWaves * 1024 +
+                                           (i < PA ? 0 : BM * kRowBytes)) = held[i];
+        };
+        // What lies beyond a row's end in its last chunk, replaced by zeros.
+        const int tail = DIRECT ? a.Kb % kChunk : 0;
+        auto clear_tail = [&](int step) {
+            char *p = lds + (step & 1) * kStageBytes;
+            const int c = a.Kb % kRowBytes / kChunk;
+            for (int row = threadIdx.x; row < BM + BN; row += kThreads) {
+                i32x4 *at = reinterpret_cast<i32x4 *>(p + row * kRowBytes + swizzled(row, c) * kChunk);
+                *at = first_bytes(*at, tail);
+            }
+            __syncthreads();
+        };
+        // This wave's reads of the stage are done and the next block's loads are there, for every wave.
+        auto meet = [&](int next) {
+            pin();
+            __builtin_amdgcn_s_waitcnt(0x0070);          // vmcnt(0) lgkmcnt(0)
+            __builtin_amdgcn_s_barrier();
+            pin();
+            if (tail && next == steps - 1) clear_tail(next);
+        };
+
+        f32x4 acc[NN][NM] = {};
+        const int fr = lane % kMF, fc = lane / kMF;
+        const int at_lo = fr * kRowBytes + swizzled(fr, fc) * kChunk;
+        const int at_hi = fr * kRowBytes + swizzled(fr, fc + 4) * kChunk;
+        const auto fetch = [&](const char *p) {
+            return join_chunks(*reinterpret_cast<const i32x4 *>(p + at_lo),
+                               *reinterpret_cast<const i32x4 *>(p + at_hi));
+        };
+        const auto fetch_a = [&](const char *stage, int i) { return fetch(stage + (wm * TM + i * kMF) * kRowBytes); };
+        const auto fetch_b = [&](const char *stage, int j) {
+            return fetch(stage + (BM + wn * TN + j * kMF) * kRowBytes);
+        };
+        const auto fetch_sx = [&](const char *stage, int i) {
+            return reinterpret_cast<const float *>(stage + kScaleAt)[wm * TM + i * kMF + fr];
+        };
+        // Of four channels of a fragment, or of all the wave's.
+        using WScale = std::conditional_t<WROWS, f32x4, float>;
+        constexpr int kWScales = WROWS ? NN : 1;
+        const auto fetch_sw = [&](const char *stage, int j) {
+            const float *s = reinterpret_cast<const float *>(stage + kScaleWAt);
+            if constexpr (WROWS)
+                return *reinterpret_cast<const f32x4 *>(s + wn * TN + j * kMF + 4 * fc);
+            else
+                return s[wn * TN / kF8Block];
+        };
+        const auto add = [](f32x4 &out, const f32x4 &sum, const WScale &of) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if constexpr (WROWS)
+                    out[e] = fmaf(sum[e], of[e], out[e]);
+                else
+                    out[e] = fmaf(sum[e], of, out[e]);
+            }
+            // Here, and not after the loads and products that follow, which would keep every pair's sums.
+            asm volatile("" : "+v"(out));
+        };
+        load_scales(0);
+        if constexpr (DIRECT)
+            load(0);
+        else
+            take(0), put(0);
+        meet(0);
+        auto load_next = [&](int step) {
+            if (step >= steps) return;
+            load_scales(step);
+            if constexpr (DIRECT)
+                load(step);
+            else
+                take(step);
+        };
+        load_next(1);
+        i32x8 fa[2];
+        F8Fragment<BSR_E4M3, WIDE> fb[NN];
+        float sxi[2];
+        WScale swj[kWScales];
+#pragma unroll
+        for (int j = 0; j < NN; ++j) fb[j].set(fetch_b(lds, j));
+#pragma unroll
+        for (int j = 0; j < kWScales; ++j) swj[j] = fetch_sw(lds, j);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) fa[i] = fetch_a(lds, i), sxi[i] = fetch_sx(lds, i);
+        // The sums that wait to be added to the outputs, and their scales.
+        f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+        WScale of{};
+        for (int s = 0; s < steps; ++s) {
+            const char *now = lds + (s & 1) * kStageBytes, *then = lds + ((s + 1) & 1) * kStageBytes;
+#pragma unroll
+            for (int i = 0; i < NM; ++i) {
+                if constexpr (!DIRECT)
+                    if (i == (NM > 2 ? NM - 3 : 0) && s + 1 < steps) put(s + 1);
+                if (i == NM - 2) {
+                    meet(s + 1);
+                    load_next(s + 2);
+                }
+                F8Fragment<XF, WIDE> x;
+                x.set(fa[i % 2]);
+                const float scale = sxi[i % 2];
+                const char *from = i + 2 < NM ? now : then;
+                const int next = i + 2 < NM ? i + 2 : i + 2 - NM;
+#pragma unroll
+                for (int j = 0; j < NN; ++j) {
+                    const f32x4 more = block_sums<XF>(fb[j], x);
+                    __builtin_amdgcn_sched_barrier(0);
+                    add(acc[j > 0 ? j - 1 : NN - 1][j > 0 ? i : i > 0 ? i - 1 : NM - 1], sum, of);
+                    sum = more;
+                    if (WROWS || j == 0) of = swj[WROWS ? j : 0] * scale;
+                    // a widened fragment leaves its codes' registers at once
+                    if (j == (WIDE ? 0 : NN - 1))
+                        fa[i % 2] = fetch_a(from, next), sxi[i % 2] = fetch_sx(from, next);
+                    if (i == NM - 1) fb[j].set(fetch_b(then, j));
+                    if (i == NM - 1 && j < kWScales) swj[j] = fetch_sw(then, j);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+        }
+        add(acc[NN - 1][NM - 1], sum, of);
+        __syncthreads();
+        constexpr bool kPast = BM * BN >= 192 * 256;
+        epilogue<bf16, Out::kScale, NN, NM, kPast>(
+            a, acc, reinterpret_cast<float *>(lds + wave * epilogue_bytes(NN)), rows.m0 + wm * TM,
+            rows.n0 + wn * TN);
+    }
+};
+
+template <int BM, int BN, int WM, int WN, int XF, bool WROWS, bool WIDE, bool DIRECT>
+__global__ __launch_bounds__(64 * WM * WN) void f8_ring_kernel(F8Args a) {
+    using K = F8RingKernel<BM, BN, WM, WN, XF, WROWS, WIDE, DIRECT>;
+    __shared__ __align__(16) char lds[K::kLds];
+    K::run(a, lds);
+}
+
+}  // namespace bsr

@@ -192,3 +192,11 @@ def test_validation_under_sanitizers(tmp_path):
                     os.path.join(ROOT, "tests", "host", "norm_f8_validate_fuzz.cpp"),
                     os.path.join(ROOT, "paper_2106_08846_amd", "csrc", "validate.cpp"),
                     "-o", exe], exe)
+
+
+@pytest.mark.skipif(shutil.which("g++") is None, reason="needs g++")
+def test_grids(tmp_path):
+    exe = str(tmp_path / "f8_grids")
+    _build_and_run(["g++", "-std=c++17", *SAN,
+                    "-I", os.path.join(ROOT, "paper_2106_08846_amd", "csrc"),
+                    os.path.join(ROOT, "tests", "host", "f8_grids.cpp"), "-o", exe], exe)
