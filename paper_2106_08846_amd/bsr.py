@@ -1122,7 +1122,7 @@ def bsr_layer_norm(X: torch.Tensor, gamma: torch.Tensor | None = None,
     save = save or mean is not None
     keep_sum = keep_sum or save or S is not None
     if Y is None:
-        Y = torch.empty(T, K, dtype=X.dtype, device=X.device)
+        Y = torch.empty_like(X)
         made.append(Y)
         ldy = K
     else:
@@ -1130,7 +1130,7 @@ def bsr_layer_norm(X: torch.Tensor, gamma: torch.Tensor | None = None,
     lds = 0
     if R is not None and keep_sum:
         if S is None:
-            S = torch.empty(T, K, dtype=X.dtype, device=X.device)
+            S = torch.empty_like(Y)
             made.append(S)
             lds = K
         else:

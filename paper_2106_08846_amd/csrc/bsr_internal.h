@@ -127,18 +127,19 @@ GatedWorkspace gated_workspace_layout(int64_t T, int64_t K, int64_t F, int32_t d
 // Norms and 8-bit floating point: the limits of the dense products.
 constexpr int kF8Block = 128;                           // columns that share a scale
 // Row groups of the norm's backward pass, each of which sums dgamma and dbeta over its rows.  Up to
-// kNormFusedWidth columns a workgroup holds a row of both operands in registers and makes dX with them:
-// one wave to 1024 columns, four rows to a workgroup; four waves to 4096, sixteen beyond.  512 workgroups
-// of four waves are two to a CU.
+// kNormFusedWidth columns a workgroup holds rows of both operands in registers and makes dX with them: one
+// wave to a row of 1024 columns, four to 4096, sixteen beyond, and several rows (kNormPlaces) side by side,
+// so that eight waves share a group's sums.
 constexpr int64_t kNormFusedWidth = 16384;
 constexpr int norm_row_waves(int64_t K) { return K <= 1024 ? 1 : K <= 4096 ? 4 : 16; }
+constexpr int kNormPlaces[] = {8, 2, 1};
 struct NormWorkspace {
     int groups;      // fp32 [groups][2][K]: the groups' sums
     size_t bytes;
 };
 inline NormWorkspace layer_norm_workspace(int64_t T, int64_t K) {
-    const int64_t rows = K <= 1024 ? 4 : K <= kNormFusedWidth ? 1 : 64;
-    const int64_t most = K <= 4096 ? 512 : K <= kNormFusedWidth ? 256 : 64;
+    const int64_t rows = K <= 1024 ? kNormPlaces[0] : K <= 4096 ? kNormPlaces[1] : K <= kNormFusedWidth ? kNormPlaces[2] : 64;
+    const int64_t most = K <= kNormFusedWidth ? 256 : 64;
     const int64_t groups = (T + rows - 1) / rows;
     const int64_t n = groups < most ? groups : most;
     return NormWorkspace{int(n), size_t(n > 0 ? n : 1) * 2 * size_t(K) * 4};

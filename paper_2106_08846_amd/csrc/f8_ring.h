@@ -3,10 +3,10 @@
 //
 // A wave's order of work in a block: token fragment i meets the channel fragments j in turn.  The sums of
 // (i, j) are added to the outputs while the matrix unit forms those of the next pair.  A token fragment is
-// read from LDS two i before its use, a channel fragment as soon as its last product is issued, so the
+// read from LDS two i before its use, a channel fragment over the last two i of the block before, so the
 // reads of a block end two i before its products do: there every wave waits for the next block's data
 // and meets the others, and the loads of the block after that go into the stage that is free from then on.
-// They have a whole block's products to arrive.
+// They have most of a block's products to arrive.
 //
 // DIRECT (rows on 16-byte boundaries): codes go straight from memory into LDS.  Otherwise they go through
 // registers, loaded at the same point and written shortly before the next meeting.
@@ -69,37 +69,32 @@ template <int BM, int BN, int WM, int WN, int XF, bool WROWS, bool WIDE, bool DI
                                                       ? (a.N - 1) / kF8Block - w_first + 1
                                                       : (BN + 127) / 128) * 4;
         const int steps = (a.Kb + kRowBytes - 1) / kRowBytes;
-        // The codes of a step into its stage.
-        auto load = [&](int step) {
+        // A step's loads in pieces, by number: codes of A (DIRECT), of B, then the scales.  Steps past the end
+        // load zeros, and the last step's scales.
+        constexpr int kCodes = DIRECT ? PA + PB : 0, kPieces = kCodes + 2;
+        auto load = [&](int step, int piece) {
             const int kb = step * kRowBytes;
-            lds_char *stage = (lds_char *)lds + (step & 1) * kStageBytes + wave * 1024;
-            const bool in = kb + c0 < a.Kb;              // chunks past the row's end: zeros
-            const unsigned va = in ? oa : kOut, vb = in ? ob : kOut;
-#pragma unroll
-            for (int i = 0; i < PA; ++i)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsa, (lds_void *)(stage + i * kWaves * 1024), 16, va,
-                                                         kb + i * kWaves * 8 * int(sa.pitch), 0, 0);
-            stage += BM * kRowBytes;
-#pragma unroll
-            for (int i = 0; i < PB; ++i)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsb, (lds_void *)(stage + i * kWaves * 1024), 16, vb,
-                                                         kb + i * kWaves * 8 * int(sb.pitch), 0, 0);
-        };
-        auto load_scales = [&](int step) {
-            lds_char *stage = (lds_char *)lds + (step & 1) * kStageBytes + kScaleAt;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int n = i * kWaves + wave;
-                if (n < kScaleLoadsX)
-                    __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                        buffer_rsrc(sx + step * args.ldsx, bytes_x), (lds_void *)(stage + n * 256), 4,
-                        n * 256 + lane * 4, 0, 0, 0);
-                else if (n < kScaleLoadsX + kScaleLoadsW)
-                    __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                        buffer_rsrc(sw + step * args.ldsw, bytes_w),
-                        (lds_void *)(stage + BM * 4 + (n - kScaleLoadsX) * 256), 4,
-                        (n - kScaleLoadsX) * 256 + lane * 4, 0, 0, 0);
+            lds_char *stage = (lds_char *)lds + (step & 1) * kStageBytes;
+            if (piece < kCodes) {
+                const bool of_a = piece < PA, in = kb + c0 < a.Kb;
+                const int i = of_a ? piece : piece - PA;
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                    of_a ? rsa : rsb,
+                    (lds_void *)(stage + (of_a ? 0 : BM * kRowBytes) + (i * kWaves + wave) * 1024), 16,
+                    in ? (of_a ? oa : ob) : kOut, kb + i * kWaves * 8 * int(of_a ? sa.pitch : sb.pitch), 0, 0);
+                return;
             }
+            const int n = (piece - kCodes) * kWaves + wave;
+            const int64_t row = step < steps ? step : steps - 1;
+            stage += kScaleAt;
+            if (n < kScaleLoadsX)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer_rsrc(sx + row * args.ldsx, bytes_x),
+                                                         (lds_void *)(stage + n * 256), 4,
+                                                         n * 256 + lane * 4, 0, 0, 0);
+            else if (n < kScaleLoadsX + kScaleLoadsW)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer_rsrc(sw + row * args.ldsw, bytes_w),
+                                                         (lds_void *)(stage + BM * 4 + (n - kScaleLoadsX) * 256),
+                                                         4, (n - kScaleLoadsX) * 256 + lane * 4, 0, 0, 0);
         };
         // !DIRECT: the codes of a step on their way through registers, in the same places.  Rows that do not
         // exist stand for the last one: they reach only outputs that do not exist.
@@ -183,27 +178,30 @@ template <int BM, int BN, int WM, int WN, int XF, bool WROWS, bool WIDE, bool DI
             // Here, and not after the loads and products that follow, which would keep every pair's sums.
             asm volatile("" : "+v"(out));
         };
-        load_scales(0);
-        if constexpr (DIRECT)
-            load(0);
-        else
-            take(0), put(0);
+        // Where in a block's products each piece is issued: with every second product from the meeting on
+        // (all at once behind it, waves wait to issue them: 8192^3 475 us, 455 so), closer where a block has
+        // few products.  The first kFirst come before the block ends, the others in the next.
+        constexpr int kSlots = NM * NN, kApart = 2 * kPieces <= kSlots ? 2 : 1;
+        constexpr int kPerSlot = (kPieces + kSlots - 1) / kSlots;
+        constexpr int kBeforeEnd = (2 * NN + kApart - 1) / kApart * kPerSlot;
+        constexpr int kFirst = kBeforeEnd < kPieces ? kBeforeEnd : kPieces;
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) load(0, i);
+        if constexpr (!DIRECT) take(0), put(0);
         meet(0);
-        auto load_next = [&](int step) {
-            if (step >= steps) return;
-            load_scales(step);
-            if constexpr (DIRECT)
-                load(step);
-            else
-                take(step);
-        };
-        load_next(1);
+#pragma unroll
+        for (int i = 0; i < kFirst; ++i) load(1, i);
+        if constexpr (!DIRECT) if (steps > 1) take(1);
         i32x8 fa[2];
-        F8Fragment<BSR_E4M3, WIDE> fb[NN];
+        // Channel fragments have two sets of registers where they fit, and the next block's are read over
+        // the last two i (8192^3 446 us, 455 with one set); in one set each is replaced as its last product
+        // is issued.
+        constexpr int kSets = WIDE || (WROWS && BM * BN > 192 * 256) || (!DIRECT && BM * BN >= 192 * 256) ? 1 : 2;
+        F8Fragment<BSR_E4M3, WIDE> fb[kSets][NN];
         float sxi[2];
         WScale swj[kWScales];
 #pragma unroll
-        for (int j = 0; j < NN; ++j) fb[j].set(fetch_b(lds, j));
+        for (int j = 0; j < NN; ++j) fb[0][j].set(fetch_b(lds, j));
 #pragma unroll
         for (int j = 0; j < kWScales; ++j) swj[j] = fetch_sw(lds, j);
 #pragma unroll
@@ -211,7 +209,8 @@ template <int BM, int BN, int WM, int WN, int XF, bool WROWS, bool WIDE, bool DI
         // The sums that wait to be added to the outputs, and their scales.
         f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
         WScale of{};
-        for (int s = 0; s < steps; ++s) {
+        using Channels = F8Fragment<BSR_E4M3, WIDE>[NN];
+        auto block = [&](int s, const Channels &mine, Channels &next_b) {
             const char *now = lds + (s & 1) * kStageBytes, *then = lds + ((s + 1) & 1) * kStageBytes;
 #pragma unroll
             for (int i = 0; i < NM; ++i) {
@@ -219,7 +218,7 @@ template <int BM, int BN, int WM, int WN, int XF, bool WROWS, bool WIDE, bool DI
                     if (i == (NM > 2 ? NM - 3 : 0) && s + 1 < steps) put(s + 1);
                 if (i == NM - 2) {
                     meet(s + 1);
-                    load_next(s + 2);
+                    if constexpr (!DIRECT) if (s + 2 < steps) take(s + 2);
                 }
                 F8Fragment<XF, WIDE> x;
                 x.set(fa[i % 2]);
@@ -228,7 +227,11 @@ template <int BM, int BN, int WM, int WN, int XF, bool WROWS, bool WIDE, bool DI
                 const int next = i + 2 < NM ? i + 2 : i + 2 - NM;
 #pragma unroll
                 for (int j = 0; j < NN; ++j) {
-                    const f32x4 more = block_sums<XF>(fb[j], x);
+                    const f32x4 more = block_sums<XF>(mine[j], x);
+                    const int slot = (i + 2) % NM * NN + j;
+#pragma unroll
+                    for (int p = 0; p < kPieces; ++p)
+                        if (p / kPerSlot * kApart == slot) load(i < NM - 2 ? s + 1 : s + 2, p);
                     __builtin_amdgcn_sched_barrier(0);
                     add(acc[j > 0 ? j - 1 : NN - 1][j > 0 ? i : i > 0 ? i - 1 : NM - 1], sum, of);
                     sum = more;
@@ -236,13 +239,31 @@ template <int BM, int BN, int WM, int WN, int XF, bool WROWS, bool WIDE, bool DI
                     // a widened fragment leaves its codes' registers at once
                     if (j == (WIDE ? 0 : NN - 1))
                         fa[i % 2] = fetch_a(from, next), sxi[i % 2] = fetch_sx(from, next);
-                    if (i == NM - 1) fb[j].set(fetch_b(then, j));
+                    if constexpr (kSets == 1) {
+                        if (i == NM - 1) next_b[j].set(fetch_b(then, j));
+                    } else {
+                        constexpr int kEvery = NN > 1 ? 2 : 1;
+                        const int at = (i - (NM - 2)) * NN + j;
+                        if (i >= NM - 2 && at % kEvery == 0 && at / kEvery < NN)
+                            next_b[at / kEvery].set(fetch_b(then, at / kEvery));
+                    }
                     if (i == NM - 1 && j < kWScales) swj[j] = fetch_sw(then, j);
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
+        };
+        if constexpr (kSets == 1) {
+            for (int s = 0; s < steps; ++s) block(s, fb[0], fb[0]);
+        } else {
+            int s = 0;
+            for (; s + 1 < steps; s += 2) {
+                block(s, fb[0], fb[1]);
+                block(s + 1, fb[1], fb[0]);
+            }
+            if (s < steps) block(s, fb[0], fb[1]);
         }
         add(acc[NN - 1][NM - 1], sum, of);
+        __builtin_amdgcn_s_waitcnt(0x0070);      // loads past the end, before LDS is used again
         __syncthreads();
         constexpr bool kPast = BM * BN >= 192 * 256;
         epilogue<bf16, Out::kScale, NN, NM, kPast>(

@@ -19,10 +19,10 @@ struct NormArgs {
 };
 
 // kVec values of a vector that may be missing.
-template <bool WHOLE>
+template <int END>
 __device__ __forceinline__ void load_or(const float *p, int k, int K, float other, float (&v)[kVec]) {
     if (p) {
-        load_vec<float, WHOLE>(p, k, K, v);
+        load_vec<float, END>(p, k, K, v);
     } else {
 #pragma unroll
         for (int i = 0; i < kVec; ++i) v[i] = other;
@@ -44,9 +44,9 @@ template <int WAVES> __device__ __forceinline__ float row_sum(float v, float *at
 
 constexpr int kHeld = 8;       // load steps of a row that the forward pass holds in registers
 
-// WAVES waves per row, ROWS rows per workgroup.  WHOLE: K is a multiple of a load step's elements.  Rows
+// WAVES waves per row, ROWS rows per workgroup, whose rows end as END says.  Rows
 // longer than the registers hold are read again for the deviations and for the outputs.
-template <class T, int WAVES, int ROWS, bool WHOLE>
+template <class T, int WAVES, int ROWS, int END>
 __global__ __launch_bounds__(64 * WAVES * ROWS) void norm_kernel(NormArgs a) {
     static_assert(WAVES == 1 || ROWS == 1, "one row per barrier");
     constexpr int kSpan = 64 * WAVES * kVec;
@@ -61,10 +61,10 @@ __global__ __launch_bounds__(64 * WAVES * ROWS) void norm_kernel(NormArgs a) {
     const int k0 = (wave % WAVES * 64 + lane) * kVec;
     // S[k ..], rounded to the type.
     const auto load = [&](int k, float (&v)[kVec]) {
-        load_vec<T, WHOLE>(x, k, K, v);
+        load_vec<T, END>(x, k, K, v);
         if (r) {
             float w[kVec];
-            load_vec<T, WHOLE>(r, k, K, w);
+            load_vec<T, END>(r, k, K, w);
 #pragma unroll
             for (int i = 0; i < kVec; ++i) v[i] = to_float(from_float<T>(v[i] + w[i]));
         }
@@ -73,7 +73,7 @@ __global__ __launch_bounds__(64 * WAVES * ROWS) void norm_kernel(NormArgs a) {
         float q = 0.0f;
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
-            const float d = WHOLE || k + i < K ? v[i] - mean : 0.0f;
+            const float d = END == kWholeSteps || k + i < K ? v[i] - mean : 0.0f;
             q = fmaf(d, d, q);
         }
         return q;
@@ -88,14 +88,14 @@ __global__ __launch_bounds__(64 * WAVES * ROWS) void norm_kernel(NormArgs a) {
 #pragma unroll
     for (int s = 0; s < kHeld; ++s) {
         if (s * kSpan >= K) break;
-        if (sum_out) write_vec<T, WHOLE>(sum_out, k0 + s * kSpan, K, v[s]);
+        if (sum_out) write_vec<T, END, true>(sum_out, k0 + s * kSpan, K, v[s]);
 #pragma unroll
         for (int i = 0; i < kVec; ++i) sum += v[s][i];
     }
     for (int k = k0 + kHeld * kSpan; k < K; k += kSpan) {
         float w[kVec];
         load(k, w);
-        if (sum_out) write_vec<T, WHOLE>(sum_out, k, K, w);
+        if (sum_out) write_vec<T, END, true>(sum_out, k, K, w);
 #pragma unroll
         for (int i = 0; i < kVec; ++i) sum += w[i];
     }
@@ -118,11 +118,11 @@ __global__ __launch_bounds__(64 * WAVES * ROWS) void norm_kernel(NormArgs a) {
     }
     const auto store = [&](int k, const float (&v)[kVec]) {
         float g[kVec], b[kVec], out[kVec];
-        load_or<WHOLE>(a.gamma, k, K, 1.0f, g);
-        load_or<WHOLE>(a.beta, k, K, 0.0f, b);
+        load_or<END>(a.gamma, k, K, 1.0f, g);
+        load_or<END>(a.beta, k, K, 0.0f, b);
 #pragma unroll
         for (int i = 0; i < kVec; ++i) out[i] = fmaf((v[i] - mean) * rstd, g[i], b[i]);
-        write_vec<T, WHOLE>(y, k, K, out);
+        write_vec<T, END, true>(y, k, K, out);
     };
 #pragma unroll
     for (int s = 0; s < kHeld; ++s) {
@@ -139,8 +139,10 @@ __global__ __launch_bounds__(64 * WAVES * ROWS) void norm_kernel(NormArgs a) {
 constexpr int64_t kRowsPerLaunch = int64_t(1) << 21;     // a grid has under 2^32 threads
 
 template <class T, int WAVES, int ROWS> void launch_norm(const NormArgs &args, void *stream) {
-    const auto kernel = args.K % (64 * WAVES * kVec) == 0 ? norm_kernel<T, WAVES, ROWS, true>
-                                                          : norm_kernel<T, WAVES, ROWS, false>;
+    const int end = row_end(args.K, 64 * WAVES * kVec);
+    const auto kernel = end == kWholeSteps     ? norm_kernel<T, WAVES, ROWS, kWholeSteps>
+                        : end == kWholeVectors ? norm_kernel<T, WAVES, ROWS, kWholeVectors>
+                                               : norm_kernel<T, WAVES, ROWS, kAnyEnd>;
     for (int64_t t = 0; t < args.T; t += kRowsPerLaunch) {
         NormArgs a = args;
         a.T = args.T - t < kRowsPerLaunch ? args.T - t : kRowsPerLaunch;
@@ -156,7 +158,8 @@ template <class T, int WAVES, int ROWS> void launch_norm(const NormArgs &args, v
 
 template <class T> void norm(const NormArgs &a, void *stream) {
     constexpr int64_t held = 64 * kVec * kHeld;   // elements of a row that a wave holds
-    if (a.K <= held)
+    // Few long rows on a wave each leave CUs idle: 777 x 1531 fp32 takes 5.8 us so and 5.2 on four.
+    if (a.K <= 1024 || (a.K <= held && a.T >= 2048))
         launch_norm<T, 1, 4>(a, stream);
     else if (a.K <= 4 * held)
         launch_norm<T, 4, 1>(a, stream);
@@ -175,99 +178,146 @@ struct NormGradArgs {
     int K;
 };
 
-// Rows of up to 1024 WAVES columns: a group of WAVES waves takes every row from its first on, one after
-// another, with its columns' gamma, dgamma and dbeta in registers.
-template <class T, int WAVES, int ROWS, bool WHOLE>
+// Rows of up to 1024 WAVES columns: a workgroup takes ROWS rows side by side, WAVES waves each, kBatch times
+// at once, and walks on over the rows with its columns' gamma, dgamma and dbeta in registers.
+template <class T, int WAVES, int ROWS, int END>
 __global__ __launch_bounds__(64 * WAVES * ROWS) void norm_backward_kernel(NormGradArgs a) {
-    static_assert(WAVES == 1 || ROWS == 1, "one row per barrier");
     constexpr int kSteps = 2, kSpan = 64 * WAVES * kVec, kWidth = kSteps * kSpan;
-    __shared__ float red[2][2][WAVES];
+    // Two rows of bf16 in flight; fp32 and sixteen waves have registers for one.
+    constexpr int kBatch = WAVES > 4 || sizeof(T) > 2 ? 1 : 2;
+    __shared__ float red[2][2 * kBatch][ROWS][WAVES];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, K = a.K;
-    const int k0 = (wave % WAVES * 64 + lane) * kVec;
+    const int place = wave / WAVES, part = wave % WAVES, k0 = (part * 64 + lane) * kVec;
     float gamma[kSteps][kVec], dgamma[kSteps][kVec] = {}, dbeta[kSteps][kVec] = {};
 #pragma unroll
     for (int s = 0; s < kSteps; ++s)
-        if (s * kSpan < K) load_or<WHOLE>(a.gamma, k0 + s * kSpan, K, 1.0f, gamma[s]);
+        if (s * kSpan < K) load_or<END>(a.gamma, k0 + s * kSpan, K, 1.0f, gamma[s]);
     int parity = 0;
-    for (int64_t row = int64_t(blockIdx.x) * ROWS + wave / WAVES; row < a.T;
-         row += int64_t(gridDim.x) * ROWS) {
-        const T *dy = static_cast<const T *>(a.dY) + row * a.lddy;
-        const T *sum = static_cast<const T *>(a.S) + row * a.lds;
-        const float mean = a.mean[row], rstd = a.rstd[row];
-        float d[kSteps][kVec], h[kSteps][kVec];
+    const int64_t stride = int64_t(gridDim.x) * ROWS;
+    struct Batch {
+        T d[kBatch][kSteps][kVec], x[kBatch][kSteps][kVec], more[kBatch][kSteps][kVec];
+        float mean[kBatch], rstd[kBatch];
+        bool in[kBatch];
+    };
+    const auto fetch = [&](int64_t base, Batch &to) {
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            if (s * kSpan >= K) break;
-            load_vec<T, WHOLE>(dy, k0 + s * kSpan, K, d[s]);
-            load_vec<T, WHOLE>(sum, k0 + s * kSpan, K, h[s]);
-        }
-        float c1 = 0.0f, c2 = 0.0f;
+        for (int b = 0; b < kBatch; ++b) {
+            const int64_t row = base + place + b * stride;
+            to.in[b] = row < a.T;
+            if (!to.in[b]) continue;
+            to.mean[b] = a.mean[row];
+            to.rstd[b] = a.rstd[row];
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            if (s * kSpan >= K) break;
-#pragma unroll
-            for (int i = 0; i < kVec; ++i) {
-                h[s][i] = (h[s][i] - mean) * rstd;
-                dgamma[s][i] = fmaf(d[s][i], h[s][i], dgamma[s][i]);
-                dbeta[s][i] += d[s][i];
-                d[s][i] *= gamma[s][i];
-                c1 += d[s][i];
-                c2 = fmaf(d[s][i], h[s][i], c2);
+            for (int s = 0; s < kSteps; ++s) {
+                if (s * kSpan >= K) break;
+                const int k = k0 + s * kSpan;
+                take_vec<T, END>(static_cast<const T *>(a.dY) + row * a.lddy, k, K, to.d[b][s]);
+                take_vec<T, END>(static_cast<const T *>(a.S) + row * a.lds, k, K, to.x[b][s]);
+                if (a.dS)
+                    take_vec<T, END>(static_cast<const T *>(a.dS) + row * a.ldds, k, K, to.more[b][s]);
             }
         }
-        if (!a.dX) continue;
-        c1 = wave_sum(c1);
-        c2 = wave_sum(c2);
-        if constexpr (WAVES > 1) {
-            // The other half is written for the next row, and this one again only after its barrier.
-            if (lane == 0) red[parity][0][wave] = c1, red[parity][1][wave] = c2;
-            __syncthreads();
-            c1 = c2 = 0.0f;
+    };
+    // The next rows are loaded before this round's sums are joined, where the registers hold them and no lane
+    // asks for the end of its row: 8192 x 4096 bf16 with dS takes 49 us so and 55 without (2048 x 8192 on
+    // sixteen waves 34 and 33).
+    constexpr bool kAhead = END != kAnyEnd && WAVES <= 4;
+    Batch next = {};
+    if (kAhead) fetch(int64_t(blockIdx.x) * ROWS, next);
+    // Every wave makes the same rounds, for their barriers.
+    for (int64_t base = int64_t(blockIdx.x) * ROWS; base < a.T; base += kBatch * stride) {
+        if (!kAhead) fetch(base, next);
+        const Batch now = next;
+        float c[2 * kBatch];
+        if (kAhead) fetch(base + kBatch * stride, next);
 #pragma unroll
-            for (int w = 0; w < WAVES; ++w) c1 += red[parity][0][w], c2 += red[parity][1][w];
+        for (int b = 0; b < kBatch; ++b) {
+            float c1 = 0.0f, c2 = 0.0f;
+            if (now.in[b]) {
+#pragma unroll
+                for (int s = 0; s < kSteps; ++s) {
+                    if (s * kSpan >= K) break;
+#pragma unroll
+                    for (int i = 0; i < kVec; ++i) {
+                        const float dy = to_float(now.d[b][s][i]), h = (to_float(now.x[b][s][i]) - now.mean[b]) * now.rstd[b];
+                        dgamma[s][i] = fmaf(dy, h, dgamma[s][i]);
+                        dbeta[s][i] += dy;
+                        const float g = dy * gamma[s][i];
+                        c1 += g;
+                        c2 = fmaf(g, h, c2);
+                    }
+                }
+            }
+            c[2 * b] = c1;
+            c[2 * b + 1] = c2;
+        }
+        if (!a.dX) continue;
+#pragma unroll
+        for (int i = 0; i < 2 * kBatch; ++i) c[i] = wave_sum(c[i]);
+        if constexpr (WAVES > 1) {
+            // The other half is written for the next round, and this one again only after its barrier.
+            if (lane == 0)
+#pragma unroll
+                for (int i = 0; i < 2 * kBatch; ++i) red[parity][i][place][part] = c[i];
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < 2 * kBatch; ++i) {
+                c[i] = 0.0f;
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) c[i] += red[parity][i][place][w];
+            }
             parity ^= 1;
         }
-        c1 /= float(K);
-        c2 /= float(K);
-        T *dx = static_cast<T *>(a.dX) + row * a.lddx;
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            if (s * kSpan >= K) break;
-            float out[kVec], more[kVec] = {};
-            if (a.dS)
-                load_vec<T, WHOLE>(static_cast<const T *>(a.dS) + row * a.ldds, k0 + s * kSpan, K, more);
+        for (int b = 0; b < kBatch; ++b) {
+            if (!now.in[b]) break;
+            const float c1 = c[2 * b] / float(K), c2 = c[2 * b + 1] / float(K);
+            T *dx = static_cast<T *>(a.dX) + (base + place + b * stride) * a.lddx;
 #pragma unroll
-            for (int i = 0; i < kVec; ++i)
-                out[i] = fmaf(d[s][i] - c1 - h[s][i] * c2, rstd, more[i]);
-            write_vec<T, WHOLE>(dx, k0 + s * kSpan, K, out);
+            for (int s = 0; s < kSteps; ++s) {
+                if (s * kSpan >= K) break;
+                float out[kVec];
+#pragma unroll
+                for (int i = 0; i < kVec; ++i) {
+                    const float h = (to_float(now.x[b][s][i]) - now.mean[b]) * now.rstd[b];
+                    out[i] = fmaf(to_float(now.d[b][s][i]) * gamma[s][i] - c1 - h * c2, now.rstd[b],
+                                  to_float(now.more[b][s][i]));
+                }
+                write_vec<T, END>(dx, k0 + s * kSpan, K, out);
+            }
         }
     }
     if (!a.partial) return;
+    if constexpr (ROWS > 1) {                  // the upper half of the places to the lower, until one is left
+        __shared__ __align__(16) float half[ROWS / 2][2][kWidth];
+#pragma unroll
+        for (int n = ROWS / 2; n > 0; n /= 2) {
+            if (place >= n && place < 2 * n)
+#pragma unroll
+                for (int s = 0; s < kSteps; ++s) {
+                    write_vec<float, kWholeSteps>(half[place - n][0], k0 + s * kSpan, kWidth, dgamma[s]);
+                    write_vec<float, kWholeSteps>(half[place - n][1], k0 + s * kSpan, kWidth, dbeta[s]);
+                }
+            __syncthreads();
+            if (place < n)
+#pragma unroll
+                for (int s = 0; s < kSteps; ++s) {
+                    float g[kVec], e[kVec];
+                    load_vec<float, kWholeSteps>(half[place][0], k0 + s * kSpan, kWidth, g);
+                    load_vec<float, kWholeSteps>(half[place][1], k0 + s * kSpan, kWidth, e);
+#pragma unroll
+                    for (int i = 0; i < kVec; ++i) dgamma[s][i] += g[i], dbeta[s][i] += e[i];
+                }
+            __syncthreads();
+        }
+        if (place > 0) return;
+    }
     float *to = a.partial + int64_t(blockIdx.x) * 2 * K;
-    if constexpr (ROWS > 1) {                  // the workgroup's rows, in order
-        __shared__ float all[ROWS][2][kWidth];
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s)
-#pragma unroll
-            for (int i = 0; i < kVec; ++i) {
-                all[wave][0][k0 + s * kSpan + i] = dgamma[s][i];
-                all[wave][1][k0 + s * kSpan + i] = dbeta[s][i];
-            }
-        __syncthreads();
-        for (int at = threadIdx.x; at < 2 * kWidth; at += 64 * ROWS) {
-            const int which = at / kWidth, k = at % kWidth;
-            float sum = 0.0f;
-#pragma unroll
-            for (int w = 0; w < ROWS; ++w) sum += all[w][which][k];
-            if (k < K) to[which * K + k] = sum;
-        }
-    } else {
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            if (s * kSpan >= K) break;
-            write_vec<float, WHOLE>(to, k0 + s * kSpan, K, dgamma[s]);
-            write_vec<float, WHOLE>(to + K, k0 + s * kSpan, K, dbeta[s]);
-        }
+    for (int s = 0; s < kSteps; ++s) {
+        if (s * kSpan >= K) break;
+        write_vec<float, END>(to, k0 + s * kSpan, K, dgamma[s]);
+        write_vec<float, END>(to + K, k0 + s * kSpan, K, dbeta[s]);
     }
 }
 
@@ -283,9 +333,9 @@ template <class T> __global__ __launch_bounds__(1024) void norm_dx_kernel(NormGr
         const float mean = a.mean[row], rstd = a.rstd[row];
         const auto load = [&](int k, float (&g)[kVec], float (&h)[kVec]) {
             float w[kVec];
-            load_vec<T, false>(dy, k, K, g);
-            load_vec<T, false>(sum, k, K, h);
-            load_or<false>(a.gamma, k, K, 1.0f, w);
+            load_vec<T, kAnyEnd>(dy, k, K, g);
+            load_vec<T, kAnyEnd>(sum, k, K, h);
+            load_or<kAnyEnd>(a.gamma, k, K, 1.0f, w);
 #pragma unroll
             for (int i = 0; i < kVec; ++i) {
                 g[i] *= w[i];
@@ -305,10 +355,10 @@ template <class T> __global__ __launch_bounds__(1024) void norm_dx_kernel(NormGr
         for (int k = k0; k < K; k += kSpan) {
             float out[kVec], more[kVec] = {};
             load(k, g, h);
-            if (a.dS) load_vec<T, false>(static_cast<const T *>(a.dS) + row * a.ldds, k, K, more);
+            if (a.dS) load_vec<T, kAnyEnd>(static_cast<const T *>(a.dS) + row * a.ldds, k, K, more);
 #pragma unroll
             for (int i = 0; i < kVec; ++i) out[i] = fmaf(g[i] - c1 - h[i] * c2, rstd, more[i]);
-            write_vec<T, false>(dx, k, K, out);
+            write_vec<T, kAnyEnd>(dx, k, K, out);
         }
     }
 }
@@ -319,8 +369,8 @@ template <class T> __global__ __launch_bounds__(kColumnThreads) void norm_column
     float dgamma[kVec] = {}, dbeta[kVec] = {};
     for (int64_t row = blockIdx.y; row < a.T; row += gridDim.y) {
         float d[kVec], h[kVec];
-        load_vec<T, false>(static_cast<const T *>(a.dY) + row * a.lddy, k, K, d);
-        load_vec<T, false>(static_cast<const T *>(a.S) + row * a.lds, k, K, h);
+        load_vec<T, kAnyEnd>(static_cast<const T *>(a.dY) + row * a.lddy, k, K, d);
+        load_vec<T, kAnyEnd>(static_cast<const T *>(a.S) + row * a.lds, k, K, h);
         const float mean = a.mean[row], rstd = a.rstd[row];
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
@@ -329,43 +379,55 @@ template <class T> __global__ __launch_bounds__(kColumnThreads) void norm_column
         }
     }
     float *to = a.partial + int64_t(blockIdx.y) * 2 * K;
-    write_vec<float, false>(to, k, K, dgamma);
-    write_vec<float, false>(to + K, k, K, dbeta);
+    write_vec<float, kAnyEnd>(to, k, K, dgamma);
+    write_vec<float, kAnyEnd>(to + K, k, K, dbeta);
 }
 
-// The groups' sums joined, in order: 64 columns to a workgroup, whose waves take every 16th group each.
-constexpr int kJoinWaves = 16;
+// The groups' sums joined, in an order fixed by their number: 32 columns to a workgroup, whose half-waves
+// take every 32nd group each, eight loads at a time.
+constexpr int kJoinWaves = 16, kJoinColumns = 32, kJoinParts = 64 / kJoinColumns * kJoinWaves;
 template <class G>
 __global__ __launch_bounds__(64 * kJoinWaves) void norm_join_kernel(const float *partial, int groups, int K,
                                                                     G *dgamma, G *dbeta) {
-    __shared__ float part[kJoinWaves][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t at = int64_t(blockIdx.x) * 64 + lane, width = 2 * int64_t(K);
+    __shared__ float parts[kJoinParts][kJoinColumns];
+    const int column = threadIdx.x % kJoinColumns, part = threadIdx.x / kJoinColumns;
+    const int64_t at = int64_t(blockIdx.x) * kJoinColumns + column, width = 2 * int64_t(K);
     float sum = 0.0f;
-    if (at < width)
-        for (int g = wave; g < groups; g += kJoinWaves) sum += partial[g * width + at];
-    part[wave][lane] = sum;
+    if (at < width) {
+        int g = part;
+        for (; g + 7 * kJoinParts < groups; g += 8 * kJoinParts) {
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = partial[(g + i * kJoinParts) * width + at];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += v[i];
+        }
+        for (; g < groups; g += kJoinParts) sum += partial[g * width + at];
+    }
+    parts[part][column] = sum;
     __syncthreads();
-    if (wave > 0 || at >= width) return;
+    if (part > 0 || at >= width) return;
     sum = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kJoinWaves; ++w) sum += part[w][lane];
+    for (int w = 0; w < kJoinParts; ++w) sum += parts[w][column];
     G *to = at < K ? dgamma : dbeta;
     if (to) to[at < K ? at : at - K] = from_float<G>(sum);
 }
 
 template <class T, int WAVES, int ROWS> void launch_backward(const NormGradArgs &a, int groups, void *stream) {
-    const auto kernel = a.K % (64 * WAVES * kVec) == 0 ? norm_backward_kernel<T, WAVES, ROWS, true>
-                                                       : norm_backward_kernel<T, WAVES, ROWS, false>;
+    const int end = row_end(a.K, 64 * WAVES * kVec);
+    const auto kernel = end == kWholeSteps     ? norm_backward_kernel<T, WAVES, ROWS, kWholeSteps>
+                        : end == kWholeVectors ? norm_backward_kernel<T, WAVES, ROWS, kWholeVectors>
+                                               : norm_backward_kernel<T, WAVES, ROWS, kAnyEnd>;
     hipLaunchKernelGGL(kernel, dim3(unsigned(groups)), dim3(64 * WAVES * ROWS), 0, as_stream(stream), a);
 }
 
 template <class T> void norm_backward(const NormGradArgs &a, int groups, void *stream) {
     if (a.K <= kNormFusedWidth) {
         switch (norm_row_waves(a.K)) {
-            case 1: return launch_backward<T, 1, 4>(a, groups, stream);
-            case 4: return launch_backward<T, 4, 1>(a, groups, stream);
-            default: return launch_backward<T, 16, 1>(a, groups, stream);
+            case 1: return launch_backward<T, 1, kNormPlaces[0]>(a, groups, stream);
+            case 4: return launch_backward<T, 4, kNormPlaces[1]>(a, groups, stream);
+            default: return launch_backward<T, 16, kNormPlaces[2]>(a, groups, stream);
         }
     }
     if (a.dX)
@@ -379,7 +441,8 @@ template <class T> void norm_backward(const NormGradArgs &a, int groups, void *s
 
 template <class G>
 void join(const float *partial, int groups, int64_t K, void *dgamma, void *dbeta, void *stream) {
-    hipLaunchKernelGGL(norm_join_kernel<G>, dim3(unsigned((2 * K + 63) / 64)), dim3(64 * kJoinWaves), 0,
+    hipLaunchKernelGGL(norm_join_kernel<G>, dim3(unsigned((2 * K + kJoinColumns - 1) / kJoinColumns)),
+                       dim3(64 * kJoinWaves), 0,
                        as_stream(stream), partial, groups, int(K), static_cast<G *>(dgamma),
                        static_cast<G *>(dbeta));
 }

@@ -5,6 +5,9 @@
 // By rows alone a wave takes rows of 512 elements, four blocks side by side, each held by 16 lanes.
 // Everything else goes by tiles of 128 x 128 that stay in registers between the maxima and the codes; the
 // transpose is made of 8 x 8 pieces in the lanes and put together in LDS.
+#include <type_traits>
+#include <utility>
+
 #include "row_vec.h"
 
 namespace bsr {
@@ -23,19 +26,20 @@ struct QuantizeArgs {
     int64_t t0;              // first row of this launch (a multiple of 128)
 };
 
-// What a block's largest magnitude (its bits) makes of it.
+// What a block's largest magnitude (its bits) makes of it.  Two divisions, so the lanes that hold a block
+// share the work: each makes the scale of one of their rows.
 template <int FMT> struct BlockScale {
     static constexpr float kLargest = FMT == BSR_E4M3 ? 448.0f : 57344.0f;
-    float scale, lift, r;
-    bool plain;              // else zeros, or with an infinity or a NaN: every code is 0
+    float scale, lift, r;    // r: 0 for a block of zeros or with an infinity or a NaN, whose codes are 0
     __device__ __forceinline__ explicit BlockScale(unsigned top) {
         const float a = __uint_as_float(top);
-        plain = top > 0 && top < 0x7f800000u;
+        const bool plain = top > 0 && top < 0x7f800000u;
         lift = a < 0x1p-64f ? 0x1p64f : 1.0f;
         r = plain ? kLargest / (a * lift) : 0.0f;
         scale = a / kLargest;
     }
-    __device__ __forceinline__ float of(float x) const { return plain ? (x * lift) * r : 0.0f; }
+    // Codes are x r.
+    __device__ __forceinline__ bool ordinary() const { return r > 0.0f && lift == 1.0f; }
 };
 
 // Codes of four values, the first in the lowest byte (nearest, ties to even; none is beyond the largest
@@ -51,16 +55,20 @@ template <int FMT> __device__ __forceinline__ unsigned codes4(float a, float b, 
     }
     return unsigned(v);
 }
-template <int FMT> __device__ __forceinline__ uint2 codes8(const BlockScale<FMT> &s, const float (&v)[kVec]) {
-    return uint2{codes4<FMT>(s.of(v[0]), s.of(v[1]), s.of(v[2]), s.of(v[3])),
-                 codes4<FMT>(s.of(v[4]), s.of(v[5]), s.of(v[6]), s.of(v[7]))};
+// Codes of a block's values.  ORDINARY: lift is 1 and r is not 0.
+template <int FMT, bool ORDINARY>
+__device__ __forceinline__ uint2 codes8(float lift, float r, const float (&v)[kVec]) {
+    float x[kVec];
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) x[i] = ORDINARY ? v[i] * r : r == 0.0f ? 0.0f : (v[i] * lift) * r;
+    return uint2{codes4<FMT>(x[0], x[1], x[2], x[3]), codes4<FMT>(x[4], x[5], x[6], x[7])};
 }
 
 // The first n of N bytes of v at p.
 template <int N, class V> __device__ __forceinline__ void store_bytes(uint8_t *p, int64_t n, const V &v) {
     static_assert(sizeof(V) == N, "whole values");
     if (n >= N) {
-        __builtin_memcpy(p, &v, N);
+        stream_out(p, v);
     } else {
         uint8_t b[N];
         __builtin_memcpy(b, &v, N);
@@ -77,6 +85,14 @@ __device__ __forceinline__ unsigned top_of(const float (&v)[kVec]) {
     return top;
 }
 
+// f(constant 0), ..., f(constant N - 1).
+template <int... I, class F> __device__ __forceinline__ void each(std::integer_sequence<int, I...>, F &&f) {
+    (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F> __device__ __forceinline__ void each(F &&f) {
+    each(std::make_integer_sequence<int, N>{}, f);
+}
+
 // By rows, blocks of 1 x 128: 16 rows of 512 columns to a workgroup, four rows to a wave, all loaded at
 // once.  The scales of one block lie side by side for the rows, so they are stored 16 at a time.
 constexpr int kStripRows = 16, kStripColumns = 64 * kVec;
@@ -91,15 +107,26 @@ template <class T, int FMT> __global__ __launch_bounds__(kThreads) void quantize
 #pragma unroll
     for (int i = 0; i < kRows; ++i) {
         const int64_t t = t0 + wave * kRows + i;
-        if (t < a.T) load_vec<T, false>(static_cast<const T *>(a.X) + t * a.ldx, k, K, v[i]);
+        if (t < a.T) load_vec<T, kAnyEnd>(static_cast<const T *>(a.X) + t * a.ldx, k, K, v[i]);
     }
+    unsigned top[kRows];
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-        const int64_t t = t0 + wave * kRows + i;
-        const BlockScale<FMT> s(row_max(top_of(v[i])));
-        if (lane % 16 == 0) scales[lane / 16][wave * kRows + i] = s.scale;
-        if (t < a.T && k < K) store_bytes<8>(a.Q + t * a.ldq + k, K - k, codes8(s, v[i]));
-    }
+    for (int i = 0; i < kRows; ++i) top[i] = row_max(top_of(v[i]));
+    const int own = lane % kRows;              // the row whose scale this lane makes
+    const BlockScale<FMT> s(own < 2 ? (own == 0 ? top[0] : top[1]) : (own == 2 ? top[2] : top[3]));
+    if (lane % 16 < kRows) scales[lane / 16][wave * kRows + own] = s.scale;
+    const auto store = [&](auto ordinary) {
+        each<kRows>([&](auto i) {
+            const int64_t t = t0 + wave * kRows + i;
+            const uint2 codes =
+                codes8<FMT, decltype(ordinary)::value>(quad_lane<i>(s.lift), quad_lane<i>(s.r), v[i]);
+            if (t < a.T && k < K) store_bytes<8>(a.Q + t * a.ldq + k, K - k, codes);
+        });
+    };
+    if (__all(s.ordinary()))
+        store(std::true_type{});
+    else
+        store(std::false_type{});
     __syncthreads();
     const int b = threadIdx.x / kStripRows, i = threadIdx.x % kStripRows;
     if (b < kBlocks && c0 + b * kF8Block < K && t0 + i < a.T)
@@ -111,6 +138,7 @@ template <class T, int FMT> __global__ __launch_bounds__(kThreads) void quantize
 template <class T, int FMT, int ROWS> __global__ __launch_bounds__(kThreads) void quantize_tile_kernel(QuantizeArgs a) {
     constexpr int kB = kF8Block, kWaves = kThreads / 64;
     __shared__ unsigned tops[kWaves][kB];
+    __shared__ __align__(16) float column_r[kB], column_lift[kB];
     __shared__ __align__(16) uint8_t turned[kB * kB];
     const int tiles = (a.K + kB - 1) / kB;
     const int64_t t0 = a.t0 + int64_t(blockIdx.x / tiles) * kB;
@@ -122,72 +150,100 @@ template <class T, int FMT, int ROWS> __global__ __launch_bounds__(kThreads) voi
     float v[kVec][kVec] = {};
 #pragma unroll
     for (int i = 0; i < kVec; ++i)
-        if (t + i < a.T) load_vec<T, false>(static_cast<const T *>(a.X) + (t + i) * a.ldx, k, K, v[i]);
+        if (t + i < a.T) load_vec<T, kAnyEnd>(static_cast<const T *>(a.X) + (t + i) * a.ldx, k, K, v[i]);
 
-    unsigned whole = 0;                        // ROWS = 128: the tile's largest
+    unsigned top[kVec];                        // of the thread's rows, in this tile
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) top[i] = top_of(v[i]);
+    unsigned own = 0;                          // ROWS = 1: of row c % 8; 128: the tile's
     if constexpr (ROWS > 1) {
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) whole = max(whole, top_of(v[i]));
-        whole = row_max(whole);
-        if (lane % 16 == 0) tops[wave][lane / 16] = whole;
+        for (int i = 0; i < kVec; ++i) own = max(own, top[i]);
+        own = column_max(row_max(own));
+        if (lane == 0) tops[wave][0] = own;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) whole = max(whole, tops[w][i]);
-        const BlockScale<FMT> s(whole);
-        if (threadIdx.x == 0) {
-            if (a.Q) a.scale[(k0 / kB) * a.ldscale + t0 / kB] = s.scale;
-            if (a.QT) a.scale_t[(t0 / kB) * a.ldscale_t + k0 / kB] = s.scale;
-        }
-    }
-    if (a.Q) {
+        for (int w = 0; w < kWaves; ++w) own = max(own, tops[w][0]);
+    } else if (a.Q) {
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
-            const BlockScale<FMT> s(ROWS > 1 ? whole : row_max(top_of(v[i])));
-            if (t + i >= a.T) continue;
-            if (ROWS == 1 && c == 0) a.scale[(k0 / kB) * a.ldscale + t + i] = s.scale;
-            if (k < K) store_bytes<8>(a.Q + (t + i) * a.ldq + k, K - k, codes8(s, v[i]));
+            const unsigned whole = row_max(top[i]);
+            if (c % kVec == i) own = whole;
         }
+    }
+    const BlockScale<FMT> s(own);
+    if (ROWS > 1 && threadIdx.x == 0) {
+        if (a.Q) a.scale[(k0 / kB) * a.ldscale + t0 / kB] = s.scale;
+        if (a.QT) a.scale_t[(t0 / kB) * a.ldscale_t + k0 / kB] = s.scale;
+    }
+    if (a.Q) {
+        if (ROWS == 1 && c < kVec && t + c < a.T) a.scale[(k0 / kB) * a.ldscale + t + c] = s.scale;
+        const auto store = [&](auto ordinary) {
+            each<kVec>([&](auto i) {
+                const float lift = ROWS > 1 ? s.lift : row_lane<i>(s.lift);
+                const float scale = ROWS > 1 ? s.r : row_lane<i>(s.r);
+                const uint2 codes = codes8<FMT, decltype(ordinary)::value>(lift, scale, v[i]);
+                if (t + i < a.T && k < K) store_bytes<8>(a.Q + (t + i) * a.ldq + k, K - k, codes);
+            });
+        };
+        if (__all(s.ordinary()))
+            store(std::true_type{});
+        else
+            store(std::false_type{});
     }
     if (!a.QT) return;
-    if constexpr (ROWS == 1) {                 // the largest of every column
+    bool ordinary = s.ordinary();
+    if constexpr (ROWS == 1) {                 // the scales of the columns, one to a thread
 #pragma unroll
         for (int j = 0; j < kVec; ++j) {
-            unsigned top = 0;
+            unsigned most = 0;
 #pragma unroll
-            for (int i = 0; i < kVec; ++i) top = max(top, abs_bits(v[i][j]));
-            top = max(top, unsigned(__shfl_xor(int(top), 16)));
-            top = max(top, unsigned(__shfl_xor(int(top), 32)));
-            if (lane < 16) tops[wave][c * kVec + j] = top;
+            for (int i = 0; i < kVec; ++i) most = max(most, abs_bits(v[i][j]));
+            most = column_max(most);
+            if (lane < 16) tops[wave][c * kVec + j] = most;
         }
         __syncthreads();
-    }
-    // Column f of the tile is row f of `turned`, whose 16-byte chunks are permuted by f / 8.
+        const int f = threadIdx.x;
+        ordinary = true;
+        if (f < kB) {
+            unsigned most = 0;
 #pragma unroll
-    for (int j = 0; j < kVec; ++j) {
-        const int f = c * kVec + j;
-        unsigned top = whole;
-        if constexpr (ROWS == 1) {
-#pragma unroll
-            for (int w = 0; w < kWaves; ++w) top = max(top, tops[w][f]);
+            for (int w = 0; w < kWaves; ++w) most = max(most, tops[w][f]);
+            const BlockScale<FMT> column(most);
+            column_r[f] = column.r;
+            column_lift[f] = column.lift;
+            if (k0 + f < K) a.scale_t[(t0 / kB) * a.ldscale_t + k0 + f] = column.scale;
+            ordinary = column.ordinary();
         }
-        const BlockScale<FMT> s(top);
-        if (ROWS == 1 && r == 0 && k0 + f < K) a.scale_t[(t0 / kB) * a.ldscale_t + k0 + f] = s.scale;
-        float column[kVec];
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) column[i] = v[i][j];
-        *reinterpret_cast<uint2 *>(turned + f * kB + (((r >> 1) ^ (c & 7)) << 4) + (r & 1) * 8) =
-            codes8(s, column);
+        ordinary = __syncthreads_and(ordinary);
     }
+    // Column f of the tile becomes row f of `turned`: rows are swapped in pairs and their 16-byte chunks
+    // permuted by f / 8, so that the 8 bytes of a wave's lanes meet every bank twice.
+    const auto turn = [&](auto plain) {
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) {
+            const int f = c * kVec + j;
+            float column[kVec];
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) column[i] = v[i][j];
+            const float lift = ROWS > 1 ? s.lift : column_lift[f], scale = ROWS > 1 ? s.r : column_r[f];
+            *reinterpret_cast<uint2 *>(turned + (f ^ (c & 1)) * kB + (((r >> 1) ^ (c >> 1)) << 4) +
+                                       (r & 1) * 8) = codes8<FMT, decltype(plain)::value>(lift, scale, column);
+        }
+    };
+    if (ordinary)
+        turn(std::true_type{});
+    else
+        turn(std::false_type{});
     __syncthreads();
 #pragma unroll
     for (int e = 0; e < kB * kB / 16 / kThreads; ++e) {
-        const int at = e * kThreads + threadIdx.x, f = at / 8, part = at % 8;
+        const int at = e * kThreads + threadIdx.x, f = at / 8, part = at % 8, of = f / kVec;
         const int64_t left = a.T - t0 - part * 16;
         if (k0 + f < K && left > 0)
             store_bytes<16>(a.QT + (k0 + f) * a.ldqt + t0 + part * 16, left,
-                            *reinterpret_cast<const uint4 *>(turned + f * kB + ((part ^ ((f >> 3) & 7)) << 4)));
+                            *reinterpret_cast<const uint4 *>(turned + (f ^ (of & 1)) * kB +
+                                                             ((part ^ (of >> 1)) << 4)));
     }
 }
 
