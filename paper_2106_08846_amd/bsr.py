@@ -1188,22 +1188,26 @@ def bsr_layer_norm_backward(dY: torch.Tensor, S: torch.Tensor, mean: torch.Tenso
         grad_dtype = S.dtype if given is None else given.dtype
     if grad_dtype not in _DATA_DTYPES:
         raise TypeError("grad_dtype must be float32 or bfloat16")
+    device = S.device
     made = []
 
     def make(*shape, dtype):
-        made.append(torch.empty(*shape, dtype=dtype, device=S.device))
+        made.append(torch.empty(*shape, dtype=dtype, device=device))
         return made[-1]
 
-    if need_dX and dX is None:
+    lddx = K
+    if dX is not None:
+        lddx = _matrix_arg(dX, "dX", T, K, kind)
+    elif need_dX:
         dX = make(T, K, dtype=S.dtype)
-    lddx = 0 if dX is None else _matrix_arg(dX, "dX", T, K, kind)
-    if affine and dgamma is None:
+    if dgamma is not None:
+        _vector_arg(dgamma, "dgamma", K, grad_dtype)
+    elif affine:
         dgamma = make(K, dtype=grad_dtype)
-    if affine and dbeta is None:
+    if dbeta is not None:
+        _vector_arg(dbeta, "dbeta", K, grad_dtype)
+    elif affine:
         dbeta = make(K, dtype=grad_dtype)
-    for t, name in ((dgamma, "dgamma"), (dbeta, "dbeta")):
-        if t is not None:
-            _vector_arg(t, name, K, grad_dtype)
     if workspace is None:
         if dgamma is not None or dbeta is not None:
             workspace = make(max(bsr_layer_norm_workspace_bytes(T, K), 1), dtype=torch.uint8)
@@ -1247,19 +1251,20 @@ def bsr_quantize_f8(X: torch.Tensor, block_rows: int = 1, q_dtype: torch.dtype =
         raise TypeError("q_dtype must be float8_e4m3fn or float8_e5m2")
     ldx = _matrix_arg(X, "X", None, None, _DATA_DTYPES)
     T, K = X.shape
+    device = X.device
     made = []
 
     def codes(t, name, rows, cols):
         if t is None:
-            pitch = (cols + 15) // 16 * 16
-            t = torch.empty(rows, pitch, dtype=q_dtype, device=X.device)
+            pitch = max((cols + 15) // 16 * 16, 16)
+            t = torch.empty_strided((rows, cols), (pitch, 1), dtype=q_dtype, device=device)
             made.append(t)
-            return (t if pitch == cols else t[:, :cols]), max(pitch, 1)
+            return t, pitch
         return t, _matrix_arg(t, name, rows, cols, (q_dtype,))
 
     def scales(t, name, rows, cols):
         if t is None:
-            t = torch.empty(rows, cols, dtype=_F32, device=X.device)
+            t = torch.empty(rows, cols, dtype=_F32, device=device)
             made.append(t)
             return t, max(cols, 1)
         return t, _matrix_arg(t, name, rows, cols, _F32_DTYPES)

@@ -17,18 +17,18 @@ constexpr int kF8TileCount = int(sizeof kF8Tiles / sizeof kF8Tiles[0]);
 
 // What a round of workgroups over the chip takes in each tile, in tenths of a microsecond at K = 4096
 // (MI355X, grids of 1 to 32 rounds), and what one workgroup takes that has its CU to itself: the smaller
-// tiles leave room for two to four on a CU.  0: not used, its registers do not hold it.  In this order:
-// rows on 16-byte boundaries or not; bf16 or fp32 output; a scale for 128 rows of B or for each.
-// So bf16 4096 x 4096 x 4096 with a weight's scales takes 64 us in 256 x 256 tiles, 76 in 128 x 128 and 107
-// in 64 x 64; 2048 x 2048 x 4096 58, 28 and 31.
+// tiles leave room for two to four on a CU.  0: not used, because its registers do not hold it or two rounds of
+// half its size take less.  In this order: rows on 16-byte boundaries or not; bf16 or fp32 output; a scale
+// for 128 rows of B or for each.  So bf16 4096 x 4096 x 4096 with a weight's scales takes 61 us in 256 x 256
+// tiles, 75 in 128 x 128 and 112 in 64 x 64; 2048 x 2048 x 4096 49, 27 and 31.
 struct F8Cost {
     int round[kF8TileCount], alone[kF8TileCount];
 };
 constexpr F8Cost kF8Costs[2][2][2] = {
-    {{{{979, 790, 700, 320, 140}, {979, 790, 700, 521, 270}}, {{0, 825, 700, 330, 143}, {0, 825, 700, 528, 270}}},
-     {{{0, 1140, 880, 525, 163}, {0, 1140, 880, 582, 330}}, {{0, 0, 910, 545, 168}, {0, 0, 910, 603, 330}}}},
-    {{{{640, 460, 372, 190, 67}, {640, 460, 372, 278, 140}}, {{726, 530, 415, 212, 71}, {726, 530, 415, 287, 145}}},
-     {{{1100, 797, 620, 330, 103}, {1100, 797, 620, 431, 210}}, {{0, 874, 665, 403, 110}, {0, 874, 665, 453, 215}}}}};
+    {{{{990, 783, 0, 340, 141}, {990, 783, 0, 510, 265}}, {{0, 835, 0, 343, 141}, {0, 835, 0, 518, 267}}},
+     {{{0, 1155, 885, 545, 168}, {0, 1155, 885, 592, 309}}, {{0, 0, 923, 588, 172}, {0, 0, 923, 633, 318}}}},
+    {{{{612, 430, 365, 190, 68}, {612, 430, 365, 268, 118}}, {{702, 500, 412, 204, 71}, {702, 500, 412, 270, 118}}},
+     {{{1090, 770, 620, 330, 103}, {1090, 770, 620, 433, 171}}, {{0, 845, 665, 408, 110}, {0, 845, 665, 459, 177}}}}};
 
 inline const F8Cost &f8_cost(bool aligned, bool wide, bool w_rows) {
     return kF8Costs[aligned ? 1 : 0][wide ? 1 : 0][w_rows ? 1 : 0];
@@ -68,6 +68,14 @@ inline int f8_largest(const F8Cost &c) {
     int i = 0;
     while (c.round[i] == 0) ++i;
     return i;
+}
+
+// Parts of the waves of a 64 x 64 workgroup (rows on 16-byte boundaries) that share out the blocks of a long
+// contraction where every workgroup has a CU to itself: 128 x 4096 x 4096 takes 13.3 us with one part, 10.6
+// with two and 10.9 with four (fp32 output 20.9, 16.1 and 15.9), 1024 x 1024 x 16384 60, 42 and 35.
+inline int f8_parts(int64_t M, int64_t N, int64_t K, int64_t cus) {
+    if (tiles_across(M, 64) * tiles_across(N, 64) > cus) return 1;
+    return K >= 8192 ? 4 : K >= 2048 ? 2 : 1;
 }
 
 // Whether a product goes to the kernel for few tokens: up to 32, or as many groups of 32 tokens x 16

@@ -14,10 +14,10 @@ template <class K, int BM> void launch_tiles(void (*kernel)(F8Args), F8Args a, v
                        as_stream(stream), a);
 }
 
-template <int BM, int BN, int WM, int WN, int XF, bool WROWS, bool WIDE, bool DIRECT>
+template <int BM, int BN, int WM, int WN, int XF, bool WROWS, bool WIDE, bool DIRECT, int PARTS = 1>
 void launch_ring(const F8Args &a, void *stream) {
-    launch_tiles<F8RingKernel<BM, BN, WM, WN, XF, WROWS, WIDE, DIRECT>, BM>(
-        f8_ring_kernel<BM, BN, WM, WN, XF, WROWS, WIDE, DIRECT>, a, stream);
+    launch_tiles<F8RingKernel<BM, BN, WM, WN, XF, WROWS, WIDE, DIRECT, PARTS>, BM>(
+        f8_ring_kernel<BM, BN, WM, WN, XF, WROWS, WIDE, DIRECT, PARTS>, a, stream);
 }
 template <int XF, bool WROWS, bool WIDE, bool DIRECT> void launch_tile(const F8Args &a, int tile, void *stream) {
     constexpr F8Cost cost = kF8Costs[DIRECT ? 1 : 0][WIDE ? 1 : 0][WROWS ? 1 : 0];
@@ -30,9 +30,18 @@ template <int XF, bool WROWS, bool WIDE, bool DIRECT> void launch_tile(const F8A
             if constexpr (cost.round[1] > 0)
                 return launch_ring<192, 256, 2, 4, XF, WROWS, WIDE, DIRECT>(a, stream);
             break;
-        case 2: return launch_ring<128, 256, 2, 4, XF, WROWS, WIDE, DIRECT>(a, stream);
+        case 2:
+            if constexpr (cost.round[2] > 0)
+                return launch_ring<128, 256, 2, 4, XF, WROWS, WIDE, DIRECT>(a, stream);
+            break;
         case 3: return launch_ring<128, 128, 2, 4, XF, WROWS, WIDE, DIRECT>(a, stream);
-        default: return launch_ring<64, 64, 2, 2, XF, WROWS, WIDE, DIRECT>(a, stream);
+        default:
+            if constexpr (DIRECT) {
+                const int parts = f8_parts(a.p.M, a.p.N, a.p.Kb, device_cu_count());
+                if (parts == 4) return launch_ring<64, 64, 2, 2, XF, WROWS, WIDE, DIRECT, 4>(a, stream);
+                if (parts == 2) return launch_ring<64, 64, 2, 2, XF, WROWS, WIDE, DIRECT, 2>(a, stream);
+            }
+            return launch_ring<64, 64, 2, 2, XF, WROWS, WIDE, DIRECT>(a, stream);
     }
 }
 
@@ -50,12 +59,19 @@ bool rows_aligned(const void *p, int64_t ld) {
     return ((reinterpret_cast<uintptr_t>(p) | uintptr_t(ld)) & 15) == 0;
 }
 
-template <int NT, int XF, bool WROWS> void launch_rows(const F8Args &a, bool aligned, void *stream) {
-    using K = F8RowsKernel<NT, XF, WROWS, true>;
-    const auto kernel = aligned ? f8_rows_kernel<NT, XF, WROWS, true> : f8_rows_kernel<NT, XF, WROWS, false>;
+template <int WAVES, int NT, int XF, bool WROWS> void launch_rows(const F8Args &a, bool aligned, void *stream) {
+    using K = F8RowsKernel<WAVES, NT, XF, WROWS, true>;
+    const auto kernel = aligned ? f8_rows_kernel<WAVES, NT, XF, WROWS, true>
+                                : f8_rows_kernel<WAVES, NT, XF, WROWS, false>;
     const unsigned groups_n = unsigned((a.p.N + K::kChannels - 1) / K::kChannels);
     const unsigned groups_m = unsigned((a.p.M + 16 * NT - 1) / (16 * NT));
     hipLaunchKernelGGL(kernel, dim3(groups_n, groups_m), dim3(64 * K::kWaves), 0, as_stream(stream), a);
+}
+template <int NT, int XF, bool WROWS>
+void launch_few(const F8Args &a, bool aligned, int64_t cus, void *stream) {
+    const int64_t groups = tiles_across(a.p.M, 16 * NT) * tiles_across(a.p.N, 16);
+    groups <= cus ? launch_rows<16, NT, XF, WROWS>(a, aligned, stream)
+                  : launch_rows<8, NT, XF, WROWS>(a, aligned, stream);
 }
 
 template <int XF, bool WROWS, bool WIDE> void product(const F8Args &a, void *stream) {
@@ -64,8 +80,8 @@ template <int XF, bool WROWS, bool WIDE> void product(const F8Args &a, void *str
     // 64 x 1024 x 4096 takes 9 us there and 14 in tiles (fp32 output 21), 128 x 1024 x 8192 14 and 25; two
     // rounds of it, 32 x 12288 x 4096, 20 and 19 (fp32 22).
     if (f8_few_tokens(M, a.p.N, cus))
-        return M <= 16 ? launch_rows<1, XF, WROWS>(a, aligned, stream)
-                       : launch_rows<2, XF, WROWS>(a, aligned, stream);
+        return M <= 16 ? launch_few<1, XF, WROWS>(a, aligned, cus, stream)
+                       : launch_few<2, XF, WROWS>(a, aligned, cus, stream);
     const F8Cost &cost = f8_cost(aligned, WIDE, WROWS);
     const auto launch = aligned ? launch_tile<XF, WROWS, WIDE, true> : launch_tile<XF, WROWS, WIDE, false>;
     const int large = f8_largest(cost);

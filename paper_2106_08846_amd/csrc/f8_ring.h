@@ -18,8 +18,8 @@
 
 namespace bsr {
 
-template <int BM, int BN, int WM, int WN, int XF, bool WROWS, bool WIDE, bool DIRECT> struct F8RingKernel {
-    static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves;
+template <int BM, int BN, int WM, int WN, int XF, bool WROWS, bool WIDE, bool DIRECT, int PARTS = 1> struct F8RingKernel {
+    static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves * PARTS;    // kWaves: of a part
     static constexpr int TM = BM / WM, TN = BN / WN;
     static constexpr int NM = TM / kMF, NN = TN / kMF;
     static constexpr int kRowBytes = kF8Block;
@@ -28,11 +28,16 @@ template <int BM, int BN, int WM, int WN, int XF, bool WROWS, bool WIDE, bool DI
     static constexpr int kScaleLoadsX = BM / 64, kScaleLoadsW = WROWS ? BN / 64 : 1;
     static constexpr int kScaleAt = (BM + BN) * kRowBytes, kScaleWAt = kScaleAt + BM * 4;
     static constexpr int kStageBytes = kScaleWAt + kScaleLoadsW * 256;
+    static constexpr int kStages = 2;        // four are no faster, not in the smallest tile either
     static constexpr int kEpiBytes = kWaves * epilogue_bytes(NN);
-    static constexpr int kLds = 2 * kStageBytes > kEpiBytes ? 2 * kStageBytes : kEpiBytes;
+    static constexpr int kPartBytes = kStages * kStageBytes;
+    static constexpr int kLds = PARTS * kPartBytes > kEpiBytes ? PARTS * kPartBytes : kEpiBytes;
+    // Parts hand their sums over through the stages, behind the epilogue's own LDS.
+    static constexpr int kSumBytes = NM * NN * 16 * 64 * kWaves;
+    static_assert(kLds >= (PARTS > 1 ? kEpiBytes + (PARTS - 1) * kSumBytes : 0), "room for the parts' sums");
     static constexpr int kTileN = BN;
     static_assert(BM % (8 * kWaves) == 0 && BN % (8 * kWaves) == 0 && BM % 64 == 0, "whole loads");
-    static_assert(kScaleLoadsX + kScaleLoadsW <= 2 * kWaves, "two scale loads of a wave at most");
+    static_assert(kScaleLoadsX + kScaleLoadsW <= kWaves, "one scale load of a wave");
     static_assert(kF8Block % TN == 0 && NM >= 2, "one scale of B for a wave's channels");
     static_assert(kLds <= 160 * 1024, "LDS of a CU");
 
@@ -44,8 +49,11 @@ template <int BM, int BN, int WM, int WN, int XF, bool WROWS, bool WIDE, bool DI
 
     static __device__ __forceinline__ void run(const F8Args &args, char *lds) {
         const ProductArgs &a = args.p;
-        const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+        const int lane = threadIdx.x & 63, part = uniform(threadIdx.x >> 6) / kWaves;
+        const int wave = uniform(threadIdx.x >> 6) % kWaves;
         const int wm = wave % WM, wn = wave / WM;
+        char *const all = lds;
+        lds += part * kPartBytes;
         const TileRows<BM, kTileN, false> rows(a);
         const Source &sa = rows.a, &sb = rows.b0;
         constexpr unsigned kOut = 0x80000000u;      // out of every range: loads zeros
@@ -68,12 +76,13 @@ template <int BM, int BN, int WM, int WN, int XF, bool WROWS, bool WIDE, bool DI
                                        : unsigned((a.N - 1) / kF8Block - w_first + 1 < (BN + 127) / 128
                                                       ? (a.N - 1) / kF8Block - w_first + 1
                                                       : (BN + 127) / 128) * 4;
-        const int steps = (a.Kb + kRowBytes - 1) / kRowBytes;
-        // A step's loads in pieces, by number: codes of A (DIRECT), of B, then the scales.  Steps past the end
-        // load zeros, and the last step's scales.
-        constexpr int kCodes = DIRECT ? PA + PB : 0, kPieces = kCodes + 2;
+        // Part p takes every PARTS-th block from p on; blocks past the end are zeros.
+        const int blocks = (a.Kb + kRowBytes - 1) / kRowBytes, steps = (blocks + PARTS - 1) / PARTS;
+        // A step's loads in pieces, by number: codes of A (DIRECT), of B, then scales, as many in every wave (some
+        // load the same scales).  Steps past the end load zeros, and the last step's scales.
+        constexpr int kCodes = DIRECT ? PA + PB : 0, kPieces = kCodes + 1;
         auto load = [&](int step, int piece) {
-            const int kb = step * kRowBytes;
+            const int block = step * PARTS + part, kb = block * kRowBytes;
             lds_char *stage = (lds_char *)lds + (step & 1) * kStageBytes;
             if (piece < kCodes) {
                 const bool of_a = piece < PA, in = kb + c0 < a.Kb;
@@ -84,17 +93,13 @@ template <int BM, int BN, int WM, int WN, int XF, bool WROWS, bool WIDE, bool DI
                     in ? (of_a ? oa : ob) : kOut, kb + i * kWaves * 8 * int(of_a ? sa.pitch : sb.pitch), 0, 0);
                 return;
             }
-            const int n = (piece - kCodes) * kWaves + wave;
-            const int64_t row = step < steps ? step : steps - 1;
-            stage += kScaleAt;
-            if (n < kScaleLoadsX)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer_rsrc(sx + row * args.ldsx, bytes_x),
-                                                         (lds_void *)(stage + n * 256), 4,
-                                                         n * 256 + lane * 4, 0, 0, 0);
-            else if (n < kScaleLoadsX + kScaleLoadsW)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer_rsrc(sw + row * args.ldsw, bytes_w),
-                                                         (lds_void *)(stage + BM * 4 + (n - kScaleLoadsX) * 256),
-                                                         4, (n - kScaleLoadsX) * 256 + lane * 4, 0, 0, 0);
+            const int n = wave % (kScaleLoadsX + kScaleLoadsW);
+            const int64_t row = block < blocks ? block : blocks - 1;
+            const bool of_x = n < kScaleLoadsX;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                of_x ? buffer_rsrc(sx + row * args.ldsx, bytes_x) : buffer_rsrc(sw + row * args.ldsw, bytes_w),
+                (lds_void *)(stage + kScaleAt + n * 256), 4,
+                (of_x ? n : n - kScaleLoadsX) * 256 + lane * 4, 0, 0, 0);
         };
         // !DIRECT: the codes of a step on their way through registers, in the same places.  Rows that do not
         // exist stand for the last one: they reach only outputs that do not exist.
@@ -106,7 +111,8 @@ template <int BM, int BN, int WM, int WN, int XF, bool WROWS, bool WIDE, bool DI
                 chunk[i].set(i < PA ? sa : sb, row0 + (i < PA ? i : i - PA) * kWaves * 8, c0, a.Kb);
         }
         auto take = [&](int step) {
-            const int kb = step * kRowBytes;
+            if (step >= steps) return;
+            const int kb = (step * PARTS + part) * kRowBytes;
             if (kb + kRowBytes <= a.Kb) {
 #pragma unroll
                 for (int i = 0; i < PA + PB; ++i) held[i] = chunk[i].load(kb, kChunk);
@@ -116,6 +122,7 @@ template <int BM, int BN, int WM, int WN, int XF, bool WROWS, bool WIDE, bool DI
             }
         };
         auto put = [&](int step) {
+            if (step >= steps) return;
             char *p = lds + (step & 1) * kStageBytes + wave * 1024 + lane * kChunk;
 #pragma unroll
             for (int i = 0; i < PA + PB; ++i)
@@ -127,10 +134,11 @@ template <int BM, int BN, int WM, int WN, int XF, bool WROWS, bool WIDE, bool DI
         auto clear_tail = [&](int step) {
             char *p = lds + (step & 1) * kStageBytes;
             const int c = a.Kb % kRowBytes / kChunk;
-            for (int row = threadIdx.x; row < BM + BN; row += kThreads) {
-                i32x4 *at = reinterpret_cast<i32x4 *>(p + row * kRowBytes + swizzled(row, c) * kChunk);
-                *at = first_bytes(*at, tail);
-            }
+            if (step * PARTS + part == blocks - 1)
+                for (int row = wave * 64 + lane; row < BM + BN; row += 64 * kWaves) {
+                    i32x4 *at = reinterpret_cast<i32x4 *>(p + row * kRowBytes + swizzled(row, c) * kChunk);
+                    *at = first_bytes(*at, tail);
+                }
             __syncthreads();
         };
         // This wave's reads of the stage are done and the next block's loads are there, for every wave.
@@ -191,12 +199,12 @@ template <int BM, int BN, int WM, int WN, int XF, bool WROWS, bool WIDE, bool DI
         meet(0);
 #pragma unroll
         for (int i = 0; i < kFirst; ++i) load(1, i);
-        if constexpr (!DIRECT) if (steps > 1) take(1);
+        if constexpr (!DIRECT) take(1);
         i32x8 fa[2];
         // Channel fragments have two sets of registers where they fit, and the next block's are read over
         // the last two i (8192^3 446 us, 455 with one set); in one set each is replaced as its last product
         // is issued.
-        constexpr int kSets = WIDE || (WROWS && BM * BN > 192 * 256) || (!DIRECT && BM * BN >= 192 * 256) ? 1 : 2;
+        constexpr int kSets = WIDE || !DIRECT || (WROWS && BM * BN > 192 * 256) ? 1 : 2;
         F8Fragment<BSR_E4M3, WIDE> fb[kSets][NN];
         float sxi[2];
         WScale swj[kWScales];
@@ -209,16 +217,18 @@ template <int BM, int BN, int WM, int WN, int XF, bool WROWS, bool WIDE, bool DI
         // The sums that wait to be added to the outputs, and their scales.
         f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
         WScale of{};
-        using Channels = F8Fragment<BSR_E4M3, WIDE>[NN];
-        auto block = [&](int s, const Channels &mine, Channels &next_b) {
+        // Block s, whose channel fragments are in the given set of registers.
+        auto block = [&](int s, auto set) {
+            constexpr int kMine = decltype(set)::value;
+            F8Fragment<BSR_E4M3, WIDE>(&mine)[NN] = fb[kMine], (&next_b)[NN] = fb[kSets - 1 - kMine];
             const char *now = lds + (s & 1) * kStageBytes, *then = lds + ((s + 1) & 1) * kStageBytes;
 #pragma unroll
             for (int i = 0; i < NM; ++i) {
                 if constexpr (!DIRECT)
-                    if (i == (NM > 2 ? NM - 3 : 0) && s + 1 < steps) put(s + 1);
+                    if (i == (NM > 2 ? NM - 3 : 0)) put(s + 1);
                 if (i == NM - 2) {
                     meet(s + 1);
-                    if constexpr (!DIRECT) if (s + 2 < steps) take(s + 2);
+                    if constexpr (!DIRECT) take(s + 2);
                 }
                 F8Fragment<XF, WIDE> x;
                 x.set(fa[i % 2]);
@@ -252,19 +262,39 @@ template <int BM, int BN, int WM, int WN, int XF, bool WROWS, bool WIDE, bool DI
                 }
             }
         };
+        using std::integral_constant;
         if constexpr (kSets == 1) {
-            for (int s = 0; s < steps; ++s) block(s, fb[0], fb[0]);
+            for (int s = 0; s < steps; ++s) block(s, integral_constant<int, 0>{});
         } else {
             int s = 0;
             for (; s + 1 < steps; s += 2) {
-                block(s, fb[0], fb[1]);
-                block(s + 1, fb[1], fb[0]);
+                block(s, integral_constant<int, 0>{});
+                block(s + 1, integral_constant<int, 1>{});
             }
-            if (s < steps) block(s, fb[0], fb[1]);
+            if (s < steps) block(s, integral_constant<int, 0>{});
         }
         add(acc[NN - 1][NM - 1], sum, of);
         __builtin_amdgcn_s_waitcnt(0x0070);      // loads past the end, before LDS is used again
         __syncthreads();
+        if constexpr (PARTS > 1) {               // the first part adds the others' sums, in order
+            f32x4 *sums = reinterpret_cast<f32x4 *>(all + kEpiBytes) + wave * 64 + lane;
+            constexpr int kStride = 64 * kWaves;
+            if (part > 0) {
+#pragma unroll
+                for (int j = 0; j < NN; ++j)
+#pragma unroll
+                    for (int i = 0; i < NM; ++i)
+                        sums[((part - 1) * NN * NM + j * NM + i) * kStride] = acc[j][i];
+            }
+            __syncthreads();
+            if (part > 0) return;
+#pragma unroll
+            for (int p = 0; p < PARTS - 1; ++p)
+#pragma unroll
+                for (int j = 0; j < NN; ++j)
+#pragma unroll
+                    for (int i = 0; i < NM; ++i) acc[j][i] += sums[(p * NN * NM + j * NM + i) * kStride];
+        }
         constexpr bool kPast = BM * BN >= 192 * 256;
         epilogue<bf16, Out::kScale, NN, NM, kPast>(
             a, acc, reinterpret_cast<float *>(lds + wave * epilogue_bytes(NN)), rows.m0 + wm * TM,
@@ -272,9 +302,9 @@ template <int BM, int BN, int WM, int WN, int XF, bool WROWS, bool WIDE, bool DI
     }
 };
 
-template <int BM, int BN, int WM, int WN, int XF, bool WROWS, bool WIDE, bool DIRECT>
-__global__ __launch_bounds__(64 * WM * WN) void f8_ring_kernel(F8Args a) {
-    using K = F8RingKernel<BM, BN, WM, WN, XF, WROWS, WIDE, DIRECT>;
+template <int BM, int BN, int WM, int WN, int XF, bool WROWS, bool WIDE, bool DIRECT, int PARTS = 1>
+__global__ __launch_bounds__(64 * WM * WN * PARTS) void f8_ring_kernel(F8Args a) {
+    using K = F8RingKernel<BM, BN, WM, WN, XF, WROWS, WIDE, DIRECT, PARTS>;
     __shared__ __align__(16) char lds[K::kLds];
     K::run(a, lds);
 }

@@ -1,11 +1,13 @@
 // The product of 8-bit floating-point matrices (f8_product.h) for few tokens: the weights go straight from
 // memory into the operand registers, and that read is the whole cost.
 //
-// A workgroup makes 16 channels for 16 NT tokens (blockIdx.y counts groups of them).  Its eight waves
-// split the contraction: wave w takes every eighth run of kHeld blocks, loads their codes and scales all
-// at once, and keeps its own scaled sums; they are added over the waves, in order, through LDS.  A single
-// token is bound by latency: 4096 columns are one run per wave, so that everything a workgroup needs is in
-// flight together.  Codes are widened to bf16 for either output type, which costs nothing beside the loads.
+// A workgroup makes 16 channels for 16 NT tokens (blockIdx.y counts groups of them).  Its waves split the
+// contraction: wave w takes every WAVES-th run of kHeld blocks, loads their codes and scales all at once,
+// and keeps its own scaled sums; they are added over the waves, in order, through LDS.  A single token is
+// bound by latency: 4096 columns are one run per wave, so that everything a workgroup needs is in flight
+// together.  Where every workgroup has a CU to itself sixteen waves share the work, else eight (one token,
+// 4096 to 4096: 6.0 and 6.7 us; 4096 to 12288: 15.4 and 13.7).  Codes are widened to bf16 for either output
+// type, which costs nothing beside the loads.
 #pragma once
 
 #include "f8_product.h"
@@ -37,9 +39,9 @@ template <> struct F8Chunks<false> : RowChunks<int8_t, Load::kShifted> {
     static __device__ __forceinline__ i32x4 cut(i32x4 v, int) { return v; }     // load() has zeros there
 };
 
-template <int NT, int XF, bool WROWS, bool ALIGNED> struct F8RowsKernel {
-    static constexpr int kWaves = 8, kChannels = 16;
-    static constexpr int kHeld = NT == 1 ? 4 : 2;        // blocks of a run
+template <int WAVES, int NT, int XF, bool WROWS, bool ALIGNED> struct F8RowsKernel {
+    static constexpr int kWaves = WAVES, kChannels = 16;
+    static constexpr int kHeld = NT == 1 && WAVES <= 8 ? 4 : 2;        // blocks of a run
     static constexpr int kLds = kWaves * NT * 64 * 16;
 
     static __device__ __forceinline__ void run(const F8Args &args, char *lds) {
@@ -127,9 +129,9 @@ template <int NT, int XF, bool WROWS, bool ALIGNED> struct F8RowsKernel {
     }
 };
 
-template <int NT, int XF, bool WROWS, bool ALIGNED>
-__global__ __launch_bounds__(512) void f8_rows_kernel(F8Args a) {
-    using K = F8RowsKernel<NT, XF, WROWS, ALIGNED>;
+template <int WAVES, int NT, int XF, bool WROWS, bool ALIGNED>
+__global__ __launch_bounds__(64 * WAVES) void f8_rows_kernel(F8Args a) {
+    using K = F8RowsKernel<WAVES, NT, XF, WROWS, ALIGNED>;
     __shared__ __align__(16) char lds[K::kLds];
     K::run(a, lds);
 }

@@ -31,13 +31,14 @@ void tiled(const F8Cost &c, int tile, int64_t M, int64_t N) {
         std::printf("tile %d for %lld, %lld\n", tile, (long long)M, (long long)N);
         std::exit(1);
     }
-    grid(f8_tiles(tile, M, N), kF8Tiles[tile].threads, 1, M, N);
+    const int parts = tile == 4 ? f8_parts(M, N, 1 << 20, 256) : 1;
+    grid(f8_tiles(tile, M, N), kF8Tiles[tile].threads * parts, 1, M, N);
 }
 
 void product(int64_t M, int64_t N, int64_t cus) {
     if (M < 1 || N < 1 || M > kDenseMaxTokens || N > kDenseMaxWidth || M * N > kDenseMaxOut) return;
     if (f8_few_tokens(M, N, cus))
-        return grid(tiles_across(N, 16), 512, tiles_across(M, M <= 16 ? 16 : 32), M, N);
+        return grid(tiles_across(N, 16), 1024, tiles_across(M, M <= 16 ? 16 : 32), M, N);
     for (int v = 0; v < 8; ++v) {
         const F8Cost &c = f8_cost(v & 1, v & 2, v & 4);
         const int large = f8_largest(c);
