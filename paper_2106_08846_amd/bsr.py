@@ -1188,29 +1188,28 @@ def bsr_layer_norm_backward(dY: torch.Tensor, S: torch.Tensor, mean: torch.Tenso
         grad_dtype = S.dtype if given is None else given.dtype
     if grad_dtype not in _DATA_DTYPES:
         raise TypeError("grad_dtype must be float32 or bfloat16")
-    device = S.device
     made = []
-
-    def make(*shape, dtype):
-        made.append(torch.empty(*shape, dtype=dtype, device=device))
-        return made[-1]
-
     lddx = K
     if dX is not None:
         lddx = _matrix_arg(dX, "dX", T, K, kind)
     elif need_dX:
-        dX = make(T, K, dtype=S.dtype)
+        dX = torch.empty_like(dY)
+        made.append(dX)
     if dgamma is not None:
         _vector_arg(dgamma, "dgamma", K, grad_dtype)
     elif affine:
-        dgamma = make(K, dtype=grad_dtype)
+        dgamma = torch.empty(K, dtype=grad_dtype, device=S.device)
+        made.append(dgamma)
     if dbeta is not None:
         _vector_arg(dbeta, "dbeta", K, grad_dtype)
     elif affine:
-        dbeta = make(K, dtype=grad_dtype)
+        dbeta = torch.empty(K, dtype=grad_dtype, device=S.device)
+        made.append(dbeta)
     if workspace is None:
         if dgamma is not None or dbeta is not None:
-            workspace = make(max(bsr_layer_norm_workspace_bytes(T, K), 1), dtype=torch.uint8)
+            workspace = torch.empty(_lib().bsr_layer_norm_workspace_bytes(T, K) or 1, dtype=torch.uint8,
+                                    device=S.device)
+            made.append(workspace)
     elif (not isinstance(workspace, torch.Tensor) or workspace.dtype != torch.uint8
             or workspace.dim() != 1 or not workspace.is_contiguous()):
         raise ValueError("workspace must be a contiguous uint8 tensor")
@@ -1232,6 +1231,24 @@ def _f8_blocks(n: int, rows: int = _F8_BLOCK) -> int:
     return (n + rows - 1) // rows
 
 
+def _f8_out(X, codes, scale, name: str, rows: int, cols: int, blocks: int, scales: int, q_dtype, made):
+    """One order's outputs of bsr_quantize_f8, checked where given and allocated where not: codes, their
+    pitch, scales, their pitch."""
+    if codes is None:
+        ldq = (cols + 15) // 16 * 16 or 16
+        codes = torch.empty_strided((rows, cols), (ldq, 1), dtype=q_dtype, device=X.device)
+        made.append(codes)
+    else:
+        ldq = _matrix_arg(codes, name, rows, cols, (q_dtype,))
+    if scale is None:
+        lds = scales or 1
+        scale = torch.empty(blocks, scales, dtype=_F32, device=X.device)
+        made.append(scale)
+    else:
+        lds = _matrix_arg(scale, "scale" if name == "Q" else "scale_t", blocks, scales, _F32_DTYPES)
+    return codes, ldq, scale, lds
+
+
 def bsr_quantize_f8(X: torch.Tensor, block_rows: int = 1, q_dtype: torch.dtype = torch.float8_e4m3fn,
                     form: str = "rows", Q: torch.Tensor | None = None,
                     scale: torch.Tensor | None = None, QT: torch.Tensor | None = None,
@@ -1251,34 +1268,18 @@ def bsr_quantize_f8(X: torch.Tensor, block_rows: int = 1, q_dtype: torch.dtype =
         raise TypeError("q_dtype must be float8_e4m3fn or float8_e5m2")
     ldx = _matrix_arg(X, "X", None, None, _DATA_DTYPES)
     T, K = X.shape
-    device = X.device
-    made = []
-
-    def codes(t, name, rows, cols):
-        if t is None:
-            pitch = max((cols + 15) // 16 * 16, 16)
-            t = torch.empty_strided((rows, cols), (pitch, 1), dtype=q_dtype, device=device)
-            made.append(t)
-            return t, pitch
-        return t, _matrix_arg(t, name, rows, cols, (q_dtype,))
-
-    def scales(t, name, rows, cols):
-        if t is None:
-            t = torch.empty(rows, cols, dtype=_F32, device=device)
-            made.append(t)
-            return t, max(cols, 1)
-        return t, _matrix_arg(t, name, rows, cols, _F32_DTYPES)
-
     if (form == "columns" and (Q is not None or scale is not None)) or (
             form == "rows" and (QT is not None or scale_t is not None)):
         raise ValueError(f'an output is given that form "{form}" does not make')
+    made = []
+    kb, tb = (K + 127) // 128, (T + 127) // 128
     ldq = ldscale = ldqt = ldscale_t = 0
     if form != "columns":
-        Q, ldq = codes(Q, "Q", T, K)
-        scale, ldscale = scales(scale, "scale", _f8_blocks(K), _f8_blocks(T, block_rows))
+        Q, ldq, scale, ldscale = _f8_out(X, Q, scale, "Q", T, K, kb, T if block_rows == 1 else tb, q_dtype,
+                                         made)
     if form != "rows":
-        QT, ldqt = codes(QT, "QT", K, T)
-        scale_t, ldscale_t = scales(scale_t, "scale_t", _f8_blocks(T), _f8_blocks(K, block_rows))
+        QT, ldqt, scale_t, ldscale_t = _f8_out(X, QT, scale_t, "QT", K, T, tb,
+                                               K if block_rows == 1 else kb, q_dtype, made)
     _one_device(X, Q, scale, QT, scale_t)
     _check(_lib().bsr_quantize_f8(_ptr(X), _DTYPE_CODE[X.dtype], T, K, ldx, block_rows, _F8_CODE[q_dtype],
                                   _ptr(Q), ldq, _ptr(scale), ldscale, _ptr(QT), ldqt, _ptr(scale_t),

@@ -264,6 +264,60 @@ def test_matmul_many_columns_of_scales():
            bound[:T2], "Y")
 
 
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_products_beside_a_large_one(out):
+    """1 - 1 + 2^-s in one group of eight: fp32 output keeps every s, bf16 output, whose sums the 8-bit matrix
+    instructions form, down to 2^-13 of the largest product; products in other groups are kept in both."""
+    T = N = 512                                        # enough for tiles
+    for s in range(4, 15):
+        for at in (2, 7, 8, 100):
+            x, w = np.zeros((T, 128), np.float32), np.zeros((N, 128), np.float32)
+            x[:, 0], w[:, 0], x[:, 1], w[:, 1] = 1, 1, -1, 1
+            x[:, at], w[:, at] = 2.0 ** -(s // 2), 2.0 ** -(s - s // 2)
+            one = torch.ones(1, T, device=DEV)
+            y = B.bsr_matmul_f8(codes(F.encode(x, "e4m3"), "e4m3"), one, codes(F.encode(w, "e4m3"), "e4m3"),
+                                one, out_dtype=TORCH[out])
+            kept = out == "f32" or s <= 13 or at >= 8
+            assert bool((y == (2.0 ** -s if kept else 0.0)).all()), (s, at)
+
+
+@pytest.mark.parametrize("T,N,K", [(1000003, 24, 64), (40, 100003, 48), (70001, 72, 130)])
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_matmul_long_and_narrow(T, N, K, out):
+    rng = np.random.default_rng(31)
+    x, w = (rng.integers(-4, 5, s).astype(np.float32) for s in ((T, K), (N, K)))
+    kb = -(-K // 128)
+    sx = (2.0 ** rng.integers(-1, 2, (kb, T))).astype(np.float32)
+    sw = (2.0 ** rng.integers(-1, 2, (kb, N))).astype(np.float32)
+    y = B.bsr_matmul_f8(codes(F.encode(x, "e4m3"), "e4m3"), torch.from_numpy(sx).to(DEV),
+                        codes(F.encode(w, "e4m3"), "e4m3"), torch.from_numpy(sw).to(DEV),
+                        out_dtype=TORCH[out])
+    want = 0
+    for b in range(kb):
+        k = slice(128 * b, 128 * b + 128)
+        part = torch.from_numpy(x[:, k]).to(DEV) @ torch.from_numpy(w[:, k]).to(DEV).t()
+        want = want + part * torch.from_numpy(sx[b]).to(DEV)[:, None] * torch.from_numpy(sw[b]).to(DEV)
+    assert torch.equal(y, want.to(TORCH[out]))        # integers and powers of two: exact
+
+
+def test_calls_side_by_side():
+    """Products and quantisations on two streams at once."""
+    rng = np.random.default_rng(15)
+    w = B.bsr_quantize_f8(rand(rng, 1100, 1024, sigma=0.02).to(DEV), 128)
+    xs = [rand(rng, T, 1024, dtype="bf16").to(DEV) for T in (900, 7)]
+    want = [B.bsr_matmul_f8(*B.bsr_quantize_f8(x), *w) for x in xs]
+    streams = [torch.cuda.Stream() for _ in xs]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(8):
+        for i, (x, s) in enumerate(zip(xs, streams)):
+            with torch.cuda.stream(s):
+                got[i].append(B.bsr_matmul_f8(*B.bsr_quantize_f8(x), *w))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(g, want[i]) for g in got[i])
+
+
 def test_streams_and_graphs():
     rng = np.random.default_rng(14)
     xs = [rand(rng, 300, 640, dtype="bf16").to(DEV) for _ in range(3)]

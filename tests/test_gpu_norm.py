@@ -171,6 +171,46 @@ def test_long_offsets():
     within(db, *got["dbeta"], "dbeta")
 
 
+def test_more_rows_than_a_launch():
+    T, K = (1 << 21) + 37, 8
+    rng = np.random.default_rng(10)
+    x = rand(rng, T, K, dtype="bf16")
+    X = x.to(DEV)
+    gamma = rand(rng, K) + 1.0
+    Y, S, mean, rstd = B.bsr_layer_norm(X, gamma.to(DEV), R=X, save=True)
+    s = x.float().numpy() * 2
+    want, bound = N.layer_norm(s, gamma.numpy(), out="bf16")
+    within(Y, want, bound, "Y")
+    dX, dg, db = B.bsr_layer_norm_backward(X, S, mean, rstd, gamma.to(DEV), grad_dtype=torch.float32)
+    got = N.backward(f64(x), s, f64(mean), f64(rstd), gamma.numpy(), out="bf16")
+    within(dX, *got["dX"], "dX")
+    within(dg, *got["dgamma"], "dgamma")
+    within(db, *got["dbeta"], "dbeta")
+
+
+def test_backward_side_by_side():
+    """Backward passes on two streams at once, with a workspace each."""
+    rng = np.random.default_rng(12)
+    T, K = 1100, 2304
+    sides = []
+    for i in range(2):
+        x, dy, gamma, _ = operands(rng, T, K, "bf16")
+        X, dY, g = dev(x), dev(dy), dev(gamma)
+        _, S, mean, rstd = B.bsr_layer_norm(X, g, save=True)
+        want = B.bsr_layer_norm_backward(dY, S, mean, rstd, g, grad_dtype=torch.float32)
+        ws = torch.empty(B.bsr_layer_norm_workspace_bytes(T, K), dtype=torch.uint8, device=DEV)
+        sides.append((torch.cuda.Stream(), (dY, S, mean, rstd, g), ws, want, []))
+    torch.cuda.synchronize()
+    for _ in range(8):
+        for stream, ops, ws, _, got in sides:
+            with torch.cuda.stream(stream):
+                got.append(B.bsr_layer_norm_backward(*ops, grad_dtype=torch.float32, workspace=ws))
+    torch.cuda.synchronize()
+    for _, _, _, want, got in sides:
+        for g in got:
+            assert all(torch.equal(p, q) for p, q in zip(g, want))
+
+
 def test_repeated_calls_and_streams():
     rng = np.random.default_rng(4)
     x, dy, gamma, beta = operands(rng, 1500, 1030, "bf16")
