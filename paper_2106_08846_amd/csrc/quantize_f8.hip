@@ -5,6 +5,10 @@
 // By rows alone a wave takes rows of 512 elements, four blocks side by side, each held by 16 lanes.
 // Everything else goes by tiles of 128 x 128 that stay in registers between the maxima and the codes; the
 // transpose is made of 8 x 8 pieces in the lanes and put together in LDS.
+//
+// MI355X: by rows 8192 x 4096 bf16 17.5 us (5.8 TB/s), in both orders 6144 x 2048 bf16 9.8 us (5.2 TB/s), fp32
+// 8192 x 4096 in blocks of 128 x 128 in both orders 39.5 us (5.1 TB/s).  Half of the first kernel's time was
+// the divisions of every lane for its block's scale, before the lanes shared them.
 #include <type_traits>
 #include <utility>
 
