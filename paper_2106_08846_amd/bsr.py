@@ -1138,7 +1138,7 @@ def bsr_layer_norm(X: torch.Tensor, gamma: torch.Tensor | None = None,
     if save:
         if mean is None:
             mean = torch.empty(T, dtype=_F32, device=X.device)
-            rstd = torch.empty(T, dtype=_F32, device=X.device)
+            rstd = torch.empty_like(mean)
             made += [mean, rstd]
         else:
             _vector_arg(mean, "mean", T)
@@ -1203,7 +1203,7 @@ def bsr_layer_norm_backward(dY: torch.Tensor, S: torch.Tensor, mean: torch.Tenso
     if dbeta is not None:
         _vector_arg(dbeta, "dbeta", K, grad_dtype)
     elif affine:
-        dbeta = torch.empty(K, dtype=grad_dtype, device=S.device)
+        dbeta = torch.empty_like(dgamma)
         made.append(dbeta)
     if workspace is None:
         if dgamma is not None or dbeta is not None:

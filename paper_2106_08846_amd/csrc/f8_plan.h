@@ -15,20 +15,26 @@ struct F8Tile {
 constexpr F8Tile kF8Tiles[] = {{256, 256, 512}, {192, 256, 512}, {128, 256, 512}, {128, 128, 512}, {64, 64, 256}};
 constexpr int kF8TileCount = int(sizeof kF8Tiles / sizeof kF8Tiles[0]);
 
-// What a round of workgroups over the chip takes in each tile, in tenths of a microsecond at K = 4096
-// (MI355X, grids of 1 to 32 rounds), and what one workgroup takes that has its CU to itself: the smaller
-// tiles leave room for two to four on a CU.  0: not used, because its registers do not hold it or two rounds of
-// half its size take less.  In this order: rows on 16-byte boundaries or not; bf16 or fp32 output; a scale
-// for 128 rows of B or for each.  So bf16 4096 x 4096 x 4096 with a weight's scales takes 61 us in 256 x 256
-// tiles, 75 in 128 x 128 and 112 in 64 x 64; 2048 x 2048 x 4096 49, 27 and 31.
+// What a round of workgroups over the chip takes in each tile, in tenths of a microsecond (MI355X, grids of
+// 1 to 64 rounds): at K = 4096 (`round`), of that independent of K (`fixed`: the first loads and the epilogue,
+// which a tile that fills its CU does not hide), and at K = 4096 where a workgroup has its CU to itself
+// (`alone`: the smaller tiles leave room for two to four on a CU).  0: not used, because its registers do not
+// hold it or two rounds of half its size take less.  In this order: rows on 16-byte boundaries or not; bf16
+// or fp32 output; a scale for 128 rows of B or for each.  So bf16 4096 x 4096 x 4096 with a weight's scales
+// takes 61 us in 256 x 256 tiles, 75 in 128 x 128 and 112 in 64 x 64; 2048 x 2048 x 4096 49, 27 and 31; and
+// 8192 x 8192 x 256 56, 47 and 65.
 struct F8Cost {
-    int round[kF8TileCount], alone[kF8TileCount];
+    int round[kF8TileCount], fixed[kF8TileCount], alone[kF8TileCount];
 };
 constexpr F8Cost kF8Costs[2][2][2] = {
-    {{{{990, 783, 0, 340, 141}, {990, 783, 0, 510, 265}}, {{0, 835, 0, 343, 141}, {0, 835, 0, 518, 267}}},
-     {{{0, 1155, 885, 545, 168}, {0, 1155, 885, 592, 309}}, {{0, 0, 923, 588, 172}, {0, 0, 923, 633, 318}}}},
-    {{{{612, 430, 365, 190, 68}, {612, 430, 365, 268, 118}}, {{702, 500, 412, 204, 71}, {702, 500, 412, 270, 118}}},
-     {{{1090, 770, 620, 330, 103}, {1090, 770, 620, 433, 171}}, {{0, 845, 665, 408, 110}, {0, 845, 665, 459, 177}}}}};
+    {{{{990, 783, 0, 340, 141}, {218, 157, 0, 45, 19}, {990, 783, 0, 510, 265}},
+      {{0, 835, 0, 343, 141}, {0, 156, 0, 46, 19}, {0, 835, 0, 518, 267}}},
+     {{{0, 1155, 885, 545, 168}, {0, 166, 140, 85, 27}, {0, 1155, 885, 592, 309}},
+      {{0, 0, 923, 588, 172}, {0, 0, 142, 84, 26}, {0, 0, 923, 633, 318}}}},
+    {{{{605, 430, 355, 183, 66}, {110, 68, 51, 19, 7}, {605, 430, 355, 268, 118}},
+      {{692, 500, 400, 200, 69}, {111, 67, 51, 18, 6}, {692, 500, 400, 270, 118}}},
+     {{{1070, 770, 612, 320, 100}, {166, 84, 69, 21, 7}, {1070, 770, 612, 433, 171}},
+      {{0, 843, 658, 404, 106}, {0, 85, 69, 39, 6}, {0, 843, 658, 459, 177}}}}};
 
 inline const F8Cost &f8_cost(bool aligned, bool wide, bool w_rows) {
     return kF8Costs[aligned ? 1 : 0][wide ? 1 : 0][w_rows ? 1 : 0];
@@ -36,32 +42,36 @@ inline const F8Cost &f8_cost(bool aligned, bool wide, bool w_rows) {
 inline int64_t f8_tiles(int tile, int64_t M, int64_t N) {
     return tiles_across(M, kF8Tiles[tile].bm) * tiles_across(N, kF8Tiles[tile].bn);
 }
-inline int64_t f8_tile_cost(const F8Cost &c, int tile, int64_t M, int64_t N, int64_t cus) {
-    const int64_t rounds = tiles_across(f8_tiles(tile, M, N), cus) * c.round[tile];
-    return rounds > c.alone[tile] ? rounds : c.alone[tile];
+// In units of 1 / 4096 of the table's.
+inline int64_t f8_tile_cost(const F8Cost &c, int tile, int64_t M, int64_t N, int64_t K, int64_t cus) {
+    const int64_t fixed = int64_t(c.fixed[tile]) * 4096;
+    const int64_t rounds =
+        tiles_across(f8_tiles(tile, M, N), cus) * (fixed + (c.round[tile] - c.fixed[tile]) * K);
+    const int64_t alone = fixed + (c.alone[tile] - c.fixed[tile]) * K;
+    return rounds > alone ? rounds : alone;
 }
-// The tile of least cost, the larger of equals.
-inline int f8_tile(const F8Cost &c, int64_t M, int64_t N, int64_t cus) {
+// The tile of least cost whose grid has under 2^32 threads, the larger of equals.
+inline int f8_tile(const F8Cost &c, int64_t M, int64_t N, int64_t K, int64_t cus) {
     int best = -1;
     int64_t least = 0;
     for (int i = 0; i < kF8TileCount; ++i) {
-        if (c.round[i] == 0) continue;
-        const int64_t cost = f8_tile_cost(c, i, M, N, cus);
+        if (c.round[i] == 0 || f8_tiles(i, M, N) * kF8Tiles[i].threads >= int64_t(1) << 32) continue;
+        const int64_t cost = f8_tile_cost(c, i, M, N, K, cus);
         if (best < 0 || cost < least) best = i, least = cost;
     }
     return best;
 }
 // A product whose last round of its largest tile is not full goes in two launches where that saves a
-// twentieth: as many channels as fill whole rounds, then the rest in the tile that suits it.  The channels
-// of the first launch, whole tiles; 0: one launch.
-inline int64_t f8_whole_rounds(const F8Cost &c, int large, int64_t M, int64_t N, int64_t cus) {
+// twentieth, the second launch's 2 us counted: as many channels as fill whole rounds, then the rest in the
+// tile that suits it.  The channels of the first launch, whole tiles; 0: one launch.
+inline int64_t f8_whole_rounds(const F8Cost &c, int large, int64_t M, int64_t N, int64_t K, int64_t cus) {
     const int64_t tiles_m = tiles_across(M, kF8Tiles[large].bm), tiles_n = tiles_across(N, kF8Tiles[large].bn);
     const int64_t columns = tiles_m * tiles_n / cus * cus / tiles_m;
     if (columns == 0 || columns == tiles_n) return 0;
     const int64_t first = columns * kF8Tiles[large].bn, rest = N - first;
-    const int64_t whole = f8_tile_cost(c, f8_tile(c, M, N, cus), M, N, cus);
-    const int64_t parts = f8_tile_cost(c, large, M, first, cus) +
-                          f8_tile_cost(c, f8_tile(c, M, rest, cus), M, rest, cus);
+    const int64_t whole = f8_tile_cost(c, f8_tile(c, M, N, K, cus), M, N, K, cus);
+    const int64_t parts = f8_tile_cost(c, large, M, first, K, cus) +
+                          f8_tile_cost(c, f8_tile(c, M, rest, K, cus), M, rest, K, cus) + 20 * 4096;
     return parts * 20 <= whole * 19 ? first : 0;
 }
 inline int f8_largest(const F8Cost &c) {

@@ -76,22 +76,22 @@ void launch_few(const F8Args &a, bool aligned, int64_t cus, void *stream) {
 
 template <int XF, bool WROWS, bool WIDE> void product(const F8Args &a, void *stream) {
     const bool aligned = rows_aligned(a.p.A, a.p.lda) && rows_aligned(a.p.B0, a.p.ldb0);
-    const int64_t cus = device_cu_count(), M = a.p.M;
+    const int64_t cus = device_cu_count(), M = a.p.M, N = a.p.N, K = a.p.Kb;
     // 64 x 1024 x 4096 takes 9 us there and 14 in tiles (fp32 output 21), 128 x 1024 x 8192 14 and 25; two
     // rounds of it, 32 x 12288 x 4096, 20 and 19 (fp32 22).
-    if (f8_few_tokens(M, a.p.N, cus))
+    if (f8_few_tokens(M, N, cus))
         return M <= 16 ? launch_few<1, XF, WROWS>(a, aligned, cus, stream)
                        : launch_few<2, XF, WROWS>(a, aligned, cus, stream);
     const F8Cost &cost = f8_cost(aligned, WIDE, WROWS);
     const auto launch = aligned ? launch_tile<XF, WROWS, WIDE, true> : launch_tile<XF, WROWS, WIDE, false>;
     const int large = f8_largest(cost);
-    const int64_t whole = f8_whole_rounds(cost, large, M, a.p.N, cus);
-    if (whole == 0) return launch(a, f8_tile(cost, M, a.p.N, cus), stream);
+    const int64_t whole = f8_whole_rounds(cost, large, M, N, K, cus);
+    if (whole == 0) return launch(a, f8_tile(cost, M, N, K, cus), stream);
     const F8Args rest = channels_from(a, whole, WROWS);
     F8Args first = a;
     first.p.N = whole;
     launch(first, large, stream);
-    launch(rest, f8_tile(cost, M, rest.p.N, cus), stream);
+    launch(rest, f8_tile(cost, M, rest.p.N, K, cus), stream);
 }
 template <int XF> void product(const F8Args &a, bool w_rows, void *stream) {
     const auto f = w_rows ? (a.p.out_bf16 ? product<XF, true, false> : product<XF, true, true>)

@@ -303,8 +303,9 @@ template <int BM, int BN, int WM, int WN, int XF, bool WROWS, bool WIDE, bool DI
 #pragma unroll
                     for (int i = 0; i < NM; ++i) acc[j][i] += sums[(p * NN * NM + j * NM + i) * kStride];
         }
-        constexpr bool kPast = BM * BN >= 192 * 256;
-        epilogue<bf16, Out::kScale, NN, NM, kPast>(
+        // Past the caches: 9616 x 768 x 656 with bf16 output takes 14.5 us through them and 12.3 so, 4096 x 1024
+        // x 1024 with fp32 output 17.8 and 16.1.
+        epilogue<bf16, Out::kScale, NN, NM, true>(
             a, acc, reinterpret_cast<float *>(lds + wave * epilogue_bytes(NN)), rows.m0 + wm * TM,
             rows.n0 + wn * TN);
     }

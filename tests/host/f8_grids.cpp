@@ -35,20 +35,20 @@ void tiled(const F8Cost &c, int tile, int64_t M, int64_t N) {
     grid(f8_tiles(tile, M, N), kF8Tiles[tile].threads * parts, 1, M, N);
 }
 
-void product(int64_t M, int64_t N, int64_t cus) {
+void product(int64_t M, int64_t N, int64_t K, int64_t cus) {
     if (M < 1 || N < 1 || M > kDenseMaxTokens || N > kDenseMaxWidth || M * N > kDenseMaxOut) return;
     if (f8_few_tokens(M, N, cus))
         return grid(tiles_across(N, 16), 1024, tiles_across(M, M <= 16 ? 16 : 32), M, N);
     for (int v = 0; v < 8; ++v) {
         const F8Cost &c = f8_cost(v & 1, v & 2, v & 4);
         const int large = f8_largest(c);
-        const int64_t whole = f8_whole_rounds(c, large, M, N, cus);
+        const int64_t whole = f8_whole_rounds(c, large, M, N, K, cus);
         if (whole == 0) {
-            tiled(c, f8_tile(c, M, N, cus), M, N);
+            tiled(c, f8_tile(c, M, N, K, cus), M, N);
         } else {
             if (whole % kF8Block || whole >= N) std::exit(1);
             tiled(c, large, M, whole);
-            tiled(c, f8_tile(c, M, N - whole, cus), M, N - whole);
+            tiled(c, f8_tile(c, M, N - whole, K, cus), M, N - whole);
         }
     }
 }
@@ -68,14 +68,15 @@ int main() {
                              (1 << 20) - 1, 1 << 20, (1 << 20) + 1, (1 << 24) - 1, 1 << 24};
     for (const int64_t cus : {1, 64, 256, 304}) {
         for (const int64_t M : sizes)
-            for (const int64_t N : sizes) product(M, N, cus);
-        for (const int64_t M : sizes) product(M, kDenseMaxOut / M, cus);
-        for (const int64_t N : sizes) product(kDenseMaxOut / N, N, cus);
+            for (const int64_t N : sizes)
+                for (const int64_t K : {int64_t(1), int64_t(300), kDenseMaxWidth}) product(M, N, K, cus);
+        for (const int64_t M : sizes) product(M, kDenseMaxOut / M, 4096, cus);
+        for (const int64_t N : sizes) product(kDenseMaxOut / N, N, 4096, cus);
     }
     for (int i = 0; i < 300000; ++i) {
         const int64_t M = int64_t(std::exp2(24 * unit())), most = kDenseMaxOut / M;
         const double bits = std::log2(double(most < kDenseMaxWidth ? most : kDenseMaxWidth));
-        product(M, int64_t(std::exp2(bits * (1 - unit() * unit()))), 256);
+        product(M, int64_t(std::exp2(bits * (1 - unit() * unit()))), int64_t(std::exp2(20 * unit())), 256);
     }
     std::printf("ok %lld\n", (long long)g_most);
     return 0;

@@ -158,27 +158,33 @@ def test_matmul(T, N, K, rows, x_fmt, pad, shift):
     assert torch.equal(again, y)
 
 
-@pytest.mark.parametrize("T,N", [(4096, 4096), (1536, 8192), (2048, 4096), (2050, 4099), (4900, 4096)])
+@pytest.mark.parametrize("T,N,K", [(4096, 4096, 272), (1536, 8192, 389), (2050, 4099, 389), (4900, 4096, 272),
+                                   (4096, 4096, 2064), (1536, 8192, 2053), (2048, 4096, 4112),
+                                   (3136, 8192, 2053)])
 @pytest.mark.parametrize("rows,x_fmt", [(128, "e4m3"), (1, "e5m2")])
 @pytest.mark.parametrize("out", ["f32", "bf16"])
-@pytest.mark.parametrize("K,pad", [(272, 0), (389, 0), (389, 11)])
-def test_matmul_large_tiles(T, N, rows, x_fmt, out, K, pad):
-    """Sizes that take each of the larger tiles, and two launches; tokens from every part of the grid."""
+@pytest.mark.parametrize("pad", [0, 7, -1])
+def test_matmul_large_tiles(T, N, K, rows, x_fmt, out, pad):
+    """Sizes that take each of the larger tiles, on and off 16-byte boundaries (pad -1: on), and two
+    launches; tokens from every part of the grid."""
     rng = np.random.default_rng(T + N + K)
+    pad = -K % 16 if pad < 0 else pad
     xq, sx, wq, sw = product_case(rng, T, N, K, rows, x_fmt)
     bias = rand(rng, N)
     y = B.bsr_matmul_f8(codes(xq, x_fmt, pad), torch.from_numpy(sx).to(DEV), codes(wq, "e4m3", pad),
                         torch.from_numpy(sw).to(DEV), bias.to(DEV), out_dtype=TORCH[out])
-    t = np.unique(np.concatenate([np.arange(0, T, 167), [T - 1, 127, 128, 191, 192, 255, 256]]))
+    t = np.unique(np.concatenate([np.arange(0, T, 167 if K < 1000 else 977), [T - 1, 127, 128, 191, 255, 256]]))
     want, bound = F.matmul(xq[t], sx[:, t], wq, sw, rows, bias.numpy(), x_fmt, out)
     within(y[torch.from_numpy(t).to(DEV)], want, bound, "Y")
     # the codes of integers, whose sums are exact, over the whole of it
-    x, w = (rng.integers(-4, 5, s).astype(np.float32) for s in ((T, K), (N, K)))
+    x, w = (torch.from_numpy(rng.integers(-4, 5, s).astype(np.float32)) for s in ((T, K), (N, K)))
     sx[:], sw[:] = 0.5, 0.25
-    one = B.bsr_matmul_f8(codes(F.encode(x, x_fmt), x_fmt, pad), torch.from_numpy(sx).to(DEV),
-                          codes(F.encode(w, "e4m3"), "e4m3", pad), torch.from_numpy(sw).to(DEV),
-                          out_dtype=TORCH[out])
-    exact = (torch.from_numpy(x).to(DEV) @ torch.from_numpy(w).to(DEV).t()) * 0.125
+
+    def small(v, fmt):
+        return codes(v.to(F8[fmt]).view(torch.uint8).numpy(), fmt, pad)
+    one = B.bsr_matmul_f8(small(x, x_fmt), torch.from_numpy(sx).to(DEV), small(w, "e4m3"),
+                          torch.from_numpy(sw).to(DEV), out_dtype=TORCH[out])
+    exact = (x.to(DEV) @ w.to(DEV).t()) * 0.125
     assert torch.equal(one, exact.to(TORCH[out]))
 
 
