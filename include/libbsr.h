@@ -602,12 +602,14 @@ LIBBSR_API bsr_status bsr_gated_i8(const int8_t *Xq, int64_t T, int64_t ldx, con
  *   Y[t][k] = (S[t][k] - mean[t]) * rstd[t] * gamma[k] + beta[k],
  * in fp32 throughout, Y rounded once to the type.  The mean is formed before the deviations, so a row far
  * from zero keeps its variance.  The statistics are fp32: of a row whose squared deviations sum to 2^128 or
- * more rstd is 0, and so is (S - mean) * rstd.  A NaN or an infinity in a row reaches that row only.
+ * more rstd is 0, and so is (S - mean) * rstd; a row whose magnitudes sum to 2^128 or more may give NaN.
+ * A NaN or an infinity in a row reaches that row only.
  * X, R, Y, S: device, T x K of `dtype` (BSR_F32 or BSR_BF16), row pitches >= K.  R may be NULL; S (written
  *   with R only) may be NULL.  gamma, beta: device fp32[K], each may be NULL (ones, zeros).  mean, rstd:
  *   device fp32[T], kept for bsr_layer_norm_backward, or both NULL.
- * T = 0 is a no-op; K >= 1; eps >= 0 and finite (with 0, a row of equal values gives NaN).  Outputs must
- * not overlap an input or each other (columns of one buffer at the same pitch in bytes do not).
+ * T = 0 is a no-op; K >= 1; eps >= 0 and finite (with 0, a row of equal values gives NaN, and deviations
+ * whose squares underflow infinities).  Outputs must not overlap an input or each other (columns of one
+ * buffer at the same pitch in bytes do not).
  * Errors: BSR_ERR_NULL (also: one of mean and rstd without the other), BSR_ERR_SHAPE, BSR_ERR_ARG (unknown
  *   dtype, eps, S without R, overlap), BSR_ERR_DTYPE (BSR_I8), BSR_ERR_UNSUPPORTED (K or a pitch above
  *   2^20, T above 2^24), BSR_ERR_ARCH, BSR_ERR_HIP.
@@ -655,9 +657,9 @@ typedef enum { BSR_E4M3 = 0, BSR_E5M2 = 1 } bsr_f8_format;
  * columns, shorter at the ends.  With a = max |x| over the block and m the format's largest value:
  *   s = a / m;  r = m / a;  q = x r, rounded to the nearest value of the format, ties to even;
  * every operation is rounded to fp32, so codes and scales are defined to the bit; x ~ s q.  A block with
- * a < 2^-64 is multiplied by 2^64 first (exact), for r and q only.  A block of zeros has q = 0 and s = 0.
- * One that holds an infinity has s = infinity and q = 0, one that holds a NaN s = NaN and q = 0: every
- * output of a product with it is NaN.
+ * a < 2^-64 is multiplied by 2^64 first (exact), for r and q only; an s below 2^-126 loses bits.  A block
+ * of zeros has q = 0 and s = 0.  One that holds an infinity has s = infinity and q = 0, one that holds a
+ * NaN s = NaN and q = 0: every output of a product with it is NaN.
  * block_rows = 1 is the form of activations and gradients, 128 that of a weight.
  * X: device, T x K of x_dtype (BSR_F32 or BSR_BF16), row pitch ldx >= K.
  * Q: device, T x K codes, row pitch ldq >= K; scale: device fp32, ceil(K / 128) x ceil(T / block_rows):
@@ -681,10 +683,10 @@ LIBBSR_API bsr_status bsr_quantize_f8(const void *X, bsr_dtype x_dtype, int64_t 
  *   Y[t][n] = sum over blocks b of  sx[b][t] sw[b][n'] * (sum over k in b of Xq[t][k] Wq[n][k])  +  bias[n],
  * b = k / 128 and n' = n / w_block_rows.  Products and sums are fp32, in an order fixed by the sizes
  * (repeated calls are bitwise reproducible); sx * sw is formed first, so where it lies below 2^-126 its
- * bits are lost.  bf16 output is rounded once, from the sum with the bias, and may come from the 8-bit
- * matrix instructions: of every eight consecutive products they drop what lies below 2^-13 of the largest
- * one's power of two (of a sum of normally distributed products about 1.5e-5, where bf16 rounds by 4e-3).
- * fp32 output keeps every product.
+ * bits are lost, and from 2^128 on it is infinite.  bf16 output is rounded once, from the sum with the
+ * bias, and may come from the 8-bit matrix instructions: of every eight consecutive products they drop
+ * what lies below 2^-13 of the largest one's power of two (of a sum of normally distributed products about
+ * 1.5e-5, where bf16 rounds by 4e-3).  fp32 output keeps every product.
  * With the codes and scales of bsr_quantize_f8 it is a layer's forward product (X by rows, W in blocks of
  * 128 rows), its way back to the inputs (dY by rows, W's transpose), and the gradient of W (dY's and X's
  * transposes with a scale for each row: w_block_rows = 1).

@@ -138,8 +138,9 @@ struct NormWorkspace {
     size_t bytes;
 };
 inline NormWorkspace layer_norm_workspace(int64_t T, int64_t K) {
-    const int64_t rows = K <= 1024 ? kNormPlaces[0] : K <= 4096 ? kNormPlaces[1] : K <= kNormFusedWidth ? kNormPlaces[2] : 64;
-    const int64_t most = K <= kNormFusedWidth ? 256 : 64;
+    const bool fused = K <= kNormFusedWidth;
+    const int64_t rows = K <= 1024 ? kNormPlaces[0] : K <= 4096 ? kNormPlaces[1] : fused ? kNormPlaces[2] : 64;
+    const int64_t most = fused ? 256 : 64;
     const int64_t groups = (T + rows - 1) / rows;
     const int64_t n = groups < most ? groups : most;
     return NormWorkspace{int(n), size_t(n > 0 ? n : 1) * 2 * size_t(K) * 4};

@@ -26,7 +26,8 @@
 
 namespace bsr {
 
-template <int BM, int BN, int WM, int WN, int XF, bool WROWS, bool WIDE, bool DIRECT, int PARTS = 1> struct F8RingKernel {
+template <int BM, int BN, int WM, int WN, int XF, bool WROWS, bool WIDE, bool DIRECT, int PARTS = 1>
+struct F8RingKernel {
     static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves * PARTS;    // kWaves: of a part
     static constexpr int TM = BM / WM, TN = BN / WN;
     static constexpr int NM = TM / kMF, NN = TN / kMF;
@@ -87,7 +88,8 @@ template <int BM, int BN, int WM, int WN, int XF, bool WROWS, bool WIDE, bool DI
         // Part p takes every PARTS-th block from p on; blocks past the end are zeros.
         const int blocks = (a.Kb + kRowBytes - 1) / kRowBytes, steps = (blocks + PARTS - 1) / PARTS;
         // A step's loads in pieces, by number: codes of A (DIRECT), of B, then scales, as many in every wave (some
-        // load the same scales).  Steps past the end load zeros, and the last step's scales.
+        // load the same scales).  Steps past the end load zeros, scales too: a part that has no block there
+        // adds 0, also where sx sw is infinite.
         constexpr int kCodes = DIRECT ? PA + PB : 0, kPieces = kCodes + 1;
         auto load = [&](int step, int piece) {
             const int block = step * PARTS + part, kb = block * kRowBytes;
@@ -102,12 +104,12 @@ template <int BM, int BN, int WM, int WN, int XF, bool WROWS, bool WIDE, bool DI
                 return;
             }
             const int n = wave % (kScaleLoadsX + kScaleLoadsW);
-            const int64_t row = block < blocks ? block : blocks - 1;
-            const bool of_x = n < kScaleLoadsX;
+            const bool of_x = n < kScaleLoadsX, in = block < blocks;
+            const int64_t row = in ? block : 0;
             __builtin_amdgcn_raw_ptr_buffer_load_lds(
                 of_x ? buffer_rsrc(sx + row * args.ldsx, bytes_x) : buffer_rsrc(sw + row * args.ldsw, bytes_w),
                 (lds_void *)(stage + kScaleAt + n * 256), 4,
-                (of_x ? n : n - kScaleLoadsX) * 256 + lane * 4, 0, 0, 0);
+                in ? (of_x ? n : n - kScaleLoadsX) * 256 + lane * 4 : kOut, 0, 0, 0);
         };
         // !DIRECT: the codes of a step on their way through registers, in the same places.  Rows that do not
         // exist stand for the last one: they reach only outputs that do not exist.

@@ -245,7 +245,8 @@ __global__ __launch_bounds__(64 * WAVES * ROWS) void norm_backward_kernel(NormGr
                     if (s * kSpan >= K) break;
 #pragma unroll
                     for (int i = 0; i < kVec; ++i) {
-                        const float dy = to_float(now.d[b][s][i]), h = (to_float(now.x[b][s][i]) - now.mean[b]) * now.rstd[b];
+                        const float dy = to_float(now.d[b][s][i]);
+                        const float h = (to_float(now.x[b][s][i]) - now.mean[b]) * now.rstd[b];
                         dgamma[s][i] = fmaf(dy, h, dgamma[s][i]);
                         dbeta[s][i] += dy;
                         const float g = dy * gamma[s][i];
@@ -472,7 +473,7 @@ bsr_status launch_layer_norm_backward(const void *dY, int64_t lddy, const void *
     const int groups = layer_norm_workspace(T, K).groups;
     const NormGradArgs a{dY, S, dS, gamma, mean, rstd, dX, vectors ? static_cast<float *>(workspace) : nullptr,
                          T, lddy, lds, ldds, lddx, int(K)};
-    if (T > 0) dtype == BSR_BF16 ? norm_backward<bf16>(a, groups, stream) : norm_backward<float>(a, groups, stream);
+    if (T > 0) (dtype == BSR_BF16 ? norm_backward<bf16> : norm_backward<float>)(a, groups, stream);
     if (vectors)
         (grad_dtype == BSR_BF16 ? join<bf16> : join<float>)(a.partial, groups, K, dgamma, dbeta, stream);
     return launch_status();

@@ -139,7 +139,8 @@ template <class T, int FMT> __global__ __launch_bounds__(kThreads) void quantize
 
 // Tiles of 128 x 128: a thread holds 8 rows of 8 columns.  ROWS: rows of a block by rows (1 or 128),
 // which is the width of one by columns.
-template <class T, int FMT, int ROWS> __global__ __launch_bounds__(kThreads) void quantize_tile_kernel(QuantizeArgs a) {
+template <class T, int FMT, int ROWS>
+__global__ __launch_bounds__(kThreads) void quantize_tile_kernel(QuantizeArgs a) {
     constexpr int kB = kF8Block, kWaves = kThreads / 64;
     __shared__ unsigned tops[kWaves][kB];
     __shared__ __align__(16) float column_r[kB], column_lift[kB];

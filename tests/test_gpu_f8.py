@@ -188,6 +188,48 @@ def test_matmul_large_tiles(T, N, K, rows, x_fmt, out, pad):
     assert torch.equal(one, exact.to(TORCH[out]))
 
 
+@pytest.mark.parametrize("T,N,K", [(200, 1000, 2048), (257, 520, 2170), (150, 1100, 2200), (513, 1024, 8700),
+                                   (512, 1000, 8200), (130, 2050, 8400), (193, 900, 8500)])
+@pytest.mark.parametrize("rows,x_fmt", [(128, "e4m3"), (1, "e5m2")])
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("pad", [0, -1])
+def test_matmul_long_contractions(T, N, K, rows, x_fmt, out, pad):
+    """Few tiles and many blocks of columns, whose number parts of a workgroup's waves may not divide."""
+    rng = np.random.default_rng(T + N + K)
+    pad = -K % 16 if pad < 0 else pad
+    xq, sx, wq, sw = product_case(rng, T, N, K, rows, x_fmt)
+    bias = rand(rng, N)
+    y = B.bsr_matmul_f8(codes(xq, x_fmt, pad), torch.from_numpy(sx).to(DEV), codes(wq, "e4m3", pad),
+                        torch.from_numpy(sw).to(DEV), bias.to(DEV), out_dtype=TORCH[out])
+    t = np.unique(np.append(np.arange(0, T, 41), [63, 64, 127, 128, T - 1]))
+    want, bound = F.matmul(xq[t], sx[:, t], wq, sw, rows, bias.numpy(), x_fmt, out)
+    within(y[torch.from_numpy(t).to(DEV)], want, bound, "Y")
+    # integers and powers of two, whose sums are exact, over the whole of it
+    x, w = (torch.from_numpy(rng.integers(-4, 5, s).astype(np.float32)) for s in ((T, K), (N, K)))
+    sx[:], sw[:] = 0.5, 0.25
+    x8, w8 = (codes(v.to(F8[f]).view(torch.uint8).numpy(), f, pad) for v, f in ((x, x_fmt), (w, "e4m3")))
+    one = B.bsr_matmul_f8(x8, torch.from_numpy(sx).to(DEV), w8, torch.from_numpy(sw).to(DEV),
+                          out_dtype=TORCH[out])
+    exact = (x.to(DEV) @ w.to(DEV).t()) * 0.125
+    assert torch.equal(one, exact.to(TORCH[out]))
+
+
+@pytest.mark.parametrize("T,N,K", [(8, 40, 2170), (200, 1000, 2170), (300, 700, 8200), (1100, 1300, 700)])
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [1, 128])
+@pytest.mark.parametrize("pad", [3, -1])
+def test_scales_whose_product_overflows(T, N, K, out, rows, pad):
+    """sx sw is formed first: where it passes the largest fp32 value the outputs are infinite, not NaN."""
+    pad = -K % 16 if pad < 0 else pad
+    kb = -(-K // 128)
+    sx = torch.ones(kb, T, device=DEV)
+    sw = torch.ones(kb, -(-N // rows), device=DEV)
+    sx[kb - 1], sw[kb - 1] = 2.0 ** 70, 2.0 ** 70
+    x, w = (codes(F.encode(np.ones(s, np.float32), "e4m3"), "e4m3", pad) for s in ((T, K), (N, K)))
+    y = B.bsr_matmul_f8(x, sx, w, sw, out_dtype=TORCH[out])
+    assert bool((y == float("inf")).all())
+
+
 @pytest.mark.parametrize("T,N,K", [(1, 48, 4096), (19, 70, 770), (200, 300, 1000), (600, 700, 512)])
 @pytest.mark.parametrize("rows", [1, 128])
 def test_matmul_exact(T, N, K, rows):

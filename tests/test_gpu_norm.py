@@ -131,7 +131,8 @@ def test_special_rows(dtype, K):
     beta = torch.linspace(-1, 1, K)
     Y, S, mean, rstd = B.bsr_layer_norm(t.to(DEV), None, beta.to(DEV), save=True)
     y = f64(Y)
-    want, bound = N.layer_norm(t.double().numpy(), None, beta.numpy(), 1e-5, dtype)
+    with np.errstate(all="ignore"):                  # the rows that are not finite
+        want, bound = N.layer_norm(t.double().numpy(), None, beta.numpy(), 1e-5, dtype)
     for row in (0, 1, 5, 7, 8, 9):
         assert np.all(np.abs(y[row] - want[row]) <= bound[row]), row
     assert np.all(np.isnan(y[2:5]).any(1)) and np.all(np.isnan(f64(rstd)[2:5]))
