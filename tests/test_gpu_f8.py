@@ -158,6 +158,15 @@ def test_matmul(T, N, K, rows, x_fmt, pad, shift):
     assert torch.equal(again, y)
 
 
+@pytest.mark.parametrize("T,N,K", [(1, 4500, 4301), (16, 5000, 4232), (17, 4201, 2500), (32, 9000, 301),
+                                   (5, 5003, 130), (32, 64, 9001), (64, 500, 4500), (2, 12300, 512)])
+@pytest.mark.parametrize("rows,x_fmt", [(128, "e4m3"), (1, "e5m2")])
+@pytest.mark.parametrize("pad,shift", [(1, 3), (-1, 0)])
+def test_matmul_few_tokens(T, N, K, rows, x_fmt, pad, shift):
+    """More channels than a round of the chip holds, more blocks than a workgroup's waves take at once."""
+    test_matmul(T, N, K, rows, x_fmt, pad, shift)
+
+
 @pytest.mark.parametrize("T,N,K", [(4096, 4096, 272), (1536, 8192, 389), (2050, 4099, 389), (4900, 4096, 272),
                                    (4096, 4096, 2064), (1536, 8192, 2053), (2048, 4096, 4112),
                                    (3136, 8192, 2053)])

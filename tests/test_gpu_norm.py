@@ -86,6 +86,19 @@ def test_backward(T, K, dtype, grad, pad, shift, extra):
     assert clean()
 
 
+# Several rounds over the rows for a workgroup of the backward pass; forward, rows of up to 4096 columns on a
+# wave.  Every width of a workgroup, and every end of a row.
+MANY_ROWS = [(4103, 96), (6151, 520), (4099, 1024), (2051, 1531), (2049, 2056), (2050, 4096), (1031, 4095),
+             (771, 5000), (514, 4099), (515, 8192), (259, 16383), (201, 16392)]
+
+
+@pytest.mark.parametrize("T,K", MANY_ROWS)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_many_rows(T, K, dtype):
+    test_norm(T, K, dtype, 8, 0, True)
+    test_backward(T, K, dtype, "f32", 8, 0, (T + K) % 2 == 0)
+
+
 @pytest.mark.parametrize("T,K", [(37, 768), (9, 2050), (4, 20000)])
 def test_parts_of_the_gradients(T, K):
     """Each gradient alone has the bits of all of them together; the workspace may be the caller's."""
