@@ -80,11 +80,14 @@ inline int f8_largest(const F8Cost &c) {
     return i;
 }
 
-// Parts of the waves of a 64 x 64 workgroup (rows on 16-byte boundaries) that share out the blocks of a long
-// contraction where every workgroup has a CU to itself: 128 x 4096 x 4096 takes 13.3 us with one part, 10.6
-// with two and 10.9 with four (fp32 output 20.9, 16.1 and 15.9), 1024 x 1024 x 16384 60, 42 and 35.
-inline int f8_parts(int64_t M, int64_t N, int64_t K, int64_t cus) {
+// Parts of the waves of a 64 x 64 workgroup that share out the blocks of a long contraction where every
+// workgroup has a CU to itself.  Rows on 16-byte boundaries: 128 x 4096 x 4096 takes 13.3 us with one part,
+// 10.6 with two and 10.9 with four (fp32 output 20.9, 16.1 and 15.9), 1024 x 1024 x 16384 60, 42 and 35.
+// Others go through registers, too many for four parts where B has a scale for each row (1000 x 1000 x 8191
+// with fp32 output 57, 48 and 70 us); 333 x 1024 x 1531 takes 15.8 and 14.8 us, 333 x 2304 x 770 8.9 and 9.0.
+inline int f8_parts(bool aligned, int64_t M, int64_t N, int64_t K, int64_t cus) {
     if (tiles_across(M, 64) * tiles_across(N, 64) > cus) return 1;
+    if (!aligned) return K >= 1024 ? 2 : 1;
     return K >= 8192 ? 4 : K >= 2048 ? 2 : 1;
 }
 

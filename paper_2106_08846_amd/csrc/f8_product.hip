@@ -36,11 +36,10 @@ template <int XF, bool WROWS, bool WIDE, bool DIRECT> void launch_tile(const F8A
             break;
         case 3: return launch_ring<128, 128, 2, 4, XF, WROWS, WIDE, DIRECT>(a, stream);
         default:
-            if constexpr (DIRECT) {
-                const int parts = f8_parts(a.p.M, a.p.N, a.p.Kb, device_cu_count());
+            const int parts = f8_parts(DIRECT, a.p.M, a.p.N, a.p.Kb, device_cu_count());
+            if constexpr (DIRECT)
                 if (parts == 4) return launch_ring<64, 64, 2, 2, XF, WROWS, WIDE, DIRECT, 4>(a, stream);
-                if (parts == 2) return launch_ring<64, 64, 2, 2, XF, WROWS, WIDE, DIRECT, 2>(a, stream);
-            }
+            if (parts == 2) return launch_ring<64, 64, 2, 2, XF, WROWS, WIDE, DIRECT, 2>(a, stream);
             return launch_ring<64, 64, 2, 2, XF, WROWS, WIDE, DIRECT>(a, stream);
     }
 }

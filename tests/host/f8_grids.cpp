@@ -31,7 +31,7 @@ void tiled(const F8Cost &c, int tile, int64_t M, int64_t N) {
         std::printf("tile %d for %lld, %lld\n", tile, (long long)M, (long long)N);
         std::exit(1);
     }
-    const int parts = tile == 4 ? f8_parts(M, N, 1 << 20, 256) : 1;
+    const int parts = tile == 4 ? f8_parts(true, M, N, 1 << 20, 256) : 1;
     grid(f8_tiles(tile, M, N), kF8Tiles[tile].threads * parts, 1, M, N);
 }
 
