@@ -9,15 +9,17 @@
 // They have most of a block's products to arrive.
 //
 // DIRECT (rows on 16-byte boundaries): codes go straight from memory into LDS.  Otherwise they go through
-// registers, loaded at the same point and written shortly before the next meeting.
+// registers, loaded byte-aligned at the same point and written shortly before the next meeting (128 x 4096 x
+// 4095 takes 26 us so in one part, 34 where the codes are shifted out of aligned words).
 //
 // PARTS: so many groups of WM x WN waves share out the blocks of a contraction, each with stages of its own,
 // and add their sums at the end.
 //
-// MI355X, 8192^3: bf16 output 452 us (2.43 Pflop/s; the matrix units busy 61% of the cycles at the 1.9 GHz that
-// the card's power leaves them; the library's product with one scale takes 339).  fp32 output 1.35 Pflop/s,
-// and with a scale for each row of B 1.1: there the vector instructions (12 and 18 to four matrix
-// instructions) and the matrix instructions take turns (with a scale for each row 47% and 42% of the cycles).
+// MI355X, 8192^3: bf16 output 447 to 470 us, card by card (2.4 Pflop/s; the matrix units busy 61% of the
+// cycles at the 1.9 GHz that the power leaves them; the library's product with one scale takes 339).  fp32
+// output 1.35 Pflop/s, and with a scale for each row of B 1.1: there the vector instructions (12 and 18 to
+// four matrix instructions) and the matrix instructions take turns (with a scale for each row 47% and 42% of
+// the cycles).
 #pragma once
 
 #include <type_traits>

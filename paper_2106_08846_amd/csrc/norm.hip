@@ -225,8 +225,8 @@ __global__ __launch_bounds__(64 * WAVES * ROWS) void norm_backward_kernel(NormGr
         }
     };
     // The next rows are loaded before this round's sums are joined, where the registers hold them and no lane
-    // asks for the end of its row: 8192 x 4096 bf16 with dS takes 49 us so and 55 without (2048 x 8192 on
-    // sixteen waves 34 and 33).
+    // asks for the end of its row: 8192 x 4096 bf16 with dS takes this kernel 49 us so and 55 without
+    // (2048 x 8192 on sixteen waves 34 and 33).
     constexpr bool kAhead = END != kAnyEnd && WAVES <= 4;
     Batch next = {};
     if (kAhead) fetch(int64_t(blockIdx.x) * ROWS, next);
