@@ -273,6 +273,31 @@ def test_matmul_not_finite(T, N, K):
     assert np.all((np.abs(Y - clean[0]) <= clean[1])[~bad])
 
 
+@pytest.mark.parametrize("T,N,K", [(5, 40, 300), (150, 200, 300), (260, 600, 2300), (700, 1500, 200)])
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("pad", [5, -1])
+def test_codes_that_are_not_finite(T, N, K, out, pad):
+    """A NaN code of a token or a channel gives NaN there; an infinite code of a token (E5M2) infinities of
+    its products' signs, NaN where the channel's code is 0; the rest stays within its bound."""
+    rng = np.random.default_rng(T + K)
+    pad = -K % 16 if pad < 0 else pad
+    xq, sx, wq, sw = product_case(rng, T, N, K, 128, "e5m2")
+    nan_k, inf_k, w_k = K - 1, K // 2, 17
+    wq[:, inf_k] = F.encode(np.where(np.arange(N) % 3 == 0, 0.0, np.where(np.arange(N) % 3 == 1, 1.5, -2.0))
+                            .astype(np.float32), "e4m3")
+    xq[:, [inf_k, nan_k, w_k]] = 0
+    clean, bound = F.matmul(xq, sx, wq, sw, 128, None, "e5m2", out)
+    xq[2, inf_k], xq[3, inf_k], xq[4, nan_k], wq[11, w_k] = 0x7C, 0xFC, 0x7F, 0x7F
+    want = clean.copy()
+    sign = np.array([np.nan, 1.0, -1.0])[np.arange(N) % 3]
+    want[2], want[3], want[4], want[:, 11] = np.inf * sign, -np.inf * sign, np.nan, np.nan
+    y = f64(B.bsr_matmul_f8(codes(xq, "e5m2", pad), torch.from_numpy(sx).to(DEV), codes(wq, "e4m3", pad),
+                            torch.from_numpy(sw).to(DEV), out_dtype=TORCH[out]))
+    special = ~np.isfinite(want)
+    assert np.array_equal(y[special], want[special], equal_nan=True)
+    assert np.all((np.abs(y - clean) <= bound)[~special])
+
+
 def test_matmul_of_views():
     """Tokens, blocks and channels cut out of larger matrices, with the scales' views."""
     rng = np.random.default_rng(8)
