@@ -34,7 +34,7 @@ constexpr F8Cost kF8Costs[2][2][2] = {
     {{{{605, 430, 355, 183, 66}, {110, 68, 51, 19, 7}, {605, 430, 355, 268, 118}},
       {{692, 500, 400, 200, 69}, {111, 67, 51, 18, 6}, {692, 500, 400, 270, 118}}},
      {{{1070, 770, 612, 320, 100}, {166, 84, 69, 21, 7}, {1070, 770, 612, 433, 171}},
-      {{0, 843, 658, 404, 106}, {0, 85, 69, 39, 6}, {0, 843, 658, 459, 177}}}}};
+      {{1210, 843, 658, 404, 106}, {170, 85, 69, 39, 6}, {1210, 843, 658, 459, 177}}}}};
 
 inline const F8Cost &f8_cost(bool aligned, bool wide, bool w_rows) {
     return kF8Costs[aligned ? 1 : 0][wide ? 1 : 0][w_rows ? 1 : 0];

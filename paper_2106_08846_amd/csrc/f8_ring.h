@@ -4,9 +4,9 @@
 // A wave's order of work in a block: token fragment i meets the channel fragments j in turn.  The sums of
 // (i, j) are added to the outputs while the matrix unit forms those of the next pair.  A token fragment is
 // read from LDS two i before its use, a channel fragment over the last two i of the block before, so the
-// reads of a block end two i before its products do: there every wave waits for the next block's data
-// and meets the others, and the loads of the block after that go into the stage that is free from then on.
-// They have most of a block's products to arrive.
+// reads of a block end two i before its products do (kDepth; one i in the tile with the least registers left):
+// there every wave waits for the next block's data and meets the others, and the loads of the block after
+// that go into the stage that is free from then on.  They have most of a block's products to arrive.
 //
 // DIRECT (rows on 16-byte boundaries): codes go straight from memory into LDS.  Otherwise they go through
 // registers, loaded byte-aligned at the same point and written shortly before the next meeting (128 x 4096 x
@@ -47,6 +47,11 @@ struct F8RingKernel {
     static constexpr int kSumBytes = NM * NN * 16 * 64 * kWaves;
     static_assert(kLds >= (PARTS > 1 ? kEpiBytes + (PARTS - 1) * kSumBytes : 0), "room for the parts' sums");
     static constexpr int kTileN = BN;
+    // How many i ahead token fragments are read.  256 x 256 with widened codes and a scale for each row of B takes
+    // more than the 256 registers of a wave (nine go to memory, two ahead 25), and still gains on two rounds of
+    // half the tile: 8192 x 2048 x 6144 191 us and 205, 4096 x 4096 x 4096 121 and 133, 8192^3 922 and 966.
+    static constexpr int kDepth = WIDE && WROWS && BM * BN > 192 * 256 ? 1 : 2;
+    static_assert(DIRECT || kDepth == 2, "codes on their way through registers are put in place two i ahead");
     static_assert(BM % (8 * kWaves) == 0 && BN % (8 * kWaves) == 0 && BM % 64 == 0, "whole loads");
     static_assert(kScaleLoadsX + kScaleLoadsW <= kWaves, "one scale load of a wave");
     static_assert(kF8Block % TN == 0 && NM >= 2, "one scale of B for a wave's channels");
@@ -203,7 +208,7 @@ struct F8RingKernel {
         // few products.  The first kFirst come before the block ends, the others in the next.
         constexpr int kSlots = NM * NN, kApart = 2 * kPieces <= kSlots ? 2 : 1;
         constexpr int kPerSlot = (kPieces + kSlots - 1) / kSlots;
-        constexpr int kBeforeEnd = (2 * NN + kApart - 1) / kApart * kPerSlot;
+        constexpr int kBeforeEnd = (kDepth * NN + kApart - 1) / kApart * kPerSlot;
         constexpr int kFirst = kBeforeEnd < kPieces ? kBeforeEnd : kPieces;
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) load(0, i);
@@ -212,20 +217,20 @@ struct F8RingKernel {
 #pragma unroll
         for (int i = 0; i < kFirst; ++i) load(1, i);
         if constexpr (!DIRECT) take(1);
-        i32x8 fa[2];
+        i32x8 fa[kDepth];
         // Channel fragments have two sets of registers where they fit, and the next block's are read over
         // the last two i (8192^3 446 us, 455 with one set); in one set each is replaced as its last product
         // is issued.
         constexpr int kSets = WIDE || !DIRECT || (WROWS && BM * BN > 192 * 256) ? 1 : 2;
         F8Fragment<BSR_E4M3, WIDE> fb[kSets][NN];
-        float sxi[2];
+        float sxi[kDepth];
         WScale swj[kWScales];
 #pragma unroll
         for (int j = 0; j < NN; ++j) fb[0][j].set(fetch_b(lds, j));
 #pragma unroll
         for (int j = 0; j < kWScales; ++j) swj[j] = fetch_sw(lds, j);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) fa[i] = fetch_a(lds, i), sxi[i] = fetch_sx(lds, i);
+        for (int i = 0; i < kDepth; ++i) fa[i] = fetch_a(lds, i), sxi[i] = fetch_sx(lds, i);
         // The sums that wait to be added to the outputs, and their scales.
         f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
         WScale of{};
@@ -238,29 +243,29 @@ struct F8RingKernel {
             for (int i = 0; i < NM; ++i) {
                 if constexpr (!DIRECT)
                     if (i == (NM > 2 ? NM - 3 : 0)) put(s + 1);
-                if (i == NM - 2) {
+                if (i == NM - kDepth) {
                     meet(s + 1);
                     if constexpr (!DIRECT) take(s + 2);
                 }
                 F8Fragment<XF, WIDE> x;
-                x.set(fa[i % 2]);
-                const float scale = sxi[i % 2];
-                const char *from = i + 2 < NM ? now : then;
-                const int next = i + 2 < NM ? i + 2 : i + 2 - NM;
+                x.set(fa[i % kDepth]);
+                const float scale = sxi[i % kDepth];
+                const char *from = i + kDepth < NM ? now : then;
+                const int next = (i + kDepth) % NM;
 #pragma unroll
                 for (int j = 0; j < NN; ++j) {
                     const f32x4 more = block_sums<XF>(mine[j], x);
-                    const int slot = (i + 2) % NM * NN + j;
+                    const int slot = (i + kDepth) % NM * NN + j;
 #pragma unroll
                     for (int p = 0; p < kPieces; ++p)
-                        if (p / kPerSlot * kApart == slot) load(i < NM - 2 ? s + 1 : s + 2, p);
+                        if (p / kPerSlot * kApart == slot) load(i < NM - kDepth ? s + 1 : s + 2, p);
                     __builtin_amdgcn_sched_barrier(0);
                     add(acc[j > 0 ? j - 1 : NN - 1][j > 0 ? i : i > 0 ? i - 1 : NM - 1], sum, of);
                     sum = more;
                     if (WROWS || j == 0) of = swj[WROWS ? j : 0] * scale;
                     // a widened fragment leaves its codes' registers at once
                     if (j == (WIDE ? 0 : NN - 1))
-                        fa[i % 2] = fetch_a(from, next), sxi[i % 2] = fetch_sx(from, next);
+                        fa[i % kDepth] = fetch_a(from, next), sxi[i % kDepth] = fetch_sx(from, next);
                     if constexpr (kSets == 1) {
                         if (i == NM - 1) next_b[j].set(fetch_b(then, j));
                     } else {
