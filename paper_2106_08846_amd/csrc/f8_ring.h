@@ -17,8 +17,8 @@
 //
 // MI355X, 8192^3: bf16 output 447 to 470 us, card by card (2.4 Pflop/s; the matrix units busy 61% of the
 // cycles at the 1.9 GHz that the power leaves them; the library's product with one scale takes 339).  fp32
-// output 1.35 Pflop/s, and with a scale for each row of B 1.1: there the vector instructions (12 and 18 to
-// four matrix instructions) and the matrix instructions take turns (with a scale for each row 47% and 42% of
+// output 1.35 Pflop/s, and with a scale for each row of B 1.16: there the vector instructions (12 and 15 to
+// four matrix instructions) and the matrix instructions take turns (with a scale for each row 43% and 45% of
 // the cycles).
 #pragma once
 
