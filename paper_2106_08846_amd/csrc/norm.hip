@@ -48,6 +48,12 @@ template <int WAVES> __device__ __forceinline__ float row_sum(float v, float *at
     return v;
 }
 
+// Whether element i of the vector at k is one of the row's K.  The sums ask: beyond the row's end a value
+// reads as 0, which may be far from the row's mean.
+template <int END> __device__ __forceinline__ bool in_row(int k, int i, int K) {
+    return END == kWholeSteps || (END == kWholeVectors ? k < K : k + i < K);
+}
+
 constexpr int kHeld = 8;       // load steps of a row that the forward pass holds in registers
 
 // WAVES waves per row, ROWS rows per workgroup, whose rows end as END says.  Rows
@@ -79,7 +85,7 @@ __global__ __launch_bounds__(64 * WAVES * ROWS) void norm_kernel(NormArgs a) {
         float q = 0.0f;
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
-            const float d = END == kWholeSteps || k + i < K ? v[i] - mean : 0.0f;
+            const float d = in_row<END>(k, i, K) ? v[i] - mean : 0.0f;
             q = fmaf(d, d, q);
         }
         return q;
@@ -246,7 +252,10 @@ __global__ __launch_bounds__(64 * WAVES * ROWS) void norm_backward_kernel(NormGr
 #pragma unroll
                     for (int i = 0; i < kVec; ++i) {
                         const float dy = to_float(now.d[b][s][i]);
-                        const float h = (to_float(now.x[b][s][i]) - now.mean[b]) * now.rstd[b];
+                        // beyond the row's end mean * rstd may be infinite, and 0 times it NaN
+                        const float h = in_row<END>(k0 + s * kSpan, i, K)
+                                            ? (to_float(now.x[b][s][i]) - now.mean[b]) * now.rstd[b]
+                                            : 0.0f;
                         dgamma[s][i] = fmaf(dy, h, dgamma[s][i]);
                         dbeta[s][i] += dy;
                         const float g = dy * gamma[s][i];
@@ -353,7 +362,7 @@ template <class T> __global__ __launch_bounds__(1024) void norm_dx_kernel(NormGr
         for (int k = k0; k < K; k += kSpan) {
             load(k, g, h);
 #pragma unroll
-            for (int i = 0; i < kVec; ++i) c1 += g[i], c2 = fmaf(g[i], h[i], c2);
+            for (int i = 0; i < kVec; ++i) c1 += g[i], c2 = fmaf(g[i], in_row<kAnyEnd>(k, i, K) ? h[i] : 0.0f, c2);
         }
         c1 = row_sum<16>(c1, red[parity][0]) / float(K);
         c2 = row_sum<16>(c2, red[parity][1]) / float(K);

@@ -166,6 +166,27 @@ def test_offset_rows_keep_their_variance():
     assert abs(float(Y.double().std()) - float(want.std())) < 0.01
 
 
+@pytest.mark.parametrize("T,K", [(3, 5), (5, 200), (9, 768), (2100, 520), (5, 1030), (5, 1032), (7, 2056),
+                                 (3, 4500), (3, 4504), (2, 16380), (2, 20000), (2, 20001)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("affine", [True, False])
+def test_gradients_of_a_large_constant_row(T, K, dtype, affine):
+    """A row of 2^110 among ordinary ones, with eps 2^-40: its sum K 2^110 is exact, so mean is 2^110, rstd 2^20
+    and h 0 at every column.  mean * rstd is beyond fp32, and nothing but the row's own columns, whose
+    deviations are 0, may meet it."""
+    rng = np.random.default_rng(T + K)
+    x, dy, gamma, _ = operands(rng, T, K, dtype, affine)
+    ds = rand(rng, T, K, dtype=dtype)
+    x[1] = 2.0 ** 110
+    Y, S, mean, rstd = B.bsr_layer_norm(dev(x), dev(gamma), eps=2.0 ** -40, save=True)
+    assert not bool(Y[1].any()) and float(mean[1]) == 2.0 ** 110 and float(rstd[1]) == 2.0 ** 20
+    got = B.bsr_layer_norm_backward(dev(dy), S, mean, rstd, dev(gamma), dS=dev(ds), grad_dtype=torch.float32)
+    want = N.backward(f64(dy), f64(x), f64(mean), f64(rstd), None if gamma is None else gamma.numpy(),
+                      f64(ds), dtype)
+    for name, g in zip(("dX", "dgamma", "dbeta"), got):
+        within(g, *want[name], name)
+
+
 def test_long_offsets():
     """Rows beyond 2^31 elements from the first."""
     T, K, pitch = 2200, 72, 1 << 20
