@@ -187,6 +187,35 @@ def test_gradients_of_a_large_constant_row(T, K, dtype, affine):
         within(g, *want[name], name)
 
 
+@pytest.mark.parametrize("T,K,step", [(3, 64, 2.0 ** -8), (5, 512, 2.0 ** -5), (4, 768, 2.0 ** -4),
+                                      (3, 1531, 2.0 ** -3), (3, 4096, 2.0 ** -2), (2100, 4096, 2.0 ** -2),
+                                      (3, 5000, 0.5), (2, 32768, 2.0), (2, 70001, 8.0)])
+def test_statistics_far_from_zero(T, K, step):
+    """Rows of 1000 (1000 to within a step where that is not one) and up to four steps to either side, with
+    steps so large that K times the largest value is below 2^24 of them: every sum of a row's values is
+    exact, in any order, so the mean is off by its quotient's rounding alone, half a step of fp32 below
+    1024 (2^-15).  Deviations and outputs follow it to fp32's rounding."""
+    rng = np.random.default_rng(K)
+    x = 1000.0 // step * step + rng.integers(-4, 5, (T, K)) * step
+    assert np.max(np.abs(x)) * K < 2 ** 24 * step and np.all(x.astype(np.float32) == x)
+    Y, _, mean, rstd = B.bsr_layer_norm(torch.from_numpy(x.astype(np.float32)).to(DEV), save=True)
+    m = x.mean(1)
+    e_mean = 2.0 ** -15
+    assert np.all(np.abs(f64(mean) - m) <= e_mean)
+    d = x - m[:, None]
+    var = (d * d).mean(1)
+    # from a mean off by e: n (var + e^2) in squares; each deviation and square rounds once, as their sums do
+    e_var = e_mean ** 2 + (N.depth(K) + 4) * N.U32 * (var + e_mean ** 2)
+    want = 1.0 / np.sqrt(var + 1e-5)
+    r = np.sqrt((var + 1e-5) / (var + 1e-5 - e_var)) - 1.0 + 4 * N.U32
+    assert np.all(np.abs(f64(rstd) - want) <= want * r)
+    h = d * want[:, None]
+    e_d = e_mean + N.U32 * (np.abs(d) + e_mean)
+    bound = e_d * (want * (1 + r))[:, None] + np.abs(h) * (r + 2 * N.U32)[:, None]
+    assert np.max(bound) < 0.01 * np.std(h)          # a shift of the row would show
+    within(Y, h, bound, "Y")
+
+
 def test_long_offsets():
     """Rows beyond 2^31 elements from the first."""
     T, K, pitch = 2200, 72, 1 << 20
