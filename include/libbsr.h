@@ -681,13 +681,18 @@ LIBBSR_API bsr_status bsr_quantize_f8(const void *X, bsr_dtype x_dtype, int64_t 
 /*
  * The product of two matrices in 8-bit floating point with scales for blocks of 128:
  *   Y[t][n] = sum over blocks b of  sx[b][t] sw[b][n'] * (sum over k in b of Xq[t][k] Wq[n][k])  +  bias[n],
- * b = k / 128 and n' = n / w_block_rows.  Products and sums are fp32, in an order fixed by the sizes and by
- * whether rows of codes start on 16-byte boundaries (repeated calls are bitwise reproducible); sx * sw is
- * formed first, so where it lies below 2^-126 its bits are lost, and from 2^128 on it is infinite.  bf16
- * output is rounded once, from the sum with the bias, and may come from the 8-bit matrix instructions: of
- * every eight consecutive products they drop what lies below 2^-13 of the largest one's power of two (of a
- * sum of normally distributed products about 1.5e-5, where bf16 rounds by 4e-3).  fp32 output keeps every
- * product.
+ * b = k / 128 and n' = n / w_block_rows.  sx * sw is formed first, so where it lies below 2^-126 its bits are
+ * lost, and from 2^128 on it is infinite.  Products and sums are fp32, in an order fixed by T, N, K, y_dtype,
+ * w_block_rows, whether rows of codes start on 16-byte boundaries, and the device's number of CUs: repeated
+ * calls are bitwise reproducible, but a token's result is not that of the same token in a call with another T.
+ * fp32 output keeps every product.  bf16 output is rounded once, from the sum with the bias; it keeps every
+ * product where T <= 32 or ceil(T / 32) * ceil(N / 16) is at most the number of CUs.  Elsewhere its sums come
+ * from the 8-bit matrix instructions: with 2^e the largest power of two among the eight products of
+ * k = 8 i .. 8 i + 7 (the sum of the two codes' exponents, a subnormal code's being the format's least, -6 or
+ * -14; products of zero do not count), each of the eight is cut off, towards zero, below 2^(e - 13), so they
+ * lose less than 2^(e - 10) sx sw together.  Of a sum of normally distributed products that is about 1.5e-5,
+ * where bf16 rounds by up to 4e-3; where the large products of a group cancel, the small ones beside them may
+ * be lost.
  * With the codes and scales of bsr_quantize_f8 it is a layer's forward product (X by rows, W in blocks of
  * 128 rows), its way back to the inputs (dY by rows, W's transpose), and the gradient of W (dY's and X's
  * transposes with a scale for each row: w_block_rows = 1).

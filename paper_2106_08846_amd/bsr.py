@@ -1295,7 +1295,9 @@ def bsr_matmul_f8(Xq: torch.Tensor, sx: torch.Tensor, Wq: torch.Tensor, sw: torc
     """Y = X W^T + bias from 8-bit floating point in blocks of 128 (bsr_matmul_f8): Xq [T, K]
     float8_e4m3fn or float8_e5m2 with sx fp32 [ceil(K / 128), T]; Wq [N, K] float8_e4m3fn with sw fp32
     [ceil(K / 128), ceil(N / 128)] (a weight) or [ceil(K / 128), N] (a scale for each row); bias fp32 [N]; Y
-    [T, N] float32 or bfloat16 (out_dtype, when Y is None)."""
+    [T, N] float32 or bfloat16 (out_dtype, when Y is None).  float32 keeps every product; of bfloat16
+    beyond few tokens the 8-bit matrix instructions drop what lies 13 binary places below the largest of
+    eight products (libbsr.h has the bound)."""
     ldx = _matrix_arg(Xq, "Xq", None, None, _F8_DTYPES)
     T, K = Xq.shape
     ldw = _matrix_arg(Wq, "Wq", None, K, _F8_DTYPES[:1])

@@ -363,6 +363,34 @@ def test_products_beside_a_large_one(out):
             assert bool((y == (2.0 ** -s if kept else 0.0)).all()), (s, at)
 
 
+@pytest.mark.parametrize("x_fmt,x0,w0,cut", [
+    ("e4m3", 1.75, 1.75, -13),                         # 2^0 2^0, less 13: the fractions do not count
+    ("e4m3", 2.0 ** -9, 448.0, -11), ("e4m3", 448.0, 2.0 ** -9, -11),     # 2^-6 2^8
+    ("e5m2", 57344.0, 2.0 ** -9, -4),                  # 2^15 2^-6
+    ("e4m3", 0.0, 448.0, None), ("e4m3", 448.0, 0.0, None), ("e5m2", 57344.0, 0.0, None)])
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [20, 512])
+def test_products_beside_a_large_subnormal_or_zero(x_fmt, x0, w0, cut, out, T):
+    """x0 w0 - x0 w0 + 2^s in one group of eight: the 8-bit instructions that make bf16 output in tiles keep 2^s
+    from 2^-13 of the pair's exponents on, where a subnormal code's exponent is its format's least normal
+    one; beside products of zero they keep it all.  So do fp32 output and the kernel for few tokens.  The
+    sums of two groups side by side (2^s at 8) meet with the 24 bits of fp32: from 2^-24 of those exponents
+    on, 11 places further down."""
+    N = 512
+    ones_x, ones_w = torch.ones(1, T, device=DEV), torch.ones(1, N, device=DEV)
+
+    def rows(n, fmt, at, *v):
+        q = np.zeros((n, 128), np.uint8)
+        q[:, [0, 1, at]] = F.encode(np.array(v, np.float32), fmt)
+        return codes(q, fmt)
+    for s in range(-16, 0):
+        for at in (2, 7, 8, 100):
+            y = B.bsr_matmul_f8(rows(T, x_fmt, at, x0, -x0, 2.0 ** (s // 2)), ones_x,
+                                rows(N, "e4m3", at, w0, w0, 2.0 ** (s - s // 2)), ones_w, out_dtype=TORCH[out])
+            least = -99 if out == "f32" or T == 20 or cut is None else {2: cut, 7: cut, 8: cut - 11, 100: -99}[at]
+            assert bool((y == (2.0 ** s if s >= least else 0.0)).all()), (s, at)
+
+
 @pytest.mark.parametrize("T,N,K", [(1000003, 24, 64), (40, 100003, 48), (70001, 72, 130)])
 @pytest.mark.parametrize("out", ["f32", "bf16"])
 def test_matmul_long_and_narrow(T, N, K, out):
