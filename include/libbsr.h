@@ -699,7 +699,7 @@ LIBBSR_API bsr_status bsr_quantize_f8(const void *X, bsr_dtype x_dtype, int64_t 
  * Xq: device, T x K codes of x_format, row pitch ldx >= K; sx: device fp32, ceil(K / 128) x T, pitch ldsx.
  * Wq: device, N x K codes of BSR_E4M3, row pitch ldw >= K; sw: device fp32, ceil(K / 128) x
  *   ceil(N / w_block_rows), pitch ldsw; w_block_rows 1 or 128.  bias: device fp32[N] or NULL.
- *   Rows that start on 16-byte boundaries load faster.
+ *   Rows that start on 16-byte boundaries (first row and pitch, of a single row too) load faster.
  * Y: device, T x N of y_dtype (BSR_F32 or BSR_BF16), row pitch ldy >= N; must not overlap an input.
  * T = 0 is a no-op; N, K >= 1.
  * Errors: BSR_ERR_NULL, BSR_ERR_SHAPE, BSR_ERR_ARG (unknown dtype or format, w_block_rows, overlap),

@@ -15,8 +15,9 @@
 // PARTS: so many groups of WM x WN waves share out the blocks of a contraction, each with stages of its own,
 // and add their sums at the end.
 //
-// MI355X, 8192^3: bf16 output 447 to 470 us, card by card (2.4 Pflop/s; the matrix units busy 61% of the
-// cycles at the 1.9 GHz that the power leaves them; the library's product with one scale takes 339).  fp32
+// MI355X, 8192^3: bf16 output 447 to 474 us, card by card (2.3 to 2.5 Pflop/s, at the 1.9 GHz that the power
+// leaves; matrix and vector instructions take 61% and 41% of the cycles and hardly overlap; the library's
+// product with one scale takes 339).  fp32
 // output 1.35 Pflop/s, and with a scale for each row of B 1.16: there the vector instructions (12 and 15 to
 // four matrix instructions) and the matrix instructions take turns (with a scale for each row 43% and 45% of
 // the cycles).

@@ -5,9 +5,10 @@
 // taken before the deviations: two sums in turn over registers cost nothing beside the loads, and a row far
 // from zero keeps its variance.
 //
-// MI355X, 8192 x 4096 bf16 (268 MB in all): forward with R and S 50 us (5.3 TB/s), backward with dS 53 (5.1
-// TB/s); a large copy moves 5.17 TB/s.  One row of 1024 fp32 takes 2.1 us, a memory latency, two sums over a
-// wave and the two ends of a kernel.
+// MI355X, 8192 x 4096 bf16 (268 MB in all) on inputs that no cache holds: forward with R and S 57 us (4.7
+// TB/s), backward with dS and the join of the sums 60 (4.5 TB/s); on the same inputs again 40 and 48, partly
+// from the memory-side cache.  A large copy moves 5.17 TB/s.  One row of 1024 fp32 takes 1.9 us, a memory
+// latency, two sums over a wave and the two ends of a kernel.
 #include "row_vec.h"
 
 namespace bsr {
@@ -195,7 +196,9 @@ struct NormGradArgs {
 template <class T, int WAVES, int ROWS, int END>
 __global__ __launch_bounds__(64 * WAVES * ROWS) void norm_backward_kernel(NormGradArgs a) {
     constexpr int kSteps = 2, kSpan = 64 * WAVES * kVec, kWidth = kSteps * kSpan;
-    // Two rows of bf16 in flight; fp32 and sixteen waves have registers for one.
+    // Two rows of bf16 in flight; fp32 and sixteen waves have registers for one.  (fp32 rows on sixteen waves
+    // that end off a load step keep two to five registers of a lane in memory all the same: 2000 x 5000 with dS
+    // takes 42 us, 3.8 TB/s.)
     constexpr int kBatch = WAVES > 4 || sizeof(T) > 2 ? 1 : 2;
     __shared__ float red[2][2 * kBatch][ROWS][WAVES];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, K = a.K;
@@ -232,7 +235,8 @@ __global__ __launch_bounds__(64 * WAVES * ROWS) void norm_backward_kernel(NormGr
     };
     // The next rows are loaded before this round's sums are joined, where the registers hold them and no lane
     // asks for the end of its row: 8192 x 4096 bf16 with dS takes this kernel 49 us so and 55 without
-    // (2048 x 8192 on sixteen waves 34 and 33).
+    // (2048 x 8192 on sixteen waves 34 and 33).  Rows that end within a vector cost more than that: 777 x 1531
+    // fp32 takes 11.4 us and 777 x 1528 8.4, on inputs that no cache holds.
     constexpr bool kAhead = END != kAnyEnd && WAVES <= 4;
     Batch next = {};
     if (kAhead) fetch(int64_t(blockIdx.x) * ROWS, next);

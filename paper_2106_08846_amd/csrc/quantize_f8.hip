@@ -97,8 +97,9 @@ template <int N, class F> __device__ __forceinline__ void each(F &&f) {
     each(std::make_integer_sequence<int, N>{}, f);
 }
 
-// By rows, blocks of 1 x 128: 16 rows of 512 columns to a workgroup, four rows to a wave, all loaded at
-// once.  The scales of one block lie side by side for the rows, so they are stored 16 at a time.
+// By rows, blocks of 1 x 128: 16 rows of 512 columns to a workgroup, four rows to a wave.  A wave's rows arrive
+// partly in turn, bf16 ones wholly, since each is converted where its end is checked: many waves hide that, few
+// do not.  The scales of one block lie side by side for the rows, so they are stored 16 at a time.
 constexpr int kStripRows = 16, kStripColumns = 64 * kVec;
 template <class T, int FMT> __global__ __launch_bounds__(kThreads) void quantize_strip_kernel(QuantizeArgs a) {
     constexpr int kRows = 4, kBlocks = kStripColumns / kF8Block;
@@ -137,8 +138,9 @@ template <class T, int FMT> __global__ __launch_bounds__(kThreads) void quantize
         a.scale[(c0 / kF8Block + b) * a.ldscale + t0 + i] = scales[b][i];
 }
 
-// Tiles of 128 x 128: a thread holds 8 rows of 8 columns.  ROWS: rows of a block by rows (1 or 128),
-// which is the width of one by columns.
+// Tiles of 128 x 128: a thread holds 8 rows of 8 columns, loaded as the rows above (2304 x 768 in blocks of 128
+// x 128, 108 tiles, takes 7.3 us as fp32 and 9.5 as bf16).  ROWS: rows of a block by rows (1 or 128), which is
+// the width of one by columns.
 template <class T, int FMT, int ROWS>
 __global__ __launch_bounds__(kThreads) void quantize_tile_kernel(QuantizeArgs a) {
     constexpr int kB = kF8Block, kWaves = kThreads / 64;
